@@ -30,7 +30,8 @@
  *    message of the last failing call on the calling thread is apex_last_error().
  *  - Supported sizes: 1 <= E <= 64 experts, 1 <= k <= k_max <= E, d and I multiples
  *    of 8 (16-byte rows of bf16), B >= 0 tokens (B = 0 enqueues nothing).
- *  - apex_prefetch_route, apex_gate_topk and the apex_moe_ffn entry points only launch
+ *  - apex_prefetch_route, apex_gate_topk, the apex_moe_ffn entry points and the paged-cache
+ *    entry points (apex_paged_plan, apex_paged_store, apex_attention_paged) only launch
  *    kernels on the given stream (no allocation, memory set, copy or synchronisation),
  *    so a caller may capture them in a HIP graph; apex_moe_ffn_noalloc's first call on
  *    a device looks up that device's scratch array and must come before the capture.
@@ -47,7 +48,7 @@
 extern "C" {
 #endif
 
-#define APEX_ABI_VERSION 4
+#define APEX_ABI_VERSION 5
 #define APEX_MAX_EXPERTS 64
 #define APEX_MAX_PAIRS 1024     /* B * k limit of apex_moe_ffn */
 
@@ -340,6 +341,131 @@ apex_status apex_attention_decode(const float *h, const uint16_t *w_qkv, const u
                                   int B, int d, int H, int G, int hd, uint16_t *k_cache,
                                   uint16_t *v_cache, int ctx_max, int pos, float *o,
                                   void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Paged key/value cache: requests of different lengths in one pool of pages.  Per model step
+ *   apex_paged_plan       gives the new tokens their pages and slots (once for all layers);
+ * and per layer, behind the projections and rotary positions of the caller,
+ *   apex_paged_store      writes the new keys and values into their slots;
+ *   apex_attention_paged  attention of the new tokens over their requests' pages.
+ * The block is the one of apex_attention_decode (grouped-query attention, query head i uses
+ * key/value head i / (H / G)) for requests of any lengths, chunks of several tokens and windows.
+ *
+ * A position of a request lives in page block_table[r, j / page_size] at offset
+ * j mod page_size; its slot is page * page_size + offset.  Pools of keys and of values:
+ *   APEX_KV_BF16      k_pages, v_pages  device bf16 [n_pages, G, page_size, hd]; no scales
+ *   APEX_KV_FP8_E4M3  k_pages, v_pages  device E4M3 codes, one byte each, of the same shape,
+ *                     k_scales, v_scales  device fp32 [n_pages, G, page_size]: row r of a key or
+ *                     value is s_r * q as in apex_pack_expert_fp8
+ * The struct is read during the call only.  page_size: a power of two from 16 to 1024; hd 64 or
+ * 128; n_pages * page_size < 2^31; all pointers 16-byte aligned.
+ */
+typedef enum {
+    APEX_TYPE_FP32 = 0,
+    APEX_TYPE_BF16 = 1
+} apex_type;
+
+typedef enum {
+    APEX_KV_BF16 = 0,
+    APEX_KV_FP8_E4M3 = 1
+} apex_kv;
+
+typedef struct {
+    int format;                     /* apex_kv */
+    int G, hd, page_size, n_pages;
+    void *k_pages, *v_pages;
+    float *k_scales, *v_scales;     /* APEX_KV_FP8_E4M3 only; NULL otherwise */
+} apex_paged_cache;
+
+#define APEX_MAX_REQUESTS 4096
+#define APEX_MAX_STEP_TOKENS (1 << 20)   /* T of apex_attention_paged */
+
+/* Outcomes of apex_paged_plan for a request. */
+typedef enum {
+    APEX_REQ_SERVED = 0,   /* its new tokens (none, perhaps) have slots                       */
+    APEX_REQ_ENDED = 1,    /* n_new = -1: its pages were given back                           */
+    APEX_REQ_WAITS = 2,    /* no pages or rows left for it: none of its tokens has a slot     */
+    APEX_REQ_INVALID = 3   /* cached < 0, n_new < -1 or more positions than its table row has */
+} apex_request_status;
+
+/*
+ * Pages, slots and lengths of one step from the requests' lengths, on the GPU (the host needs
+ * to know none of them).  Request r holds cached[r] positions in the first
+ * ceil(cached[r] / page_size) pages of its table row and wants n_new[r] more.
+ *   1. Requests with n_new = -1 have ended: in ascending r, their pages are pushed onto the
+ *      stack of free pages in the order of their table rows (which stay as they are).
+ *   2. In ascending r, every other valid request takes the pages it lacks from the top of the
+ *      stack into the next entries of its table row.  The first request whose pages or tokens
+ *      do not fit (more pages than are free, or a total of more than T tokens) waits, and so
+ *      does every later one that wants tokens.
+ *   3. seq_len[r] = cached[r] + the tokens it was given (0 if ended); cu_new[r] = tokens given to
+ *      requests before r; token t = cu_new[r] + i has position cached[r] + i and its slot.
+ * The inputs cached, n_new and free_count are not changed, and a second call with the same ones
+ * gives the same results.  A page given back must be held by one request only.
+ *   cached, n_new    device int32 [R] (0 <= R <= APEX_MAX_REQUESTS)
+ *   free_pages       device int32 [n_pages] in/out: the stack, its top at free_count[0] - 1
+ *   free_count       device int32 [1]; taken as 0 or n_pages where it is outside of these
+ *   block_table      device int32 [R, max_blocks] in/out; a page id outside [0, n_pages) there
+ *                    or on the stack gives its positions the slot -1
+ *   seq_len          device int32 [R] out;  cu_new  device int32 [R + 1] out
+ *   slot_map         device int32 [T] out: -1 behind the last token
+ *   positions        device int32 [T] out, or NULL: -1 behind the last token
+ *   free_count_out   device int32 [1] out
+ *   status           device int32 [R] out, or NULL: apex_request_status
+ * No output may overlap an input or another output (equal pointers are refused).
+ */
+apex_status apex_paged_plan(const int32_t *cached, const int32_t *n_new, int R, int page_size,
+                            int n_pages, int max_blocks, int T, int32_t *free_pages,
+                            const int32_t *free_count, int32_t *block_table, int32_t *seq_len,
+                            int32_t *cu_new, int32_t *slot_map, int32_t *positions,
+                            int32_t *free_count_out, int32_t *status, hipStream_t stream);
+
+/*
+ * Keys and values of T tokens into their slots.  bf16 pools take bf16 rows as they are and fp32
+ * rows rounded to nearest even.  E4M3 pools take each row of hd values with a scale of its own,
+ * s = fp32(max |row| / 448), and codes q = row / s rounded to the nearest code (ties to the even
+ * one, never beyond 448): the codes and scales apex_pack_expert_fp8 gives a row.  A row of
+ * zeros, or one so small that s rounds to 0, has s = 0 and codes 0; a row with a NaN or an
+ * infinity has a NaN scale, so that its position reads as NaN.
+ *   k, v        device, type `dtype` (apex_type): token t's row [G, hd] at k + t * k_stride;
+ *               strides in values, at least G * hd and multiples of 16 bytes
+ *   slot_map    device int32 [T]: tokens whose slot is outside [0, n_pages * page_size) are
+ *               left out.  Slots must differ: of tokens with one slot, any may stay there.
+ */
+apex_status apex_paged_store(const apex_paged_cache *cache, const void *k, const void *v, int dtype,
+                             int T, int64_t k_stride, int64_t v_stride, const int32_t *slot_map,
+                             hipStream_t stream);
+
+/*
+ * Attention of new tokens over the paged cache, which already holds their own keys and values.
+ * Row t = cu_new[r] + i of request r stands at p = seq_len[r] - (cu_new[r+1] - cu_new[r]) + i and
+ *   out[t, h] = sum_j softmax_j(scale * q[t, h] . K_g[j]) V_g[j],  g = h / (H / G),
+ * over the positions 0 <= j <= p with window == 0, or j > p - window, or j < sinks (a sliding
+ * window of the last `window` positions besides which the first `sinks` stay visible).
+ * Positions in a page whose id is outside [0, n_pages) are left out too; a row that sees
+ * nothing becomes 0.  Whatever keys and values hold at positions a row does not see (NaN
+ * included) does not reach it.  Table entries and pages that no row sees are not read, so
+ * pages that left a window may be reused.  Rows before cu_new[0] and from cu_new[R] on are
+ * left as they are.
+ * Arithmetic: products on the matrix cores, sums, maxima and normalisers in fp32.  dtype
+ * APEX_TYPE_BF16: the softmax weights are rounded to bf16 for the second product, and the
+ * result once to bf16.  APEX_TYPE_FP32: no operand is rounded (fp32 values go through the
+ * matrix cores in three pieces, three times the work).  No atomics: results are deterministic.
+ *   q, out       device, type `dtype`: row t's [H, hd] at q + t * q_stride; strides in values,
+ *                at least H * hd and multiples of 16 bytes; out may be q (same stride)
+ *   cu_new, seq_len, block_table [R, max_blocks]   as apex_paged_plan leaves them
+ *   T            rows of q and out (at least cu_new[R]), at most APEX_MAX_STEP_TOKENS
+ *   H            a multiple of cache->G with H / G <= 16
+ *   window, sinks  >= 0;  scale  > 0 and finite (1 / sqrt(hd) as a rule)
+ *   workspace    device, >= apex_attention_paged_workspace_bytes(T, R, H, G, hd) bytes; must
+ *                not be shared by calls that may overlap
+ */
+size_t apex_attention_paged_workspace_bytes(int T, int R, int H, int G, int hd);
+apex_status apex_attention_paged(const apex_paged_cache *cache, const void *q, int dtype, int T,
+                                 int R, int H, int64_t q_stride, const int32_t *cu_new,
+                                 const int32_t *seq_len, const int32_t *block_table, int max_blocks,
+                                 int window, int sinks, float scale, void *out, int64_t out_stride,
+                                 void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Cache plan of one layer for one decode step (pure host function, no HIP calls).

@@ -24,10 +24,15 @@ APEX_OK, APEX_E_INVAL, APEX_E_UNSUPPORTED, APEX_E_HIP, APEX_E_CAPACITY = 0, -1, 
 SEL_CUMPROB, SEL_ORDINAL_CDF, SEL_STATIC, SEL_NONE = 0, 1, 2, 3
 MODE_EXACT, MODE_STALL_FREE = 0, 1
 WEIGHTS_BF16, WEIGHTS_FP8_E4M3, WEIGHTS_MXFP4, WEIGHTS_FP32 = 0, 1, 2, 3
-ABI_VERSION = 4
+KV_BF16, KV_FP8_E4M3 = 0, 1
+TYPE_FP32, TYPE_BF16 = 0, 1
+REQ_SERVED, REQ_ENDED, REQ_WAITS, REQ_INVALID = 0, 1, 2, 3
+ABI_VERSION = 5
 MAX_EXPERTS = 64
 MAX_PAIRS = 1024
 NOALLOC_WORKSPACE_BYTES = 64 << 20
+MAX_REQUESTS = 4096
+MAX_STEP_TOKENS = 1 << 20
 
 
 class ApexError(RuntimeError):
@@ -71,6 +76,11 @@ class DecodeRecord(C.Structure):
         "pf_idx", "pf_count", "route_idx", "route_gate", "exec_idx", "exec_gate", "resident",
         "n_copies", "missing", "n_missing")]
 
+
+class PagedCache(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("format", "G", "hd", "page_size", "n_pages")] + [
+        (n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scales", "v_scales")]
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "apex_abi_version": (C.c_int, []),
@@ -96,6 +106,11 @@ SIGNATURES = {
     "apex_attention_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
     "apex_attention_decode": (I32, [P, P, P, I32, I32, I32, I32, I32, P, P, I32, I32, P, P, SZ,
                                     P]),
+    "apex_paged_plan": (I32, [P, P, I32, I32, I32, I32, I32, P, P, P, P, P, P, P, P, P, P]),
+    "apex_paged_store": (I32, [P, P, P, I32, I32, I64, I64, P, P]),
+    "apex_attention_paged_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
+    "apex_attention_paged": (I32, [P, P, I32, I32, I32, I32, I64, P, P, P, I32, I32, I32, F32, P,
+                                   I64, P, SZ, P]),
     "apex_plan_residency": (I32, [I32, I32, P, P, I32, I32, I64, P, P, P, P, P]),
     "apex_expert_prefetch": (I32, [P, P, I32, I32, SZ, P, P, I32, I32, I64, P, P, P, P, P, P, P,
                                    P, P, P]),
@@ -311,6 +326,52 @@ def apex_attention_decode(h, w_qkv, w_o, B, d, H, G, hd, k_cache, v_cache, ctx_m
                           workspace, workspace_bytes, stream=None):
     _call("apex_attention_decode", ptr(h), ptr(w_qkv), ptr(w_o), B, d, H, G, hd, ptr(k_cache),
           ptr(v_cache), ctx_max, pos, ptr(o), ptr(workspace), workspace_bytes, stream)
+
+
+KV_FORMATS = {"bf16": KV_BF16, "fp8": KV_FP8_E4M3}
+TYPES = {"fp32": TYPE_FP32, "bf16": TYPE_BF16}
+
+
+def _code(table, v):
+    return table[v] if isinstance(v, str) else int(v)
+
+
+def paged_cache(fmt, G, hd, page_size, n_pages, k_pages, v_pages, k_scales=None, v_scales=None):
+    """The apex_paged_cache of a pool.  fmt: an APEX_KV_* code or "bf16", "fp8".  Holds the
+    pools' addresses only: the caller keeps the pools alive."""
+    return PagedCache(_code(KV_FORMATS, fmt), G, hd, page_size, n_pages, ptr(k_pages), ptr(v_pages),
+                      ptr(k_scales), ptr(v_scales))
+
+
+def _ref(cache):
+    return None if cache is None else C.addressof(cache)
+
+
+def apex_paged_plan(cached, n_new, R, page_size, n_pages, max_blocks, T, free_pages, free_count,
+                    block_table, seq_len, cu_new, slot_map, positions, free_count_out, status,
+                    stream=None):
+    _call("apex_paged_plan", ptr(cached), ptr(n_new), R, page_size, n_pages, max_blocks, T,
+          ptr(free_pages), ptr(free_count), ptr(block_table), ptr(seq_len), ptr(cu_new),
+          ptr(slot_map), ptr(positions), ptr(free_count_out), ptr(status), stream)
+
+
+def apex_paged_store(cache, k, v, dtype, T, k_stride, v_stride, slot_map, stream=None):
+    """dtype: an APEX_TYPE_* code or "fp32", "bf16"."""
+    _call("apex_paged_store", _ref(cache), ptr(k), ptr(v), _code(TYPES, dtype), T, k_stride, v_stride,
+          ptr(slot_map), stream)
+
+
+def apex_attention_paged_workspace_bytes(T, R, H, G, hd):
+    return lib().apex_attention_paged_workspace_bytes(T, R, H, G, hd)
+
+
+def apex_attention_paged(cache, q, dtype, T, R, H, q_stride, cu_new, seq_len, block_table, max_blocks,
+                         window, sinks, scale, out, out_stride, workspace, workspace_bytes,
+                         stream=None):
+    """dtype: an APEX_TYPE_* code or "fp32", "bf16"."""
+    _call("apex_attention_paged", _ref(cache), ptr(q), _code(TYPES, dtype), T, R, H, q_stride,
+          ptr(cu_new), ptr(seq_len), ptr(block_table), max_blocks, window, sinks, scale, ptr(out),
+          out_stride, ptr(workspace), workspace_bytes, stream)
 
 
 def apex_plan_residency(E, Cslots, pf_idx, pf_count, B, k_max, step, expert_of_slot, last_used,

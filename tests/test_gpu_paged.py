@@ -1,0 +1,550 @@
+"""Paged-cache operators against the float64 oracle.
+
+Attention tolerances.  Per output, with size = sum of weight * |value| and peak = the largest sum of
+|scale q k| of a visible position: a score is off by at most (hd + 8) roundings of 2^-24 of its
+peak, a weight by twice that (numerator and normaliser) and 32-bit sums by less than 2^-16 of `size`
+(64 positions at a time, the rest in tree order over wavefronts and splits).  bf16 adds half a step,
+2^-8, of every weight (of `size`) and of the output.  That bound is for each output.  Roundings
+are independent, so that over all outputs the 2-norm of the error is much smaller: 2e-6 of the
+result's with fp32, where a dropped 8-bit piece of an operand would leave 4e-6 and more, and with
+bf16 two roundings of rms 2^-8 / sqrt(3) * 0.72 = 1.6e-3 each, 2.3e-3 together, at most 4e-3.
+"""
+import numpy as np
+import pytest
+
+from oracle import fp8
+from oracle import paged as opaged
+from oracle.attention import round_bf16
+from paper_2608_11688_amd import native
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available()
+    native.lib()
+    return t
+
+
+def i32(torch, a):
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+def cdiv(a, b):
+    return -(-a // b)
+
+
+class Case:
+    """Requests of given total and new lengths over a pool of scattered pages."""
+
+    def __init__(self, torch, lens, new, H, G, hd, page, fmt, dtype, pad=0, seed=0, extra_q=0):
+        self.torch, self.H, self.G, self.hd, self.page, self.fmt, self.dtype = torch, H, G, hd, page, fmt, dtype
+        rng = np.random.default_rng(seed)
+        self.rng, self.R = rng, len(lens)
+        self.lens, self.new = np.array(lens), np.array(new)
+        self.cu = np.concatenate([[0], np.cumsum(new)])
+        self.T = int(self.cu[-1]) + pad
+        blocks = [cdiv(n, page) for n in lens]
+        self.n_pages, self.nb = sum(blocks) + 3, max(blocks + [1]) + 1
+        order = rng.permutation(self.n_pages)
+        self.table, at = np.full((self.R, self.nb), -1), 0
+        for r, b in enumerate(blocks):
+            self.table[r, :b] = order[at:at + b]
+            at += b
+        shape = (self.n_pages, G, page, hd)
+        self.k, self.v = rng.standard_normal((2,) + shape)
+        self.ks = self.vs = None
+        if fmt == "bf16":
+            self.k, self.v = round_bf16(self.k), round_bf16(self.v)
+        else:
+            self.ks, self.vs = (rng.random((2,) + shape[:3]) * 0.01 + 0.005).astype(np.float32)
+            self.k, self.v = fp8.encode(self.k * 100), fp8.encode(self.v * 100)
+        q = 2 * rng.standard_normal((self.T, H, hd))
+        self.q = round_bf16(q) if dtype == "bf16" else q.astype(np.float32).astype(np.float64)
+        self.extra_q = extra_q
+
+    def type(self):
+        return self.torch.bfloat16 if self.dtype == "bf16" else self.torch.float32
+
+    def pool(self, x):
+        t = self.torch.from_numpy(np.ascontiguousarray(x))
+        return t.cuda() if self.fmt == "fp8" else t.cuda().to(self.torch.bfloat16)
+
+    def values(self):
+        if self.fmt == "bf16":
+            return self.k, self.v
+        return (fp8.decode_array(self.k) * self.ks[..., None].astype(np.float64),
+                fp8.decode_array(self.v) * self.vs[..., None].astype(np.float64))
+
+    def device(self):
+        torch = self.torch
+        f = lambda s: None if s is None else torch.from_numpy(s).cuda()
+        self.dk, self.dv, self.dks, self.dvs = self.pool(self.k), self.pool(self.v), f(self.ks), f(self.vs)
+        self.cache = native.paged_cache(self.fmt, self.G, self.hd, self.page, self.n_pages, self.dk, self.dv,
+                                        self.dks, self.dvs)
+        wide = torch.full((self.T, self.H * self.hd + self.extra_q), 3.0, dtype=self.type(), device="cuda")
+        wide[:, :self.H * self.hd] = torch.from_numpy(self.q.reshape(self.T, -1)).cuda().to(self.type())
+        self.dq = wide[:, :self.H * self.hd]
+        self.out = torch.full((self.T, self.H * self.hd + self.extra_q), 7.0, dtype=self.type(), device="cuda")
+        self.dcu, self.dseq, self.dtable = (i32(torch, x) for x in (self.cu, self.lens, self.table))
+        n = native.apex_attention_paged_workspace_bytes(self.T, self.R, self.H, self.G, self.hd)
+        self.ws = torch.full((n,), 0xAB, dtype=torch.uint8, device="cuda")
+
+    def call(self, window=0, sinks=0, scale=None, stream=None, out=None):
+        out = self.out if out is None else out
+        native.apex_attention_paged(self.cache, self.dq, self.dtype, self.T, self.R, self.H, self.dq.stride(0),
+                                    self.dcu, self.dseq, self.dtable, self.nb, window, sinks,
+                                    scale or self.hd ** -0.5, out, out.stride(0), self.ws, self.ws.numel(), stream)
+
+    def check(self, window=0, sinks=0, norm=True):
+        self.device()
+        self.call(window, sinks)
+        self.torch.cuda.synchronize()
+        wide = self.out.double().cpu().numpy()
+        assert (wide[:, self.H * self.hd:] == 7).all()                 # between the rows
+        got = wide[:, :self.H * self.hd].reshape(self.T, self.H, self.hd)
+        k, v = self.values()
+        with np.errstate(invalid="ignore", over="ignore"):
+            want, size, peak = opaged.attend(self.q, k, v, self.cu, self.lens, self.table, window, sinks,
+                                             self.hd ** -0.5, np.full_like(got, 7.0))
+        return compare(got, want, size, peak, self.hd, self.dtype, norm)
+
+
+def compare(got, want, size, peak, hd, dtype, norm=True):
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    step = 2.0 ** -8 if dtype == "bf16" else 0.0
+    bound = size * (2 * (hd + 8) * 2.0 ** -24 * peak[..., None] + 2.0 ** -16 + step) + np.abs(want) * (step + 2.0 ** -22)
+    err = np.abs(got - want)
+    assert (err[ok] <= bound[ok] + 1e-30).all(), (err[ok] - bound[ok]).max()
+    rel = np.linalg.norm(err[ok]) / max(np.linalg.norm(want[ok]), 1e-30)
+    if norm:
+        assert rel <= (4e-3 if dtype == "bf16" else 2e-6), rel
+    return rel
+
+
+FORMATS = [("bf16", "bf16"), ("fp8", "bf16"), ("bf16", "fp32"), ("fp8", "fp32")]
+FMT_IDS = ["-".join(f) for f in FORMATS]
+
+# single tokens: total lengths of the requests, H, G, hd, page, window, sinks
+TOKENS = [
+    ([1], 1, 1, 64, 16, 0, 0),                       # nothing cached but its own position
+    ([2, 17, 16, 33], 6, 2, 128, 16, 0, 0),          # ends at, before and behind a page's end
+    ([129, 127, 500], 8, 8, 64, 32, 0, 0),           # one query head per group
+    ([300, 1, 700, 64], 20, 4, 128, 64, 0, 0),       # five heads per group
+    ([1500], 7, 1, 64, 1024, 0, 0),                  # seven, one long page
+    ([2100, 900], 16, 1, 128, 128, 0, 0),            # sixteen
+    ([400, 90, 10], 8, 2, 128, 16, 50, 4),           # window with sinks, contexts under and over it
+    ([400, 90, 10], 8, 2, 64, 32, 1, 0),             # a window of the token itself
+    ([400, 300], 8, 2, 64, 16, 37, 130),             # sinks past a unit
+    ([200, 60], 4, 1, 128, 16, 150, 100),            # sinks that reach into the window
+    ([777], 6, 2, 128, 256, 256, 1),
+]
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("lens,H,G,hd,page,window,sinks", TOKENS, ids=[str(c) for c in TOKENS])
+def test_single_tokens(torch, lens, H, G, hd, page, window, sinks, fmt, dtype):
+    c = Case(torch, lens, [1] * len(lens), H, G, hd, page, fmt, dtype, seed=1)
+    print(c.check(window, sinks))
+
+
+# chunks: (total, new) of the requests, H, G, hd, page, window, sinks, rows behind the last
+CHUNKS = [
+    ([(2, 2)], 1, 1, 64, 16, 0, 0, 0),
+    ([(5, 3), (40, 7)], 4, 2, 128, 16, 0, 0, 2),
+    ([(130, 130)], 4, 1, 64, 16, 0, 0, 0),                       # a whole prompt
+    ([(64, 64), (65, 33), (129, 128)], 2, 2, 128, 64, 0, 0, 0),  # at the units' edges
+    ([(300, 77), (1, 1), (90, 0), (200, 12)], 10, 2, 64, 32, 0, 0, 5),   # single, none, chunks; five heads
+    ([(333, 100)], 16, 1, 128, 128, 0, 0, 0),                    # eight tokens a tile
+    ([(300, 200)], 7, 1, 64, 16, 0, 0, 1),                       # 18 tokens and two empty rows a tile
+    ([(260, 150), (70, 70)], 4, 1, 128, 16, 40, 5, 0),           # window inside a tile, sinks
+    ([(500, 30), (33, 9)], 6, 2, 64, 32, 7, 0, 3),
+    ([(400, 64)], 4, 2, 128, 256, 100, 70, 0),                   # sinks past a unit
+    ([(1200, 6)], 2, 1, 64, 16, 0, 0, 0),                        # few rows, many units: split
+    ([(700, 600)], 1, 1, 128, 512, 0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("reqs,H,G,hd,page,window,sinks,pad", CHUNKS, ids=[str(c) for c in CHUNKS])
+def test_chunks(torch, reqs, H, G, hd, page, window, sinks, pad, fmt, dtype):
+    c = Case(torch, [r[0] for r in reqs], [r[1] for r in reqs], H, G, hd, page, fmt, dtype, pad=pad, seed=2,
+             extra_q=8 * pad)
+    print(c.check(window, sinks))
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("new", [1, 6])
+def test_pages_with_ids_out_of_range_are_left_out(torch, new, fmt, dtype):
+    c = Case(torch, [200, 150, 40], [new] * 3, 4, 2, 64, 16, fmt, dtype, seed=3)
+    c.table[0, [0, 5, 12]] = [-1, c.n_pages, 2 ** 31 - 1]   # the first, an inner one, its last
+    c.table[1, 3] = -2 ** 31
+    c.table[2, :] = -7                                       # sees nothing: zeros
+    c.check()
+    assert (c.out[2 * new:] == 0).all()
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("new,window,sinks", [(1, 0, 0), (1, 20, 3), (9, 0, 0), (9, 20, 3), (70, 33, 5)])
+def test_what_a_row_does_not_see_does_not_reach_it(torch, new, window, sinks, fmt, dtype):
+    """NaN and infinities behind the last position, under the window, in the first positions'
+    shadow and at later tokens of the same chunk."""
+    c = Case(torch, [150, 37 + new], [new, new], 4, 2, 128, 16, fmt, dtype, seed=4)
+    bad = np.float32("nan")
+
+    def spoil(pid, off):
+        if fmt == "fp8":
+            c.v[pid, :, off, 5], c.k[pid, :, off, 9] = 0x7F, 0xFF
+            c.vs[pid, :, off] = c.ks[pid, :, off] = bad if off % 2 else np.inf
+        else:
+            c.v[pid, :, off, 5], c.v[pid, :, off, 70], c.k[pid, :, off, 9] = np.inf, bad, -np.inf
+
+    for r in range(2):
+        n = int(c.lens[r])
+        last = n - (new + 1) // 2 if new > 1 else n              # from here on only later tokens see it
+        first = n - new
+        for j in range(c.nb * 16):
+            pid = c.table[r, j // 16]
+            if pid >= 0 and (j >= last or (window and sinks <= j <= first - window)):
+                spoil(pid, j % 16)
+    free = sorted(set(range(c.n_pages)) - set(c.table.ravel()))
+    for pid in free:
+        for off in range(16):
+            spoil(pid, off)
+    # rows that see a spoiled position are NaN (or infinite) by their own right: not compared
+    k, v = c.values()
+    c.device()
+    c.call(window, sinks)
+    torch.cuda.synchronize()
+    got = c.out.double().cpu().numpy().reshape(c.T, 4, 128)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want, size, peak = opaged.attend(c.q, k, v, c.cu, c.lens, c.table, window, sinks, 128 ** -0.5, got)
+    clean = np.isfinite(size).all(axis=(1, 2)) & np.isfinite(peak).all(axis=1)
+    assert clean.sum() >= 2 * (new // 2 if new > 1 else 1)
+    compare(got[clean], want[clean], size[clean], peak[clean], 128, dtype)
+    if new > 1:
+        assert not np.isfinite(got[~clean]).all()
+
+
+def test_a_nan_that_is_seen_is_nan(torch):
+    c = Case(torch, [50], [1], 2, 1, 64, 16, "bf16", "bf16", seed=5)
+    c.v[c.table[0, 1], 0, 3, 7] = np.nan
+    c.device()
+    c.call()
+    got = c.out.view(2, 64)
+    assert torch.isnan(got[:, 7]).all() and torch.isnan(got).sum() == 2
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_large_and_even_scores(torch, new, dtype):
+    """Scores that stand far apart (weights of one position only) and all equal ones."""
+    c = Case(torch, [333], [new], 4, 2, 64, 16, "bf16", dtype, seed=6)
+    c.q = round_bf16(c.q * 64)
+    c.check(norm=False)
+    c.q[:] = 0
+    c.check()
+
+
+def test_lengths_that_disagree_stay_inside(torch):
+    """Lengths shorter than the new tokens, past the table, no ascending list: zeros or clamped, no
+    access out of range (positions a token would have before 0 see nothing)."""
+    c = Case(torch, [40, 64, 48], [4, 2, 3], 2, 1, 64, 16, "bf16", "bf16", seed=7)
+    c.device()
+    c.dseq.copy_(i32(torch, [2, 10 ** 9, -5]))
+    c.call()
+    torch.cuda.synchronize()
+    assert (c.out[:2] == 0).all() and (c.out[2:4] != 0).any(dim=1).all()
+    assert (c.out[6:9] == 0).all()
+    c.dcu.copy_(i32(torch, [-3, 10 ** 9, 2, -1]))
+    c.call()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("new", [1, 33])
+def test_in_place_over_the_queries(torch, new):
+    c = Case(torch, [900, 300], [new, new], 4, 2, 64, 16, "bf16", "bf16", seed=8)
+    c.device()
+    c.call()
+    want = c.out.clone()
+    c.call(out=c.dq)
+    torch.cuda.synchronize()
+    assert torch.equal(c.dq, want)
+
+
+@pytest.mark.parametrize("lens,new", [([5000, 70, 1, 900], [1, 1, 1, 1]), ([3000, 200], [300, 1])])
+def test_repeated_calls_give_the_same_bits(torch, lens, new):
+    c = Case(torch, lens, new, 8, 2, 128, 32, "bf16", "bf16", seed=9)
+    c.device()
+    c.call()
+    first = c.out.clone()
+    for _ in range(3):
+        c.ws.fill_(0x55)
+        c.call()
+        assert torch.equal(c.out, first)
+
+
+def test_an_answer_does_not_depend_on_the_rest_of_the_batch(torch):
+    """The same request alone and among others: split otherwise, the same within rounding."""
+    c = Case(torch, [2000, 300, 5], [1, 1, 1], 8, 2, 128, 32, "bf16", "fp32", seed=10)
+    c.check()
+    whole = c.out.clone()
+    c.R = c.T = 1
+    c.call()
+    assert (c.out[0] - whole[0]).abs().max() <= 1e-5 * whole[0].abs().max()
+
+
+def test_offsets_past_32_bits(torch):
+    """Pools of over 4 GB each, pages at their very end."""
+    G, page, hd, n_pages = 8, 256, 128, 9000                    # 4.7 GB of keys, and of values
+    pool = [torch.empty(n_pages, G, page, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    use = [8999, 0, 8500]
+    rng = np.random.default_rng(11)
+    small = round_bf16(rng.standard_normal((2, 3, G, page, hd)))
+    slots = np.concatenate([p * page + np.arange(page) for p in use])
+    cache = native.paged_cache("bf16", G, hd, page, n_pages, *pool)
+    rows = [torch.from_numpy(small[i].transpose(0, 2, 1, 3).reshape(3 * page, G * hd).copy()).cuda().to(torch.bfloat16)
+            for i in range(2)]
+    native.apex_paged_store(cache, rows[0], rows[1], "bf16", 3 * page, G * hd, G * hd, i32(torch, slots))
+    assert torch.equal(pool[0][8999].double().cpu(), torch.from_numpy(small[0, 0]))
+    for new in (1, 40):
+        q = round_bf16(rng.standard_normal((new, G, hd)))
+        dq = torch.from_numpy(q.reshape(new, -1)).cuda().to(torch.bfloat16)
+        out = torch.zeros_like(dq)
+        n = native.apex_attention_paged_workspace_bytes(new, 1, G, G, hd)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        native.apex_attention_paged(cache, dq, "bf16", new, 1, G, G * hd, i32(torch, [0, new]), i32(torch, [700]),
+                                    i32(torch, [use]), 3, 0, 0, hd ** -0.5, out, G * hd, ws, n)
+        want, size, peak = opaged.attend(q, small[0], small[1], [0, new], [700], np.array([[0, 1, 2]]), 0, 0,
+                                         hd ** -0.5, np.zeros_like(q))
+        compare(out.double().cpu().numpy().reshape(q.shape), want, size, peak, hd, "bf16")
+
+
+# ------------------------------------------------------------------------------------- store
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("T,G,hd,page", [(1, 1, 64, 16), (37, 3, 128, 16), (130, 8, 64, 64), (5, 2, 128, 1024)])
+def test_store(torch, T, G, hd, page, fmt, dtype):
+    rng = np.random.default_rng(T)
+    n_pages = cdiv(T, page) + 2
+    slots = rng.permutation(n_pages * page)[:T].astype(np.int64)
+    if T > 3:
+        slots[1], slots[3] = -1, n_pages * page                      # left out
+    x = rng.standard_normal((2, T, G, hd)) * np.exp(rng.uniform(-20, 20, (2, T, G, 1)))
+    x[0, T // 2, 0] = 0.0                                            # a row of zeros
+    x[1, 0, 0, :8] = x[1, 0, 0, 8]                                   # equal values
+    # ties between codes: the largest value 448 * 2^-5 makes the scale 2^-5
+    tie = np.array([0.5, 1.5, 17.0, 19.0, 2.0 ** -10, 3 * 2.0 ** -10, 248.0, 464.0 - 24]) * 2.0 ** -5
+    x[0, T - 1, G - 1], x[0, T - 1, G - 1, :8], x[0, T - 1, G - 1, 9] = 0, tie, -448 * 2.0 ** -5
+    x = round_bf16(x) if dtype == "bf16" else x.astype(np.float32).astype(np.float64)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    pools, scales, refs, ref_scales = [], [None] * 2, [], [None] * 2
+    for i in range(2):
+        if fmt == "bf16":
+            pools.append(torch.full((n_pages, G, page, hd), 5.0, dtype=torch.bfloat16, device="cuda"))
+            refs.append(np.full((n_pages, G, page, hd), 5.0))
+        else:
+            pools.append(torch.full((n_pages, G, page, hd), 0x31, dtype=torch.uint8, device="cuda"))
+            refs.append(np.full((n_pages, G, page, hd), 0x31, np.uint8))
+            scales[i] = torch.full((n_pages, G, page), 9.0, device="cuda")
+            ref_scales[i] = np.full((n_pages, G, page), 9.0, np.float32)
+        opaged.store(x[i], slots, page, refs[i], ref_scales[i])
+    cache = native.paged_cache(fmt, G, hd, page, n_pages, *pools, *scales)
+    wide = torch.from_numpy(np.concatenate([x[0].reshape(T, -1), x[1].reshape(T, -1)], 1)).cuda().to(t)
+    k, v = wide[:, :G * hd], wide[:, G * hd:]
+    native.apex_paged_store(cache, k, v, dtype, T, k.stride(0), v.stride(0), i32(torch, slots))
+    torch.cuda.synchronize()
+    for i in range(2):
+        if fmt == "bf16":
+            assert np.array_equal(pools[i].double().cpu().numpy(), refs[i])
+        else:
+            assert np.array_equal(scales[i].cpu().numpy(), ref_scales[i])
+            # a code of -0 for a value of -0 is as good
+            got, want = pools[i].cpu().numpy(), refs[i]
+            same = (got == want) | ((got & 0x7F == 0) & (want & 0x7F == 0))
+            assert same.all(), (np.argwhere(~same)[:5], got[~same][:5], want[~same][:5])
+
+
+def test_store_of_rows_that_are_not_finite(torch):
+    x = torch.ones(3, 64, device="cuda")
+    x[0, 5], x[1, 63] = float("inf"), float("nan")
+    codes = [torch.zeros(1, 1, 16, 64, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(1, 1, 16, device="cuda") for _ in range(2)]
+    cache = native.paged_cache("fp8", 1, 64, 16, 1, *codes, *scales)
+    native.apex_paged_store(cache, x, x, "fp32", 3, 64, 64, i32(torch, [0, 1, 2]))
+    assert torch.isnan(scales[0][0, 0, :2]).all() and scales[1][0, 0, 2] == torch.tensor(1 / 448, dtype=torch.float32)
+    assert (codes[0][0, 0, 2] == 0x7E).all() and (codes[0][0, 0, :2] == 0).all()
+
+
+def test_store_of_tiny_rows(torch):
+    x = np.zeros((4, 64), np.float32)
+    x[0, :4] = [2e-38, 1e-38, -7e-39, 1e-39]
+    x[1, :4] = [1e-40, -5e-41, 3e-42, 0]
+    x[2, 0] = 1e-44                                                  # the scale rounds to 0
+    x[3, :2] = [3.3e38, 1.0]
+    codes = [torch.zeros(1, 1, 16, 64, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(1, 1, 16, device="cuda") for _ in range(2)]
+    cache = native.paged_cache("fp8", 1, 64, 16, 1, *codes, *scales)
+    d = torch.from_numpy(x).cuda()
+    native.apex_paged_store(cache, d, d, "fp32", 4, 64, 64, i32(torch, [0, 1, 2, 3]))
+    ref, ref_s = np.zeros((1, 1, 16, 64), np.uint8), np.zeros((1, 1, 16), np.float32)
+    opaged.store(x.astype(np.float64)[:, None], [0, 1, 2, 3], 16, ref, ref_s)
+    assert np.array_equal(scales[0].cpu().numpy(), ref_s)
+    assert np.array_equal(codes[0].cpu().numpy(), ref)
+
+
+# -------------------------------------------------------------------------------------- plan
+class PlanCall:
+    def __init__(self, torch, R, n_pages, nb, T):
+        z = lambda *s: torch.full(s, 77, dtype=torch.int32, device="cuda")
+        self.seq, self.cu, self.slots, self.pos, self.count_out, self.status = (
+            z(R), z(R + 1), z(T), z(T), z(1), z(R))
+
+    def run(self, torch, cached, n_new, page, n_pages, table, T, free, count, stream=None):
+        self.table, self.free = i32(torch, table), i32(torch, free)
+        self.args = (i32(torch, cached), i32(torch, n_new), len(cached), page, n_pages, table.shape[1], T, self.free,
+                     i32(torch, [count]), self.table, self.seq, self.cu, self.slots, self.pos, self.count_out,
+                     self.status, stream)
+        native.apex_paged_plan(*self.args)
+
+    def check(self, want):
+        for got, name in ((self.table, "block_table"), (self.free, "free_pages"), (self.seq, "seq_len"),
+                          (self.cu, "cu_new"), (self.slots, "slot_map"), (self.pos, "positions"),
+                          (self.status, "status")):
+            assert np.array_equal(got.cpu().numpy(), want[name]), name
+        assert int(self.count_out[0]) == want["free_count"]
+
+
+@pytest.mark.parametrize("R,page,nb,n_pages,T,longest", [
+    (1, 16, 1, 1, 1, 1), (5, 16, 9, 30, 40, 30), (64, 32, 20, 700, 300, 5), (64, 16, 20, 300, 200, 60),
+    (1000, 64, 7, 3000, 2500, 4), (1025, 16, 9, 4000, 9000, 40), (4096, 16, 5, 9000, 5000, 3)])
+def test_plan_over_steps(torch, R, page, nb, n_pages, T, longest):
+    """Steps of a server: each takes the tables, lengths and free pages that the one before left."""
+    rng = np.random.default_rng(R)
+    table, cached = np.full((R, nb), -1), np.zeros(R, np.int64)
+    free, count = rng.permutation(n_pages), n_pages
+    call = PlanCall(torch, R, n_pages, nb, T)
+    for step in range(6):
+        n_new = rng.integers(0, longest + 1, R)
+        n_new[rng.random(R) < 0.1] = -1
+        if step == 3:
+            n_new[rng.integers(0, R)] = nb * page + 1                # more than a row has
+        call.run(torch, cached, n_new, page, n_pages, table, T, free, count)
+        want = opaged.plan(cached, n_new, page, n_pages, table, T, free, count)
+        call.check(want)
+        native.apex_paged_plan(*call.args)                           # the same inputs again
+        call.check(want)
+        table, cached, free, count = want["block_table"], want["seq_len"], want["free_pages"], want["free_count"]
+
+
+def test_plan_of_numbers_that_make_no_sense(torch):
+    big = 2 ** 31 - 1
+    table = np.array([[3, 99], [-5, 1], [0, 1], [2, -1], [-1, -1], [-1, -1]])
+    cached = [20, 30, -7, big, 0, 0]
+    n_new = [2, 1, 3, big, -9, big]
+    for count in (-4, 3, 10 ** 6):
+        call = PlanCall(torch, 6, 4, 2, 8)
+        free = [-8, 2, 77, 1]
+        call.run(torch, cached, n_new, 16, 4, table, 8, free, count)
+        call.check(opaged.plan(cached, n_new, 16, 4, table, 8, free, count))
+
+
+def test_plan_without_requests_or_rows(torch):
+    call = PlanCall(torch, 0, 4, 2, 5)
+    free, count = i32(torch, [0, 1, 2, 3]), i32(torch, [3])
+    native.apex_paged_plan(None, None, 0, 16, 4, 2, 5, free, count, None, None, call.cu, call.slots, call.pos,
+                           call.count_out, None)
+    assert int(call.cu[0]) == 0 and (call.slots == -1).all() and int(call.count_out[0]) == 3
+    table = np.array([[1, -1]])
+    call = PlanCall(torch, 1, 4, 2, 0)
+    call.run(torch, [5], [2], 16, 4, table, 0, [0, 2, 3, 0], 3)      # no row is left for it
+    call.check(opaged.plan([5], [2], 16, 4, table, 0, [0, 2, 3, 0], 3))
+
+
+# -------------------------------------------------------------------------------- all of them
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+def test_a_server_from_prompts_to_tokens(torch, fmt, dtype):
+    """Plan, store and attention as a server calls them: prompts in chunks, then single tokens,
+    requests that end and begin; every step's attention against the oracle over all keys and
+    values so far.  Run on a stream of its own, the steps captured once and replayed."""
+    R, page, nb, G, H, hd, n_pages, T = 4, 16, 8, 2, 6, 64, 24, 40
+    rng = np.random.default_rng(20)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    pages = [torch.zeros(n_pages, G, page, hd, dtype=torch.bfloat16 if fmt == "bf16" else torch.uint8, device="cuda")
+             for _ in range(2)]
+    scales = [torch.zeros(n_pages, G, page, device="cuda") if fmt == "fp8" else None for _ in range(2)]
+    cache = native.paged_cache(fmt, G, hd, page, n_pages, *pages, *scales)
+    z = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    cached, n_new, seq, cu, slots, count, count_out = z(R), z(R), z(R), z(R + 1), z(T), z(1), z(1)
+    table, free, status, positions = z(R, nb) - 1, torch.arange(n_pages, dtype=torch.int32, device="cuda"), z(R), z(T)
+    count.fill_(n_pages)
+    qkv = torch.zeros(T, (H + 2 * G) * hd, dtype=t, device="cuda")
+    out = torch.zeros(T, H * hd, dtype=t, device="cuda")
+    n = native.apex_attention_paged_workspace_bytes(T, R, H, G, hd)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+
+    def step():
+        s = torch.cuda.current_stream().cuda_stream
+        native.apex_paged_plan(cached, n_new, R, page, n_pages, nb, T, free, count, table, seq, cu, slots, positions,
+                               count_out, status, s)
+        k, v = qkv[:, H * hd:(H + G) * hd], qkv[:, (H + G) * hd:]
+        native.apex_paged_store(cache, k, v, dtype, T, k.stride(0), v.stride(0), slots, s)
+        native.apex_attention_paged(cache, qkv, dtype, T, R, H, qkv.stride(0), cu, seq, table, nb, 40, 3, 0.125, out,
+                                    out.stride(0), ws, n, s)
+        cached.copy_(seq)
+        count.copy_(count_out)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    cached.zero_()
+    count.fill_(n_pages)
+    host = dict(cached=np.zeros(R, np.int64), table=np.full((R, nb), -1), free=np.arange(n_pages), count=n_pages)
+    ref = [np.zeros((n_pages, G, page, hd), np.float64 if fmt == "bf16" else np.uint8) for _ in range(2)]
+    ref_s = [np.zeros((n_pages, G, page), np.float32) if fmt == "fp8" else None for _ in range(2)]
+    chunks = [[20, 1, 0, 9], [20, 1, 5, 9], [1, 1, 1, 1], [1, 1, 1, -1], [1, -1, 1, 33], [1, 7, 1, 1], [1, 1, 1, 1],
+              [-1, 30, 1, 2], [12, 1, 1, 1]]
+    for i, new in enumerate(chunks):
+        x = rng.standard_normal((T, H + 2 * G, hd))
+        x = round_bf16(x) if dtype == "bf16" else x.astype(np.float32).astype(np.float64)
+        qkv.copy_(torch.from_numpy(x.reshape(T, -1)))
+        n_new.copy_(i32(torch, new))
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        if i % 3 == 2:
+            step()                                   # eager calls among the replays
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        want = opaged.plan(host["cached"], new, page, n_pages, host["table"], T, host["free"], host["count"])
+        assert np.array_equal(table.cpu().numpy(), want["block_table"])
+        assert np.array_equal(slots.cpu().numpy(), want["slot_map"]) and int(count[0]) == want["free_count"]
+        host = dict(cached=want["seq_len"], table=want["block_table"], free=want["free_pages"], count=want["free_count"])
+        for kv, lo in ((0, H), (1, H + G)):
+            opaged.store(x[:, lo:lo + G], want["slot_map"], page, ref[kv], ref_s[kv])
+        K, V = ref if fmt == "bf16" else [fp8.decode_array(c) * s[..., None].astype(np.float64) for c, s in zip(ref, ref_s)]
+        ref_out, size, peak = opaged.attend(x[:, :H], K, V, want["cu_new"], want["seq_len"], want["block_table"], 40, 3,
+                                            0.125, np.full((T, H, hd), 7.0))
+        got = out.double().cpu().numpy().reshape(T, H, hd)
+        compare(got, ref_out, size, peak, hd, dtype)
+
+
+def test_two_streams_with_workspaces_of_their_own(torch):
+    a = Case(torch, [3000, 50], [1, 1], 8, 2, 128, 16, "bf16", "bf16", seed=30)
+    b = Case(torch, [900, 400], [100, 7], 8, 2, 128, 16, "fp8", "bf16", seed=31)
+    a.device(), b.device()
+    a.call(), b.call()
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.call(stream=streams[0].cuda_stream)
+        b.call(stream=streams[1].cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])

@@ -57,6 +57,10 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxGroup = 16;      // query heads per key/value head
 constexpr float kLog2e = 1.4426950408889634f;
+// Weights are 2^(score - m) for a reference m that is raised to the running maximum only when
+// that is more than kSlack above it: they stay below 2^kSlack, where sums in 32 bits and
+// roundings, which are relative, are as good, and rescaling is rare.
+constexpr float kSlack = 8.f;
 
 // ------------------------------------------------------------------------------ schedule
 struct Item {
@@ -612,15 +616,15 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
         top = max_xor32(max_xor16(top)) * a.scale_log2;
-        const float now = fmaxf(mx, top);
-        const float ref = now == -INFINITY ? 0.f : now;
-        if (__ballot(now > mx)) {
-            const float c = __builtin_amdgcn_exp2f(mx - ref);
+        if (__ballot(top > mx + kSlack)) {
+            const float now = fmaxf(mx, top);
+            const float c = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - now);
+            mx = now;
             l *= c;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= c;
         }
-        mx = now;
+        const float ref = mx == -INFINITY ? 0.f : mx;
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -716,6 +720,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
     __shared__ __align__(1024) uint8_t st0[2 * kTileUnit * RB], st1[2 * kTileUnit * RB];   // keys, values
     __shared__ __align__(16) float scales[2][2][kTileUnit];
     __shared__ __align__(16) int group_ok[2][4];
+    __shared__ int wave_odd[kWaves];
     const int item = uniform(blockIdx.x / a.G), g = blockIdx.x - item * a.G;
     if (item >= scalar_load(&a.head->n_items, 0)) return;
     const Item it = scalar_item(a.items, item);
@@ -770,15 +775,14 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    float mx = -INFINITY, l = 0.f;    // l: of the lane's own positions
+    float mx, l;    // l: of the lane's own positions
     floatx16 o[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
 
-    const auto step = [&](auto which, int i) __attribute__((always_inline)) {
+    // CAREFUL: see below
+    bool met_odd = false;
+    const auto step = [&](auto which, auto careful, int i) __attribute__((always_inline)) {
         constexpr int buf = decltype(which)::value;
+        constexpr bool CAREFUL = decltype(careful)::value;
         wait_loads<0>();
         if constexpr (F8)
             if (lane < 32) scales[buf][lane >> 4][16 * wave + (lane & 15)] = sc;
@@ -831,15 +835,15 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[m][e]);
         top = max_xor32(top) * a.scale_log2;
-        const float now = fmaxf(mx, top);
-        const float ref = now == -INFINITY ? 0.f : now;
-        if (__ballot(now > mx)) {
-            const float c = __builtin_amdgcn_exp2f(mx - ref);
+        if (__ballot(top > mx + kSlack)) {
+            const float now = fmaxf(mx, top);
+            const float c = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - now);
+            mx = now;
             l *= c;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= c;
         }
-        mx = now;
+        const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -852,7 +856,9 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
                     s[m][e] = w;
             }
         // Where rows see different positions, a value that is no finite number must not meet the
-        // zero weights of the rows that do not see it: such a unit's products go one by one.
+        // zero weights of the rows that do not see it.  A tile that meets such a unit is worked
+        // on again, carefully: that unit's products then go one by one.  (Done at once, in this
+        // loop, the compiler moves all of o between registers three times a unit.)
         bool odd = false;
         if (!whole) {
 #pragma unroll 1
@@ -870,8 +876,9 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
                 }
             }
             odd = __ballot(odd) != 0;
+            met_odd = met_odd || odd;
         }
-        if (odd) {
+        if (CAREFUL && odd) {
 #pragma unroll 1
             for (int j = 0; j < kTileUnit; ++j) {
                 float w = 0.f;
@@ -926,11 +933,27 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
             }
         }
     };
-    if (steps > 0) issue(Int<0>{}, 0);
-    for (int i = 0; i < steps; i += 2) {
-        step(Int<0>{}, i);
-        if (i + 1 < steps) step(Int<1>{}, i + 1);
-    }
+    const auto clear = [&] {
+        mx = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    };
+    const auto all_units = [&](auto careful) __attribute__((always_inline)) {
+        clear();
+        if (steps > 0) issue(Int<0>{}, 0);
+        for (int i = 0; i < steps; i += 2) {
+            step(Int<0>{}, careful, i);
+            if (i + 1 < steps) step(Int<1>{}, careful, i + 1);
+        }
+    };
+    all_units(Int<0>{});
+    if (lane == 0) wave_odd[wave] = met_odd;
+    wait_loads<0>();
+    __syncthreads();
+    if (wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) all_units(Int<1>{});
     wait_loads<0>();
     if (!row_on) return;
     l = sum_xor32(l);

@@ -1,13 +1,14 @@
 // Attention of new tokens over a paged cache (apex_attention_paged).
 //
-// Launches of a call:
-//   schedule  one workgroup: the query tiles of all requests, the key/value units each of them
-//             sees, and the items (tile, range of units) that the next launch works on.
-//   attend    grid (G, items), one workgroup per item and key/value head.  Tiles of one token
-//             (attend_token) or of up to 128 query rows, heads of one group and consecutive
-//             tokens (attend_tile).  A tile that is one item writes its rows; the items of one
-//             that is split write weighted sums, maxima and normalisers to the workspace.
-//   merge     the items of split tiles joined by the log-sum-exp rule.
+// A tile is a group of query rows of one request and key/value head that are worked on together;
+// the positions it sees fall into units.  Launches of a call (for each 1024 tiles):
+//   attend    Every workgroup lists the tiles and their units for itself (build_list), then works
+//             on its share.  Tiles of one token (attend_token) or of up to 128 query rows, heads
+//             of one group and consecutive tokens (attend_tile).  The units of a head, tile after
+//             tile, are shared out evenly over its workgroups (or, many tiles: whole tiles).  A
+//             tile within one share is written to `out`; where shares end inside a tile, its
+//             weighted sums, maxima and normalisers go to the workspace.
+//   merge     the parts of such tiles joined by the log-sum-exp rule.
 //
 // Both kernels compute S^T = K Q^T and O^T = V^T P^T on the matrix cores: a lane then holds the
 // scores of one query row in its registers, so that maxima, sums and rescaling are a lane's own
@@ -62,20 +63,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // roundings, which are relative, are as good, and rescaling is rare.
 constexpr float kSlack = 8.f;
 
-// ------------------------------------------------------------------------------ schedule
-struct Item {
-    int r, q0;          // request, first token of the tile (from the request's first new one)
-    int u_lo, u_hi;     // its units, of those the tile sees
-    int part;           // where its partial results go, or -1: it is the whole tile
-    int pad[3];
-};
-struct SplitTile {
-    int r, q0, part, n;   // the tile's first partial result and their number
-};
-struct Header {
-    int n_items, n_split, pad[2];
-};
-
+// --------------------------------------------------------------------------------- tiles
 // The positions a tile of tokens [q0, q1) of a request sees: sink units from 0 up, then the
 // units from `first` up to the last token's position.  UP: positions of a unit.
 struct Span {
@@ -110,124 +98,143 @@ __device__ __forceinline__ Request scalar_request(const int32_t *cu_new, const i
     const int b = min(max(scalar_load(cu_new, r + 1), a), T);
     return {a, b - a, min(max(scalar_load(seq_len, r), 0), room)};
 }
-__device__ __forceinline__ Item scalar_item(const Item *items, int i) {
-    const int *p = reinterpret_cast<const int *>(items + i);
-    return {scalar_load(p, 0), scalar_load(p, 1), scalar_load(p, 2), scalar_load(p, 3), scalar_load(p, 4), {}};
-}
 
-struct ScheduleArgs {
-    const int32_t *cu_new, *seq_len;
-    int R, T, room, tile_tokens, max_tiles, window, sinks, target, G, max_items, max_split;
-    Header *head;
-    Item *items;
-    SplitTile *split;
+constexpr int kListTiles = 1024;                 // tiles of one launch
+
+struct TileList {                   // in LDS
+    int32_t cu[kListTiles + 1];     // units of the tiles before
+    int32_t first[kListTiles];      // the first tile of its request, counted over all launches
+    uint16_t r[kListTiles];
+    int wave_end[kWaves];
+    int found;
 };
 
-constexpr int kSchedThreads = 1024;
-
-__device__ __forceinline__ int block_scan(int v, int *total, int *buf) {   // exclusive
+// Inclusive scans over a workgroup (sums, or maxima of values >= -1), `before` the exclusive one.
+template <bool MAX, int CTRL>
+__device__ __forceinline__ int scan_step(int v) {
+    const int o = __builtin_amdgcn_update_dpp(MAX ? -1 : 0, v, CTRL, 0xf, 0xf, false);
+    return MAX ? max(v, o) : v + o;
+}
+template <bool MAX>
+__device__ __forceinline__ int block_scan(int v, int *wave_end, int *before, int *total) {
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    int x = v;
+    const auto join = [](int x, int y) { return MAX ? max(x, y) : x + y; };
+    int x = scan_step<MAX, 0x111>(v);   // row_shr 1, 2, 4, 8
+    x = scan_step<MAX, 0x112>(x);
+    x = scan_step<MAX, 0x114>(x);
+    x = scan_step<MAX, 0x118>(x);
+    const int r0 = __builtin_amdgcn_readlane(x, 15);
+    const int r1 = join(r0, __builtin_amdgcn_readlane(x, 31));
+    const int r2 = join(r1, __builtin_amdgcn_readlane(x, 47));
+    const int none = MAX ? -1 : 0;
+    x = join(x, lane < 16 ? none : lane < 32 ? r0 : lane < 48 ? r1 : r2);
+    if (lane == kWave - 1) wave_end[wave] = x;
+    __syncthreads();
+    int low = none, all = none;
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int o = __shfl_up(x, d);
-        if (lane >= d) x += o;
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) low = join(low, wave_end[w]);
+        all = join(all, wave_end[w]);
     }
     __syncthreads();
-    if (lane == kWave - 1) buf[wave] = x;
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kSchedThreads / kWave; ++w) {
-        if (w < wave) before += buf[w];
-        all += buf[w];
-    }
+    int prev = __shfl_up(x, 1);
+    *before = join(low, lane == 0 ? none : prev);
     *total = all;
-    return before + x - v;
+    return join(low, x);
 }
 
-// Tiles in descending order (a request's last tile sees most).  Every tile is cut into items of
-// at most s units, s chosen so that all items together, times G, come to about `target`.
+struct ListArgs {
+    const int32_t *cu_new, *seq_len;
+    int R, T, room, tile_tokens, first_tile, window, sinks;
+};
+
+// Tiles first_tile .. first_tile + 1023 of all requests' tiles, those of a request in a row;
+// returns how many there are.  A few round trips to memory and barriers, about 3 us, where a
+// launch of its own that wrote the list for the next one took 7.  Loops are kept rolled: a
+// launch this short waits for its instructions as much as for its data.
 template <int UP>
-__global__ __launch_bounds__(kSchedThreads) void schedule(ScheduleArgs a) {
-    __shared__ int32_t cu_tiles[APEX_MAX_REQUESTS + 1];
-    __shared__ int buf[kSchedThreads / kWave];
-    __shared__ long long unit_sum;
+__device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
     const int t = threadIdx.x;
-    if (t == 0) {
-        unit_sum = 0;
-        cu_tiles[0] = 0;
-    }
-    int tiles = 0;
-    for (int r0 = 0; r0 < a.R; r0 += kSchedThreads) {
-        const int r = r0 + t;
-        int n = 0, all;
-        if (r < a.R) {
-            const Request q = request_of(a.cu_new, a.seq_len, r, a.T, a.room);
-            n = (q.n + a.tile_tokens - 1) / a.tile_tokens;
-        }
-        const int at = tiles + block_scan(n, &all, buf);
-        // more than max_tiles only where cu_new is no ascending list
-        if (r < a.R) cu_tiles[r + 1] = min(at + n, a.max_tiles);
-        tiles = min(tiles + all, a.max_tiles);
-    }
-    __syncthreads();
-    struct Tile {
-        int r, q0, units;
+    const int per = (a.R + kThreads - 1) / kThreads;
+#pragma unroll 1
+    for (int i = t; i < kListTiles; i += kThreads) s.first[i] = -1;
+    const auto tiles_of = [&](int r) {
+        return int(unsigned(request_of(a.cu_new, a.seq_len, r, a.T, a.room).n + a.tile_tokens - 1) /
+                   unsigned(a.tile_tokens));
     };
-    const auto tile_at = [&](int i) {
-        const int k = tiles - 1 - i;
-        int lo = 0, hi = a.R;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (cu_tiles[mid] <= k)
-                lo = mid;
-            else
-                hi = mid;
+    int count = 0, last = 0;
+#pragma unroll 1
+    for (int r = t * per; r < min((t + 1) * per, a.R); ++r) count += last = tiles_of(r);
+    int at, total;
+    block_scan<false>(count, s.wave_end, &at, &total);
+    // the first tile of each request in the list names it
+#pragma unroll 1
+    for (int r = t * per; r < min((t + 1) * per, a.R); ++r) {
+        const int n = per == 1 ? last : tiles_of(r);
+        if (n > 0 && at + n > a.first_tile && at < a.first_tile + kListTiles) {
+            const int i = max(at - a.first_tile, 0);
+            s.first[i] = at;
+            s.r[i] = uint16_t(r);
         }
-        const Request q = request_of(a.cu_new, a.seq_len, lo, a.T, a.room);
-        const int q0 = (k - cu_tiles[lo]) * a.tile_tokens, q1 = min(q0 + a.tile_tokens, q.n);
-        const int base = q.seq - q.n;
-        return Tile{lo, q0, span_of<UP>(max(base + q0, 0), base + q1 - 1, a.window, a.sinks).units};
-    };
-    long long sum = 0;
-    for (int i = t; i < tiles; i += kSchedThreads) sum += tile_at(i).units;
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
-    if (t % kWave == 0) atomicAdd(reinterpret_cast<unsigned long long *>(&unit_sum), sum);
+        at += n;
+    }
+    const int tiles = min(max(total - a.first_tile, 0), kListTiles);
     __syncthreads();
-    const long long want = (unit_sum * a.G + a.target - 1) / a.target;
-    const int s = int(max(want, 1ll));
-    int items = 0, parts = 0, splits = 0;
-    for (int i0 = 0; i0 < tiles; i0 += kSchedThreads) {
-        const int i = i0 + t;
-        Tile tile{0, 0, 0};
-        int n = 0;
-        if (i < tiles) {
-            tile = tile_at(i);
-            n = max(1, (tile.units + s - 1) / s);
-        }
-        int all_items, all_parts, all_splits;
-        const int at = items + block_scan(n, &all_items, buf);
-        const int part = parts + block_scan(n > 1 ? n : 0, &all_parts, buf);
-        const int sp = splits + block_scan(n > 1 ? 1 : 0, &all_splits, buf);
-        for (int j = 0; j < n && at + j < a.max_items; ++j) {
-            Item &it = a.items[at + j];
-            it.r = tile.r;
-            it.q0 = tile.q0;
-            it.u_lo = int((long long)tile.units * j / n);
-            it.u_hi = int((long long)tile.units * (j + 1) / n);
-            it.part = n > 1 ? part + j : -1;
-        }
-        if (n > 1 && sp < a.max_split) a.split[sp] = {tile.r, tile.q0, part, n};
-        items += all_items;
-        parts += all_parts;
-        splits += all_splits;
+    // a thread's tiles, in a row; the tiles between two named ones are the first one's
+    const int each = (tiles + kThreads - 1) / kThreads, i0 = t * each, i1 = min(i0 + each, tiles);
+    int named = -1, before, all;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i)
+        if (s.first[i] >= 0) named = i;
+    block_scan<true>(named, s.wave_end, &before, &all);
+    int sum = 0;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+        if (s.first[i] >= 0) before = i;
+        const int k = max(before, 0), first = s.first[k], r = s.r[k];
+        const Request q = request_of(a.cu_new, a.seq_len, r, a.T, a.room);
+        const int q0 = (a.first_tile + i - first) * a.tile_tokens;
+        const int base = q.seq - q.n, q1 = min(q0 + a.tile_tokens, q.n);
+        // a tile that sees nothing still has a unit: its rows are written
+        sum += max(span_of<UP>(max(base + q0, 0), base + q1 - 1, a.window, a.sinks).units, 1);
+        s.cu[i + 1] = sum;
+        // (a named tile's own entries do not change, and no others are read)
+        s.first[i] = first;
+        s.r[i] = uint16_t(r);
     }
-    if (t == 0) {
-        a.head->n_items = min(items, a.max_items);
-        a.head->n_split = min(splits, a.max_split);
-    }
+    block_scan<false>(sum, s.wave_end, &before, &all);
+    if (t == 0) s.cu[0] = 0;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) s.cu[i + 1] += before;
+    __syncthreads();
+    return tiles;
 }
+
+// The tile of unit z, for all threads.
+__device__ __forceinline__ int tile_of(TileList &s, int tiles, int z) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < tiles; i += kThreads)
+        if (s.cu[i] <= z && z < s.cu[i + 1]) s.found = i;
+    __syncthreads();
+    return uniform(s.found);
+}
+
+// Units 0 .. all - 1 in even shares, workers <= all: none is empty.
+struct Shares {
+    int each, more;   // units of a share, and how many shares have one more
+    __device__ __forceinline__ Shares(int all, int workers) : each(all / workers), more(all % workers) {}
+    __device__ __forceinline__ int begin(int w) const { return each * w + min(w, more); }
+    __device__ __forceinline__ int worker_of(int unit) const {
+        const int wide = more * (each + 1);
+        return unit < wide ? unit / (each + 1) : more + (unit - wide) / each;
+    }
+};
+
+// A tile that begins in a worker's share and goes on in those of the next `more` workers: its
+// rows, and which of the worker's two parts it is (-1: there is none).
+struct Split {
+    int row, rows, part, more;
+};
 
 // -------------------------------------------------------------------------------- device
 struct AttendArgs {
@@ -236,14 +243,14 @@ struct AttendArgs {
     int64_t q_stride, out_stride;
     const uint8_t *k_pages, *v_pages;
     const float *k_scales, *v_scales;
-    const int32_t *cu_new, *seq_len, *block_table;
-    int T, H, G, GR, tile_tokens, max_blocks, shift, page_size, n_pages, room, window, sinks;
+    const int32_t *block_table;
+    ListArgs list;
+    int G, GR, max_blocks, shift, page_size, n_pages;
+    int workers;           // workgroups that share out a head's units
     float scale_log2;      // the softmax scale times log2(e)
-    const Header *head;
-    const Item *items;
-    const SplitTile *split;
-    float *part_o;         // [part][G][rows][hd]
-    float2 *part_ml;       // [part][G][rows]: maximum (of scores in powers of two), normaliser
+    Split *split;          // [workers][G]
+    float *part_o;         // [workers][G][2][rows][hd]
+    float2 *part_ml;       // [workers][G][2][rows]: maximum (of scores in powers of two), normaliser
 };
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
@@ -385,11 +392,10 @@ struct TokenVSwizzle {   // bf16: 8 consecutive rows, two chunks; E4M3: rows 0-7
                          : ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
     }
 };
-template <int RB, bool F8>
-struct TileVSwizzle {    // bf16: 4 consecutive rows, four chunks; E4M3: rows 0-3 and 8-11, two
+template <int RB>
+struct TileVSwizzle {    // 4 consecutive rows, four chunks
     static __device__ __forceinline__ int of(int row) {
-        if (!F8) return RB == 256 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
-        return RB == 128 ? 2 * (((row >> 1) & 1) | ((row >> 3) & 1) << 1) : 2 * ((row >> 3) & 1);
+        return RB == 256 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
     }
 };
 
@@ -422,6 +428,20 @@ __device__ __forceinline__ GlobalFloats lane_pointer(const float *p, const float
     return (GlobalFloats)(uint64_t(uint32_t(hi)) << 32 | uint32_t(lo));
 }
 
+// Where 16 rows of RB bytes are and how many bytes of them a tile may read, in scalar registers by
+// force: a load whose descriptor the compiler does not know to be uniform is wrapped in a loop
+// over the lanes' values.
+struct Extent {
+    uint64_t base;
+    uint32_t bytes;
+};
+template <int RB>
+__device__ __forceinline__ Extent extent_of(const uint8_t *pool, const Rows16 &r) {
+    const uint64_t base = reinterpret_cast<uint64_t>(pool) + r.row * RB;
+    return {uint64_t(uint32_t(uniform(int(base >> 32)))) << 32 | uint32_t(uniform(int(base))),
+            uint32_t(uniform(r.end * RB))};
+}
+
 // 16 rows of RB bytes, row_of.. of a tile, to LDS.  Rows below `from` and not below `keep` are
 // written as zeros, as are those past r.end.
 template <int RB, class SW>
@@ -429,12 +449,8 @@ __device__ __forceinline__ void load_rows16(const uint8_t *pool, const Rows16 &r
                                             uint8_t *lds, int lds_at, int row_of) {
     constexpr int CH = RB / 16, RPI = kWave / CH;   // chunks of a row, rows per load
     const int lane = threadIdx.x % kWave;
-    // in scalar registers by force: a load whose descriptor the compiler does not know to be
-    // uniform is wrapped in a loop over the lanes' values
-    const uint64_t base = reinterpret_cast<uint64_t>(pool) + r.row * RB;
-    const uint64_t at0 = uint64_t(uint32_t(uniform(int(base >> 32)))) << 32 | uint32_t(uniform(int(base)));
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at0), 0,
-                                                        uint32_t(uniform(r.end * RB)), 0x00027000);
+    const Extent x = extent_of<RB>(pool, r);
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(x.base), 0, x.bytes, 0x00027000);
 #pragma unroll
     for (int i = 0; i < 16 / RPI; ++i) {
         const int row = RPI * i + lane / CH;
@@ -460,13 +476,14 @@ __device__ __forceinline__ void store_out(void *out, int64_t at, float v) {
 // Lane (q = lane % 16, lg = lane / 16) holds the scores of row q at positions 16 m + 4 lg + i.
 constexpr int kTokenUnit = 128;
 constexpr int kTokenRows = 16;
-constexpr int kTokenTarget = 1024;   // items, all heads
 
 template <int HD, bool F8, bool F32>
 struct TokenShape {
     static constexpr int RB = HD * (F8 ? 1 : 2);
     static constexpr int kStage = 2 * 32 * RB;              // keys and values of 32 positions
-    static constexpr int NS = kStage >= 16384 ? 2 : 4;      // stages
+    static constexpr int NS = kStage > 4096 ? 2 : 4;        // stages
+    static constexpr int kRing = kWaves * NS * kStage;
+    static constexpr int kPerCu = kRing > 65536 ? 1 : 2;    // workgroups that a CU's LDS holds
     static constexpr int kLoads = kStage / 1024 + (F8 ? 1 : 0);
 };
 
@@ -482,25 +499,21 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     __shared__ __align__(1024) uint8_t st3[NS > 2 ? kWaves : 1][NS > 2 ? S::kStage : 16];
     __shared__ __align__(16) float scales[kWaves][64];
     __shared__ float red_m[kWaves][kTokenRows], red_l[kWaves][kTokenRows];
+    __shared__ TileList list;
     static_assert(sizeof(st0) >= kWaves * kTokenRows * HD * sizeof(float), "merge room");
-    const int item = uniform(blockIdx.x / a.G), g = blockIdx.x - item * a.G;
-    if (item >= scalar_load(&a.head->n_items, 0)) return;
-    const Item it = scalar_item(a.items, item);
-    const Request rq = scalar_request(a.cu_new, a.seq_len, it.r, a.T, a.room);
+    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n = lane & 15, lg = lane >> 4;
-    const int p = uniform(rq.seq - rq.n + it.q0), hi = p + 1;
-    const int low = a.window > 0 ? max(0, p - a.window + 1) : 0;
-    const Span span = span_of<kTokenUnit>(max(p, 0), p, a.window, a.sinks);
-    const int32_t *table = a.block_table + size_t(it.r) * a.max_blocks;
-    const int64_t row = rq.row0 + it.q0;
-    const int steps = it.u_hi - it.u_lo;
-
-    Pieces<F32> qf[KS];
-#pragma unroll
-    for (int u = 0; u < KS; ++u)
-        qf[u] = load_q<F32>(a.q, row * a.q_stride + (g * a.GR + (n < a.GR ? n : 0)) * HD + 32 * u + 8 * lg,
-                            n < a.GR);
+    Split *split = a.split + size_t(w) * a.G + g;
+    if (threadIdx.x == 0) split->part = -1;
+    const int tiles = build_list<kTokenUnit>(a.list, list);
+    const int all_units = uniform(list.cu[tiles]);
+    if (all_units == 0) return;
+    const int workers = min(a.workers, all_units);   // none without a unit
+    if (w >= workers) return;
+    const Shares shares(all_units, workers);
+    const int share_lo = uniform(shares.begin(w)), share_hi = uniform(shares.begin(w + 1));
+    int tile = tile_of(list, tiles, share_lo);
 
     // where this lane reads, in a stage: keys of row n (and n + 16), values of row v_row (and,
     // bf16, v_row + 16); both swizzles are the same 16 rows further
@@ -525,9 +538,30 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     const GlobalFloats scale_of = lane_pointer(a.k_scales, a.v_scales, lane >= 32);
     float sc[NS];           // this lane's scale of a stage: keys in lanes 0..31, values behind
     bool ok[NS][2];
+
+    // the share's tiles
+#pragma unroll 1
+    for (int z = share_lo; z < share_hi; ++tile) {
+    const int tile_lo = uniform(list.cu[tile]), tile_hi = uniform(list.cu[tile + 1]);
+    const int u_lo = uniform(z - tile_lo), steps = uniform(min(tile_hi, share_hi) - z);
+    const int req = uniform(list.r[tile]), q0 = uniform(a.list.first_tile + tile - list.first[tile]);
+    const Request rq = scalar_request(a.list.cu_new, a.list.seq_len, req, a.list.T, a.list.room);
+    const int p = uniform(rq.seq - rq.n + q0), hi = p + 1;
+    const int low = a.list.window > 0 ? max(0, p - a.list.window + 1) : 0;
+    const Span span = span_of<kTokenUnit>(max(p, 0), p, a.list.window, a.list.sinks);
+    const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
+    const int64_t row = rq.row0 + q0;
+    const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
+
+    Pieces<F32> qf[KS];
+#pragma unroll
+    for (int u = 0; u < KS; ++u)
+        qf[u] = load_q<F32>(a.q, row * a.q_stride + (g * a.GR + (n < a.GR ? n : 0)) * HD + 32 * u + 8 * lg,
+                            n < a.GR);
+
     const auto issue = [&](auto which, int i) __attribute__((always_inline)) {
         constexpr int st = decltype(which)::value;
-        const int j0 = span.base(it.u_lo + min(i, steps - 1), kTokenUnit) + 32 * wave;
+        const int j0 = span.base(u_lo + min(i, steps - 1), kTokenUnit) + 32 * wave;
         const int end = i < steps ? hi : 0;
         Rows16 r[2];
 #pragma unroll
@@ -544,12 +578,12 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const int j = j0 + 16 * m;
-            load_rows16<RB, KSw>(a.k_pages, r[m], low - j, a.sinks - j, at, wave * S::kStage + 16 * m * RB, 16 * m);
+            load_rows16<RB, KSw>(a.k_pages, r[m], low - j, a.list.sinks - j, at, wave * S::kStage + 16 * m * RB, 16 * m);
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const int j = j0 + 16 * m;
-            load_rows16<RB, VSw>(a.v_pages, r[m], low - j, a.sinks - j, at, wave * S::kStage + (32 + 16 * m) * RB, 16 * m);
+            load_rows16<RB, VSw>(a.v_pages, r[m], low - j, a.list.sinks - j, at, wave * S::kStage + (32 + 16 * m) * RB, 16 * m);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -563,7 +597,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
         constexpr int ahead = (st + NS - 1) % NS;
         issue(Int<ahead>{}, i + NS - 1);
         wait_loads<S::kLoads *(NS - 1)>();
-        const int j0 = span.base(it.u_lo + i, kTokenUnit) + 32 * wave;
+        const int j0 = span.base(u_lo + i, kTokenUnit) + 32 * wave;
         const uint8_t *lds = stage(which);
         float ks[8], vs[8];
         if constexpr (F8) {
@@ -600,14 +634,14 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
                 if constexpr (F8) s[4 * m + e] *= ks[4 * m + e];
             }
         }
-        const bool whole = j0 + 31 < hi && (j0 >= low || j0 + 31 < a.sinks) && ok[st][0] && ok[st][1];
+        const bool whole = j0 + 31 < hi && (j0 >= low || j0 + 31 < a.list.sinks) && ok[st][0] && ok[st][1];
         if (!whole) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + 16 * m + 4 * lg + e;
-                    const bool on = j < hi && (j >= low || j < a.sinks) && ok[st][m];
+                    const bool on = j < hi && (j >= low || j < a.list.sinks) && ok[st][m];
                     s[4 * m + e] = on ? s[4 * m + e] : -INFINITY;
                     if constexpr (F8) vs[4 * m + e] = on ? vs[4 * m + e] : 0.f;
                 }
@@ -647,24 +681,22 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    if (steps > 0) {
-        issue(Int<0>{}, 0);
+    issue(Int<0>{}, 0);
+    if constexpr (NS == 4) {
+        issue(Int<1>{}, 1);
+        issue(Int<2>{}, 2);
+    }
+    int i = 0;
+    while (true) {
+        step(Int<0>{}, i);
+        if (++i == steps) break;
+        step(Int<1>{}, i);
+        if (++i == steps) break;
         if constexpr (NS == 4) {
-            issue(Int<1>{}, 1);
-            issue(Int<2>{}, 2);
-        }
-        int i = 0;
-        while (true) {
-            step(Int<0>{}, i);
+            step(Int<2>{}, i);
             if (++i == steps) break;
-            step(Int<1>{}, i);
+            step(Int<3>{}, i);
             if (++i == steps) break;
-            if constexpr (NS == 4) {
-                step(Int<2>{}, i);
-                if (++i == steps) break;
-                step(Int<3>{}, i);
-                if (++i == steps) break;
-            }
         }
     }
     // the wavefronts' shares joined in LDS, over the first stage
@@ -684,21 +716,26 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
         const int h = idx / HD, dim = idx % HD;
         float m = red_m[0][h];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, red_m[w][h]);
+        for (int v = 1; v < kWaves; ++v) m = fmaxf(m, red_m[v][h]);
         float den = 0.f, num = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float c = red_m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[w][h] - m);
-            den = fmaf(red_l[w][h], c, den);
-            num = fmaf(red[w][h][dim], c, num);
+        for (int v = 0; v < kWaves; ++v) {
+            const float c = red_m[v][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[v][h] - m);
+            den = fmaf(red_l[v][h], c, den);
+            num = fmaf(red[v][h][dim], c, num);
         }
-        if (it.part < 0) {
+        if (part < 0) {
             store_out<F32>(a.out, row * a.out_stride + (g * a.GR + h) * HD + dim, den == 0.f ? 0.f : num / den);
         } else {
-            const size_t at = (size_t(it.part) * a.G + g) * kTokenRows + h;
+            const size_t at = ((size_t(w) * a.G + g) * 2 + part) * kTokenRows + h;
             a.part_o[at * HD + dim] = num;
             if (dim == 0) a.part_ml[at] = make_float2(m, den);
         }
+    }
+    if (part >= 0 && z == tile_lo && threadIdx.x == 0)
+        *split = {int(row), a.GR, part, shares.worker_of(tile_hi - 1) - w};
+    z += steps;
+    if (z < share_hi) __syncthreads();   // the stages are free again
     }
 }
 
@@ -710,34 +747,81 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // scores of row q at positions 32 m + 8 (i / 4) + 4 h + i % 4.
 constexpr int kTileUnit = 64;
 constexpr int kTileRows = 128;
-constexpr int kTileTarget = 512;     // items, all heads
+constexpr int kBadPage = 1, kOdd = 2;
+
+template <bool F32>
+struct TileShape {
+    static constexpr int kPerCu = F32 ? 1 : 2;   // workgroups that a CU's registers hold
+};
 
 template <int HD, bool F8, bool F32>
-__global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs a) {
-    constexpr int RB = HD * (F8 ? 1 : 2), KS = HD / 16, DT = HD / 32, NP = Pieces<F32>::N;
+__global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(AttendArgs a) {
+    constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32, NP = Pieces<F32>::N;
     using KSw = KSwizzle<RB>;
-    using VSw = TileVSwizzle<RB, F8>;
+    using VSw = TileVSwizzle<RB>;
     __shared__ __align__(1024) uint8_t st0[2 * kTileUnit * RB], st1[2 * kTileUnit * RB];   // keys, values
     __shared__ __align__(16) float scales[2][2][kTileUnit];
-    __shared__ __align__(16) int group_ok[2][4];
+    __shared__ uint8_t group_flags[2][4];   // of a unit's 16 rows each: kBadPage, kOdd
     __shared__ int wave_odd[kWaves];
-    const int item = uniform(blockIdx.x / a.G), g = blockIdx.x - item * a.G;
-    if (item >= scalar_load(&a.head->n_items, 0)) return;
-    const Item it = scalar_item(a.items, item);
-    const Request rq = scalar_request(a.cu_new, a.seq_len, it.r, a.T, a.room);
+    __shared__ TileList list;
+    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n = lane & 31, h = lane >> 5;
-    const int q1 = min(it.q0 + a.tile_tokens, rq.n), tokens = q1 - it.q0;
-    const int p_first = uniform(rq.seq - rq.n + it.q0), p_last = p_first + tokens - 1, hi = p_last + 1;
-    const int low = a.window > 0 ? max(0, p_first - a.window + 1) : 0;
-    const Span span = span_of<kTileUnit>(max(p_first, 0), p_last, a.window, a.sinks);
-    const int32_t *table = a.block_table + size_t(it.r) * a.max_blocks;
-    const int steps = it.u_hi - it.u_lo;
+    Split *split = a.split + size_t(w) * a.G + g;
+    if (threadIdx.x == 0 && w < a.workers) split->part = -1;
+    const int tiles = build_list<kTileUnit>(a.list, list);
+    const int all_units = uniform(list.cu[tiles]);
+    if (all_units == 0) return;
+    // Many tiles: one each, the last ones (of a request: the longest) first, if the last round
+    // of workgroups is full enough.  Fewer: even shares of the units.
+    const int workers = min(a.workers, all_units);   // none without a unit
+    const int rounds = (tiles + a.workers - 1) / a.workers;
+    const bool whole_tiles = rounds >= 2 && 20 * tiles >= 17 * rounds * a.workers;
+    const Shares shares(all_units, workers);
+    int share_lo, share_hi, tile;
+    if (whole_tiles) {
+        if (w >= tiles) return;
+        tile = tiles - 1 - w;
+        share_lo = uniform(list.cu[tile]);
+        share_hi = uniform(list.cu[tile + 1]);
+    } else {
+        if (w >= workers) return;
+        share_lo = uniform(shares.begin(w));
+        share_hi = uniform(shares.begin(w + 1));
+        tile = tile_of(list, tiles, share_lo);
+    }
     const int m_row = 32 * wave + n, tok = m_row / a.GR, head = m_row - tok * a.GR;
+    // where this lane reads, in a stage: keys of row n (and n + 32), values of rows v_row and
+    // v_row + 8 of 16; the swizzles are the same 8, 16 and 32 rows further
+    int k_at[KS], v_at[DT];
+    constexpr int kV = kTileUnit * RB;   // the values' place
+    const int v_row = 4 * h + ((lane & 15) >> 2);
+#pragma unroll
+    for (int u = 0; u < KS; ++u) k_at[u] = settled(n * RB + 16 * ((2 * u + h) ^ KSw::of(n)));
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+        v_at[d] = settled(kV + v_row * RB + 8 * (lane & 1) +
+                          16 * ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ VSw::of(v_row)));
+    const GlobalFloats scale_of = lane_pointer(a.k_scales, a.v_scales, lane & 16);
+
+    // the share's tiles
+#pragma unroll 1
+    for (int z = share_lo; z < share_hi; ++tile) {
+    const int tile_lo = uniform(list.cu[tile]), tile_hi = uniform(list.cu[tile + 1]);
+    const int u_lo = uniform(z - tile_lo), steps = uniform(min(tile_hi, share_hi) - z);
+    const int req = uniform(list.r[tile]);
+    const int q0 = uniform((a.list.first_tile + tile - list.first[tile]) * a.list.tile_tokens);
+    const Request rq = scalar_request(a.list.cu_new, a.list.seq_len, req, a.list.T, a.list.room);
+    const int tokens = uniform(min(a.list.tile_tokens, rq.n - q0));
+    const int p_first = uniform(rq.seq - rq.n + q0), p_last = p_first + tokens - 1, hi = p_last + 1;
+    const int low = a.list.window > 0 ? max(0, p_first - a.list.window + 1) : 0;
+    const Span span = span_of<kTileUnit>(max(p_first, 0), p_last, a.list.window, a.list.sinks);
+    const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
+    const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
     const bool row_on = tok < tokens;
     const bool wave_on = 32 * wave < tokens * a.GR;
     const int p = row_on ? p_first + tok : -1;
-    const int64_t row = rq.row0 + it.q0 + (row_on ? tok : 0);
+    const int64_t row = rq.row0 + q0 + (row_on ? tok : 0);
     const int col = (g * a.GR + (row_on ? head : 0)) * HD;
 
     Pieces<F32> qf[KS];
@@ -745,34 +829,51 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
     for (int u = 0; u < KS; ++u)
         qf[u] = load_q<F32>(a.q, row * a.q_stride + col + 16 * u + 8 * h, row_on);
 
-    // where this lane reads, in a stage: keys of row n (and n + 32), values of row v_row and (bf16)
-    // v_row + 8, of 16 rows at a time; the swizzles are the same 8 (bf16), 16 and 32 rows further
-    int k_at[KS], v_at[DT];
-    constexpr int kV = kTileUnit * RB;   // the values' place
-    const int kv = (lane & 15) >> 1, half = (lane >> 4) & 1;
-    const int v_row = F8 ? 4 * h + (kv < 4 ? kv : kv + 4) : 4 * h + ((lane & 15) >> 2);
-#pragma unroll
-    for (int u = 0; u < KS; ++u)
-        k_at[u] = settled(n * RB + (F8 ? 16 * (u ^ KSw::of(n)) + 8 * h : 16 * ((2 * u + h) ^ KSw::of(n))));
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-        v_at[d] = settled(kV + v_row * RB + 8 * (lane & 1) +
-                          16 * ((F8 ? 2 * d + half : 4 * d + 2 * half + ((lane & 3) >> 1)) ^ VSw::of(v_row)));
-    const GlobalFloats scale_of = lane_pointer(a.k_scales, a.v_scales, lane & 16);
+    // This wavefront's 16 rows of unit i: bf16 straight to LDS; codes by way of registers, widened
+    // to bf16 once for the four wavefronts (each lane 16 codes of CPL chunks).
+    constexpr int CPL = F8 ? HD / 64 : 1, CRPI = kWave * 16 / HD;   // code loads, rows of a load
     float sc = 0.f;
     bool rows_ok = false;
-    // this wavefront's 16 rows of unit i
+    uint4 codes[2][CPL];
     const auto issue = [&](auto which, int i) __attribute__((always_inline)) {
         uint8_t *lds = decltype(which)::value ? st1 : st0;
         const int at = 16 * wave * RB;
-        const int j = span.base(it.u_lo + min(i, steps - 1), kTileUnit) + 16 * wave;
+        const int j = span.base(u_lo + min(i, steps - 1), kTileUnit) + 16 * wave;
         const Rows16 r = rows16(a, table, g, j, i < steps ? hi : 0);
+        const int from = low - j, keep = a.list.sinks - j;
         rows_ok = r.ok;
-        if constexpr (F8)
+        if constexpr (F8) {
             sc = scale_of[r.row + min(lane & 15, max(r.end - 1, 0))];
-        load_rows16<RB, KSw>(a.k_pages, r, low - j, a.sinks - j, lds, at, 16 * wave);
-        load_rows16<RB, VSw>(a.v_pages, r, low - j, a.sinks - j, lds, kV + at, 16 * wave);
+            const Extent kx = extent_of<HD>(a.k_pages, r), vx = extent_of<HD>(a.v_pages, r);
+            const auto kr = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(kx.base), 0, kx.bytes, 0x00027000);
+            const auto vr = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(vx.base), 0, vx.bytes, 0x00027000);
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) {
+                const int rr = CRPI * c + lane / (HD / 16);
+                const int off = rr < from && rr >= keep ? 0x40000000 : CRPI * HD * c + 16 * lane;
+                codes[0][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kr, off, 0, 0));
+                codes[1][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(vr, off, 0, 0));
+            }
+        } else {
+            load_rows16<RB, KSw>(a.k_pages, r, from, keep, lds, at, 16 * wave);
+            load_rows16<RB, VSw>(a.v_pages, r, from, keep, lds, kV + at, 16 * wave);
+        }
         __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto commit = [&](auto which) __attribute__((always_inline)) {
+        if constexpr (F8) {
+            uint8_t *lds = decltype(which)::value ? st1 : st0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int c = 0; c < CPL; ++c) {
+                    const int rr = 16 * wave + CRPI * c + lane / (HD / 16), ch = 2 * (lane % (HD / 16));
+                    const int sw = x ? VSw::of(rr) : KSw::of(rr), at = x * kV + rr * RB;
+                    const uint4 v = codes[x][c];
+                    *reinterpret_cast<uint4 *>(lds + (at + 16 * (ch ^ sw))) = widen_e4m3(make_uint2(v.x, v.y));
+                    *reinterpret_cast<uint4 *>(lds + (at + 16 * ((ch + 1) ^ sw))) = widen_e4m3(make_uint2(v.z, v.w));
+                }
+        }
     };
 
     float mx, l;    // l: of the lane's own positions
@@ -783,17 +884,39 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
     const auto step = [&](auto which, auto careful, int i) __attribute__((always_inline)) {
         constexpr int buf = decltype(which)::value;
         constexpr bool CAREFUL = decltype(careful)::value;
-        wait_loads<0>();
         if constexpr (F8)
             if (lane < 32) scales[buf][lane >> 4][16 * wave + (lane & 15)] = sc;
-        if (lane == 0) group_ok[buf][wave] = rows_ok;
+        wait_loads<0>();
+        const int j0 = span.base(u_lo + i, kTileUnit);
+        const uint8_t *lds = buf ? st1 : st0;
+        // whether all rows see all positions (but for bad pages)
+        const bool even = j0 + kTileUnit - 1 <= p_first &&
+                          (a.list.window == 0 || j0 > p_last - a.list.window || j0 + kTileUnit - 1 < a.list.sinks);
+        int flags = rows_ok ? 0 : kBadPage;
+        if (!even) {   // any value that is no finite number?
+            uint32_t odd = 0;
+#pragma unroll
+            for (int c = 0; c < RB / 64; ++c) {
+                const uint4 v = lds_u4(lds, kV + 16 * wave * RB + 16 * lane + 1024 * c);
+                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)   // exponents of all ones carry into the sign's place
+                    odd |= ((x[e] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+            }
+            if (__ballot(odd)) flags |= kOdd;
+        }
+        if (lane == 0) group_flags[buf][wave] = uint8_t(flags);
         lds_barrier();
         issue(Int<1 - buf>{}, i + 1);
         if (!wave_on) return;
-        const int j0 = span.base(it.u_lo + i, kTileUnit);
-        const uint8_t *lds = buf ? st1 : st0;
-        const int4 gok = *reinterpret_cast<const int4 *>(group_ok[buf]);
-        const int oks = uniform((gok.x & 1) | (gok.y & 1) << 1 | (gok.z & 1) << 2 | (gok.w & 1) << 3);
+        const int all_flags = uniform(*reinterpret_cast<const int *>(group_flags[buf]));
+        __builtin_amdgcn_sched_barrier(0);
+        // keys are read AHEAD products before their own
+        constexpr int NK = 2 * KS, AHEAD = 4;
+        const auto load_k = [&](int x) { return lds_u4(lds, k_at[x % KS] + 32 * (x / KS) * RB); };
+        uint4 kf[AHEAD];
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) kf[x] = load_k(x);
         float s[2][16];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -802,30 +925,37 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
             for (int e = 0; e < 16; ++e) big[e] = small[e] = 0.f;
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
-                uint4 k;
-                if constexpr (F8)
-                    k = widen_e4m3(lds_u2(lds, k_at[u] + 32 * m * RB));
-                else
-                    k = lds_u4(lds, k_at[u] + 32 * m * RB);
+                const int x = m * KS + u;
+                const uint4 k = kf[x % AHEAD];
+                if (x + AHEAD < NK) kf[x % AHEAD] = load_k(x + AHEAD);
 #pragma unroll
                 for (int q = NP - 1; q > 0; --q) small = mfma32(k, qf[u].p[q], small);
                 big = mfma32(k, qf[u].p[0], big);
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[m][e] = F32 ? big[e] + small[e] : big[e];
-                if constexpr (F8) s[m][e] *= scales[buf][0][32 * m + 8 * (e / 4) + 4 * h + e % 4];
-            }
+            for (int e = 0; e < 16; ++e) s[m][e] = F32 ? big[e] + small[e] : big[e];
         }
-        const bool whole = j0 + kTileUnit - 1 <= p_first && oks == 15 &&
-                           (a.window == 0 || j0 > p_last - a.window || j0 + kTileUnit - 1 < a.sinks);
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);   // LDS reads
+#pragma unroll
+        for (int x = 0; x < NK; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);  // matrix products
+            if (x + AHEAD < NK) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (F8)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[m][e] *= scales[buf][0][32 * m + 8 * (e / 4) + 4 * h + e % 4];
+        const bool whole = even && !(all_flags & 0x01010101 * kBadPage);
         if (!whole) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int jj = 32 * m + 8 * (e / 4) + 4 * h + e % 4;
-                    const bool on = visible(j0 + jj, p, a.window, a.sinks) && (oks >> (jj / 16) & 1);
+                    const bool on = visible(j0 + jj, p, a.list.window, a.list.sinks) &&
+                                    !(all_flags & kBadPage << 8 * (jj / 16));
                     s[m][e] = on ? s[m][e] : -INFINITY;
                 }
         }
@@ -844,49 +974,35 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
             for (int d = 0; d < DT; ++d) o[d] *= c;
         }
         const float ref = mx == -INFINITY ? 0.f : mx;
+        // the weights of step u, 16 positions (8 of this lane's row)
+        const auto weights = [&](int u, float (&w)[8]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[m][e], a.scale_log2, -ref));
-                l += w;
+            for (int e = 0; e < 8; ++e) {
+                const int i = 8 * (u & 1) + e;
+                w[e] = __builtin_amdgcn_exp2f(fmaf(s[u / 2][i], a.scale_log2, -ref));
+                l += w[e];
                 if constexpr (F8)   // a scale that the row does not see may be anything
-                    s[m][e] = w == 0.f ? 0.f : w * scales[buf][1][32 * m + 8 * (e / 4) + 4 * h + e % 4];
-                else
-                    s[m][e] = w;
+                    w[e] = w[e] == 0.f ? 0.f : w[e] * scales[buf][1][16 * u + 8 * (e / 4) + 4 * h + e % 4];
             }
+        };
         // Where rows see different positions, a value that is no finite number must not meet the
         // zero weights of the rows that do not see it.  A tile that meets such a unit is worked
         // on again, carefully: that unit's products then go one by one.  (Done at once, in this
         // loop, the compiler moves all of o between registers three times a unit.)
-        bool odd = false;
-        if (!whole) {
-#pragma unroll 1
-            for (int c = lane; c < kTileUnit * RB / 16; c += kWave) {
-                const uint4 v = lds_u4(lds, kV + 16 * c);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    if constexpr (F8) {
-                        const uint32_t y = (w[x] & 0x7f7f7f7fu) ^ 0x7f7f7f7fu;   // 0: a NaN code
-                        odd = odd || ((y - 0x01010101u) & ~y & 0x80808080u);
-                    } else {
-                        odd = odd || (w[x] & 0x7f80u) == 0x7f80u || (w[x] & 0x7f800000u) == 0x7f800000u;
-                    }
-                }
-            }
-            odd = __ballot(odd) != 0;
-            met_odd = met_odd || odd;
-        }
+        const bool odd = all_flags & 0x01010101 * kOdd;
+        met_odd = met_odd || odd;
         if (CAREFUL && odd) {
+            float all_w[4][8];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) weights(u, all_w[u]);
 #pragma unroll 1
             for (int j = 0; j < kTileUnit; ++j) {
                 float w = 0.f;
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int u = 0; u < 4; ++u)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (32 * m + 8 * (e / 4) + e % 4 == (j & ~4)) w = s[m][e];
+                    for (int e = 0; e < 8; ++e)
+                        if (16 * u + 8 * (e / 4) + e % 4 == (j & ~4)) w = all_w[u][e];
                 const float other = __shfl_xor(w, 32);
                 w = ((j >> 2) & 1) == h ? w : other;
 #pragma unroll
@@ -894,17 +1010,9 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
 #pragma unroll
                     for (int e4 = 0; e4 < 4; ++e4) {
                         float v[4];
-                        if constexpr (F8) {
-                            const uint32_t c = *reinterpret_cast<const uint32_t *>(
-                                lds + (kV + j * RB + 16 * ((2 * d + e4 / 2) ^ VSw::of(j)) + 8 * (e4 & 1) + 4 * h));
-                            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(c), false);
-                            const auto up = __builtin_amdgcn_cvt_pk_f32_fp8(int(c), true);
-                            v[0] = lo[0], v[1] = lo[1], v[2] = up[0], v[3] = up[1];
-                        } else {
-                            const uint2 c = lds_u2(lds, kV + j * RB + 16 * ((4 * d + e4) ^ VSw::of(j)) + 8 * h);
-                            v[0] = apex::ffn::bf_lo(c.x), v[1] = apex::ffn::bf_hi(c.x);
-                            v[2] = apex::ffn::bf_lo(c.y), v[3] = apex::ffn::bf_hi(c.y);
-                        }
+                        const uint2 c = lds_u2(lds, kV + j * RB + 16 * ((4 * d + e4) ^ VSw::of(j)) + 8 * h);
+                        v[0] = apex::ffn::bf_lo(c.x), v[1] = apex::ffn::bf_hi(c.x);
+                        v[2] = apex::ffn::bf_lo(c.y), v[3] = apex::ffn::bf_hi(c.y);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             o[d][4 * e4 + e] = w == 0.f ? o[d][4 * e4 + e] : fmaf(w, v[e], o[d][4 * e4 + e]);
@@ -912,24 +1020,46 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
             }
             return;
         }
+        // The products of a step run while the next one's values are read and its weights computed.
+        const auto load_v = [&](int u, int d) {
+            const uint2 v0 = lds_tr16(lds, v_at[d] + 16 * u * RB);
+            const uint2 v1 = lds_tr16(lds, v_at[d] + (16 * u + 8) * RB);
+            return make_uint4(v0.x, v0.y, v1.x, v1.y);
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 vf[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vf[d] = load_v(0, d);
+        float w[8];
+        weights(0, w);
+        Pieces<F32> pf = pieces_of<F32>(w);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            float w[8];
+            uint4 vn[DT];
+            Pieces<F32> pn;
+            if (u < 3) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = s[u / 2][8 * (u & 1) + e];
-            const Pieces<F32> pf = pieces_of<F32>(w);
+                for (int d = 0; d < DT; ++d) vn[d] = load_v(u + 1, d);
+                weights(u + 1, w);
+                pn = pieces_of<F32>(w);
+            }
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                uint4 v;
-                if constexpr (F8) {
-                    v = widen_e4m3(lds_tr8(lds, v_at[d] + 16 * u * RB));
-                } else {
-                    const uint2 v0 = lds_tr16(lds, v_at[d] + 16 * u * RB);
-                    const uint2 v1 = lds_tr16(lds, v_at[d] + (16 * u + 8) * RB);
-                    v = make_uint4(v0.x, v0.y, v1.x, v1.y);
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int q = NP - 1; q >= 0; --q) o[d] = mfma32(vf[d], pf.p[q], o[d]);
+            if (u < 3) {
+#pragma unroll
+                for (int x = 0; x < DT * NP; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // a product
+                    if (x < DT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // values of the next step
+                    __builtin_amdgcn_sched_group_barrier(0x002, F32 ? 9 : 28 / DT, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 8 / DT, 0);
                 }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int q = NP - 1; q >= 0; --q) o[d] = mfma32(v, pf.p[q], o[d]);
+                for (int d = 0; d < DT; ++d) vf[d] = vn[d];
+                pf = pn;
             }
         }
     };
@@ -941,23 +1071,29 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     };
-    const auto all_units = [&](auto careful) __attribute__((always_inline)) {
+    const auto work = [&](auto careful) __attribute__((always_inline)) {
         clear();
-        if (steps > 0) issue(Int<0>{}, 0);
+        issue(Int<0>{}, 0);
+        commit(Int<0>{});
         for (int i = 0; i < steps; i += 2) {
             step(Int<0>{}, careful, i);
-            if (i + 1 < steps) step(Int<1>{}, careful, i + 1);
+            commit(Int<1>{});
+            if (i + 1 < steps) {
+                step(Int<1>{}, careful, i + 1);
+                commit(Int<0>{});
+            }
         }
     };
-    all_units(Int<0>{});
+    work(Int<0>{});
     if (lane == 0) wave_odd[wave] = met_odd;
     wait_loads<0>();
     __syncthreads();
-    if (wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) all_units(Int<1>{});
+    if (wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) work(Int<1>{});
     wait_loads<0>();
-    if (!row_on) return;
     l = sum_xor32(l);
-    if (it.part < 0) {
+    if (!row_on) {
+        // no row of the tile
+    } else if (part < 0) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -975,7 +1111,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
                         make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
             }
     } else {
-        const size_t at = (size_t(it.part) * a.G + g) * kTileRows + m_row;
+        const size_t at = ((size_t(w) * a.G + g) * 2 + part) * kTileRows + m_row;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -984,56 +1120,111 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void attend_tile(AttendArgs 
                     make_float4(o[d][4 * e4], o[d][4 * e4 + 1], o[d][4 * e4 + 2], o[d][4 * e4 + 3]);
         if (h == 0) a.part_ml[at] = make_float2(mx, l);
     }
+    if (part >= 0 && z == tile_lo && threadIdx.x == 0)
+        *split = {rq.row0 + q0, tokens * a.GR, part, shares.worker_of(tile_hi - 1) - w};
+    z += steps;
+    if (z < share_hi) __syncthreads();   // the stages are free again
+    }
 }
 
 // --------------------------------------------------------------------------------- merge
-// One wavefront per row of a split tile, HD / 64 dimensions per lane.
-constexpr int kMergeBlocks = 512;
-
+// Tiles of one token: grid (workers * G, GR), a workgroup per row.  Groups of HD / 4 threads take
+// the parts in turn and meet in LDS.
 template <int HD, bool F32>
-__global__ __launch_bounds__(kThreads) void merge_parts(AttendArgs a, int rows) {
-    constexpr int PER = HD / kWave;
-    const int lane = threadIdx.x % kWave;
-    const int per_tile = a.tile_tokens * a.GR * a.G;
-    const int64_t total = int64_t(a.head->n_split) * per_tile;
-    for (int64_t e = int64_t(blockIdx.x) * kWaves + threadIdx.x / kWave; e < total;
-         e += int64_t(gridDim.x) * kWaves) {
-        const int tile = uniform(int(e / per_tile)), rest = uniform(int(e - int64_t(tile) * per_tile));
-        const int m = rest / a.G, g = rest - m * a.G, tok = m / a.GR, head = m - tok * a.GR;
-        const SplitTile sp = a.split[tile];
-        const Request rq = request_of(a.cu_new, a.seq_len, sp.r, a.T, a.room);
-        if (sp.q0 + tok >= rq.n) continue;
-        const size_t step = size_t(a.G) * rows;
-        const size_t at = (size_t(sp.part) * a.G + g) * rows + m;
-        float top = -INFINITY;
-        for (int s = lane; s < sp.n; s += kWave) top = fmaxf(top, a.part_ml[at + s * step].x);
-#pragma unroll
-        for (int d = kWave / 2; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-        float den = 0.f, num[PER];
-#pragma unroll
-        for (int x = 0; x < PER; ++x) num[x] = 0.f;
+__global__ __launch_bounds__(kThreads) void merge_tokens(AttendArgs a) {
+    constexpr int LPR = HD / 4, GROUPS = kThreads / LPR;
+    __shared__ float red_m[kWaves], red_d[GROUPS];
+    __shared__ __align__(16) float red[GROUPS][HD];
+    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G, h = blockIdx.y;
+    const Split sp = a.split[size_t(w) * a.G + g];
+    if (sp.part < 0) return;
+    const int t = threadIdx.x, wave = t / kWave, lane = t % kWave, group = t / LPR, at4 = t % LPR;
+    const auto slot = [&](int s) {   // part s: the first worker's, then the next ones' first parts
+        return ((size_t(w + s) * a.G + g) * 2 + (s == 0 ? sp.part : 0)) * kTokenRows + h;
+    };
+    float top = -INFINITY;
+    for (int s = t; s <= sp.more; s += kThreads) top = fmaxf(top, a.part_ml[slot(s)].x);
+    top = max_xor32(max_xor16(apex::ffn::row_max(top)));
+    if (lane == 0) red_m[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+    float den = 0.f;
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int s = 0; s < sp.n; ++s) {
-            const float2 ml = a.part_ml[at + s * step];
+    for (int s = group; s <= sp.more; s += GROUPS) {
+        const float2 ml = a.part_ml[slot(s)];
+        const float4 o = reinterpret_cast<const float4 *>(a.part_o + slot(s) * HD)[at4];
+        const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        den = fmaf(ml.y, c, den);
+        num.x = fmaf(o.x, c, num.x);
+        num.y = fmaf(o.y, c, num.y);
+        num.z = fmaf(o.z, c, num.z);
+        num.w = fmaf(o.w, c, num.w);
+    }
+    *reinterpret_cast<float4 *>(&red[group][4 * at4]) = num;
+    if (at4 == 0) red_d[group] = den;
+    __syncthreads();
+    if (t >= HD) return;
+    float d = 0.f, v = 0.f;
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) {
+        d += red_d[q];
+        v += red[q][t];
+    }
+    store_out<F32>(a.out, sp.row * a.out_stride + (g * a.GR + h) * HD + t, d == 0.f ? 0.f : v / d);
+}
+
+// Tiles of many rows: grid (workers * G, kMergeRows), HD / 4 lanes per row.
+constexpr int kMergeRows = 16;
+template <int HD, bool F32>
+__global__ __launch_bounds__(kThreads) void merge_tiles(AttendArgs a) {
+    constexpr int LPR = HD / 4, PER = kThreads / LPR;   // rows at a time
+    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
+    const Split sp = a.split[size_t(w) * a.G + g];
+    if (sp.part < 0) return;
+    const int at4 = threadIdx.x % LPR;
+    for (int m = blockIdx.y * PER + threadIdx.x / LPR; m < sp.rows; m += gridDim.y * PER) {
+        const auto slot = [&](int s) {
+            return ((size_t(w + s) * a.G + g) * 2 + (s == 0 ? sp.part : 0)) * kTileRows + m;
+        };
+        float top = -INFINITY;
+        for (int s = 0; s <= sp.more; ++s) top = fmaxf(top, a.part_ml[slot(s)].x);
+        float den = 0.f;
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int s = 0; s <= sp.more; ++s) {
+            const float2 ml = a.part_ml[slot(s)];
+            const float4 o = reinterpret_cast<const float4 *>(a.part_o + slot(s) * HD)[at4];
             const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-            const float *o = a.part_o + (at + s * step) * HD + lane * PER;
             den = fmaf(ml.y, c, den);
-#pragma unroll
-            for (int x = 0; x < PER; ++x) num[x] = fmaf(o[x], c, num[x]);
+            num.x = fmaf(o.x, c, num.x);
+            num.y = fmaf(o.y, c, num.y);
+            num.z = fmaf(o.z, c, num.z);
+            num.w = fmaf(o.w, c, num.w);
         }
-        const int64_t out = (int64_t(rq.row0) + sp.q0 + tok) * a.out_stride + (g * a.GR + head) * HD + lane * PER;
+        const int tok = m / a.GR, head = m - tok * a.GR;
+        const int64_t at = (int64_t(sp.row) + tok) * a.out_stride + (g * a.GR + head) * HD + 4 * at4;
+        const float v[4] = {num.x, num.y, num.z, num.w};
+        float r[4];
 #pragma unroll
-        for (int x = 0; x < PER; ++x) store_out<F32>(a.out, out + x, den == 0.f ? 0.f : num[x] / den);
+        for (int e = 0; e < 4; ++e) r[e] = den == 0.f ? 0.f : v[e] / den;
+        if constexpr (F32)
+            *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = make_float4(r[0], r[1], r[2], r[3]);
+        else
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) =
+                make_uint2(pk_bf16(r[0], r[1]), pk_bf16(r[2], r[3]));
     }
 }
 
 // ---------------------------------------------------------------------------------- host
-// Which kernel a call takes and what its workspace holds.
+constexpr int kCus = 256;
+
+// Which kernel a call takes and what its workspace holds: room for the most workers that a CU
+// may hold, whatever the types.
 struct Plan {
     bool token;
-    int GR, tile_tokens, max_tiles, target, rows;
-    int max_split, max_parts, max_items;     // per key/value head
-    size_t at_items, at_split, at_ml, at_o, bytes;
+    int GR, tile_tokens, max_tiles, rows, most_workers;
+    size_t at_ml, at_o, bytes;
 };
 Plan plan_of(int T, int R, int H, int G, int hd) {
     Plan p;
@@ -1043,31 +1234,41 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
     p.token = T <= R;
     p.tile_tokens = p.token ? 1 : kTileRows / p.GR;
     p.rows = p.token ? kTokenRows : kTileRows;
-    p.target = p.token ? kTokenTarget : kTileTarget;
     p.max_tiles = T / p.tile_tokens + std::min(T, R);
-    // s units an item, s >= U G / target: fewer than target / G tiles have more than s of them,
-    // and their items are fewer than their units / s, target / G at most, and one for each
-    const int per_head = p.target / G + 1;
-    p.max_split = per_head;
-    p.max_parts = 2 * per_head;
-    p.max_items = p.max_tiles + per_head;
+    p.most_workers = std::max(1, 2 * kCus / G);
     const auto up = [](size_t v) { return apex::align_up(v, 256); };
-    p.at_items = 256;
-    p.at_split = p.at_items + up(size_t(p.max_items) * sizeof(Item));
-    p.at_ml = p.at_split + up(size_t(p.max_split) * sizeof(SplitTile));
-    const size_t parts = size_t(p.max_parts) * G * p.rows;
+    const size_t shares = size_t(p.most_workers) * G, parts = 2 * shares * p.rows;
+    p.at_ml = up(shares * sizeof(Split));
     p.at_o = p.at_ml + up(parts * sizeof(float2));
     p.bytes = p.at_o + up(parts * hd * sizeof(float));
     return p;
 }
 
-template <int HD, bool F32>
-void launch_attention(const Plan &p, bool f8, int G, hipStream_t st, const AttendArgs &a) {
-    const dim3 grid(unsigned(p.max_items) * unsigned(G));
-    const auto f = p.token ? (f8 ? attend_token<HD, true, F32> : attend_token<HD, false, F32>)
-                           : (f8 ? attend_tile<HD, true, F32> : attend_tile<HD, false, F32>);
-    hipLaunchKernelGGL(f, grid, dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL((merge_parts<HD, F32>), dim3(kMergeBlocks), dim3(kThreads), 0, st, a, p.rows);
+template <int HD, bool F8, bool F32>
+apex_status launch_attention(const Plan &p, hipStream_t st, AttendArgs a) {
+    const int per_cu = p.token ? TokenShape<HD, F8, F32>::kPerCu : TileShape<F32>::kPerCu;
+    a.workers = std::max(1, kCus * per_cu / a.G);
+    for (int f = 0; f < p.max_tiles; f += kListTiles) {
+        a.list.first_tile = f;
+        if (p.token) {
+            hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3(a.workers * a.G), dim3(kThreads), 0, st, a);
+            hipLaunchKernelGGL((merge_tokens<HD, F32>), dim3(a.workers * a.G, a.GR), dim3(kThreads), 0, st, a);
+        } else {
+            const int tiles = std::min(p.max_tiles - f, kListTiles);
+            hipLaunchKernelGGL((attend_tile<HD, F8, F32>), dim3(std::max(a.workers, tiles) * a.G),
+                               dim3(kThreads), 0, st, a);
+            hipLaunchKernelGGL((merge_tiles<HD, F32>), dim3(a.workers * a.G, kMergeRows), dim3(kThreads), 0,
+                               st, a);
+        }
+        APEX_HIP(hipGetLastError());
+    }
+    return APEX_OK;
+}
+
+template <int HD>
+apex_status launch_attention(const Plan &p, bool f8, bool f32, hipStream_t st, const AttendArgs &a) {
+    return f8 ? (f32 ? launch_attention<HD, true, true>(p, st, a) : launch_attention<HD, true, false>(p, st, a))
+              : (f32 ? launch_attention<HD, false, true>(p, st, a) : launch_attention<HD, false, false>(p, st, a));
 }
 
 }  // namespace
@@ -1118,8 +1319,6 @@ extern "C" apex_status apex_attention_paged(const apex_paged_cache *cache, const
     const Plan p = plan_of(T, R, H, G, hd);
     if (workspace_bytes < p.bytes)
         return apex::fail(APEX_E_CAPACITY, "%s: workspace %zu < %zu bytes", fn, workspace_bytes, p.bytes);
-    if (int64_t(p.max_items) * G > (int64_t(1) << 31) - 1)
-        return apex::fail(APEX_E_UNSUPPORTED, "%s: T=%d rows of %d heads are too many", fn, T, H);
     char *ws = static_cast<char *>(workspace);
     AttendArgs a;
     a.q = q;
@@ -1130,41 +1329,19 @@ extern "C" apex_status apex_attention_paged(const apex_paged_cache *cache, const
     a.v_pages = static_cast<const uint8_t *>(cache->v_pages);
     a.k_scales = cache->k_scales;
     a.v_scales = cache->v_scales;
-    a.cu_new = cu_new;
-    a.seq_len = seq_len;
     a.block_table = block_table;
-    a.T = T;
-    a.H = H;
+    a.list = {cu_new, seq_len, R, T, max_blocks * page_size, p.tile_tokens, 0, window, sinks};
     a.G = G;
     a.GR = p.GR;
-    a.tile_tokens = p.tile_tokens;
     a.max_blocks = max_blocks;
     a.shift = apex::log2_of(page_size);
     a.page_size = page_size;
     a.n_pages = cache->n_pages;
-    a.room = max_blocks * page_size;
-    a.window = window;
-    a.sinks = sinks;
+    a.workers = 1;
     a.scale_log2 = scale * kLog2e;
-    a.head = reinterpret_cast<const Header *>(ws);
-    a.items = reinterpret_cast<const Item *>(ws + p.at_items);
-    a.split = reinterpret_cast<const SplitTile *>(ws + p.at_split);
+    a.split = reinterpret_cast<Split *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.at_ml);
     a.part_o = reinterpret_cast<float *>(ws + p.at_o);
-    const ScheduleArgs sa{cu_new, seq_len, R, T, a.room, p.tile_tokens, p.max_tiles, window, sinks,
-                          p.target, G, p.max_items, p.max_split,
-                          reinterpret_cast<Header *>(ws), reinterpret_cast<Item *>(ws + p.at_items),
-                          reinterpret_cast<SplitTile *>(ws + p.at_split)};
-    if (p.token)
-        hipLaunchKernelGGL(schedule<kTokenUnit>, dim3(1), dim3(kSchedThreads), 0, stream, sa);
-    else
-        hipLaunchKernelGGL(schedule<kTileUnit>, dim3(1), dim3(kSchedThreads), 0, stream, sa);
-    APEX_HIP(hipGetLastError());
     const bool f32 = dtype == APEX_TYPE_FP32, f8 = cache->format == APEX_KV_FP8_E4M3;
-    if (hd == 64)
-        f32 ? launch_attention<64, true>(p, f8, G, stream, a) : launch_attention<64, false>(p, f8, G, stream, a);
-    else
-        f32 ? launch_attention<128, true>(p, f8, G, stream, a) : launch_attention<128, false>(p, f8, G, stream, a);
-    APEX_HIP(hipGetLastError());
-    return APEX_OK;
+    return hd == 64 ? launch_attention<64>(p, f8, f32, stream, a) : launch_attention<128>(p, f8, f32, stream, a);
 }

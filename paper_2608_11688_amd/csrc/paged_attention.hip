@@ -1,7 +1,7 @@
 // Attention of new tokens over a paged cache (apex_attention_paged).
 //
 // A tile is a group of query rows of one request and key/value head that are worked on together;
-// the positions it sees fall into units.  Launches of a call (for each 1024 tiles):
+// the positions it sees fall into units.  Launches of a call (for each 512 tiles):
 //   attend    Every workgroup lists the tiles and their units for itself (build_list), then works
 //             on its share.  Tiles of one token (attend_token) or of up to 128 query rows, heads
 //             of one group and consecutive tokens (attend_tile).  The units of a head, tile after
@@ -92,19 +92,15 @@ __device__ __forceinline__ Request request_of(const int32_t *cu_new, const int32
     const int a = min(max(cu_new[r], 0), T), b = min(max(cu_new[r + 1], a), T);
     return {a, b - a, min(max(seq_len[r], 0), room)};
 }
-__device__ __forceinline__ Request scalar_request(const int32_t *cu_new, const int32_t *seq_len, int r,
-                                                  int T, int room) {
-    const int a = min(max(scalar_load(cu_new, r), 0), T);
-    const int b = min(max(scalar_load(cu_new, r + 1), a), T);
-    return {a, b - a, min(max(scalar_load(seq_len, r), 0), room)};
-}
-
-constexpr int kListTiles = 1024;                 // tiles of one launch
+constexpr int kListTiles = 512;                  // tiles of one launch
 
 struct TileList {                   // in LDS
     int32_t cu[kListTiles + 1];     // units of the tiles before
+    int32_t row[kListTiles];        // the tile's first row of q
+    int32_t p[kListTiles];          // that row's position
     int32_t first[kListTiles];      // the first tile of its request, counted over all launches
-    uint16_t r[kListTiles];
+    uint16_t r[kListTiles];         // its request
+    uint8_t tokens[kListTiles];
     int wave_end[kWaves];
     int found;
 };
@@ -148,7 +144,7 @@ struct ListArgs {
     int R, T, room, tile_tokens, first_tile, window, sinks;
 };
 
-// Tiles first_tile .. first_tile + 1023 of all requests' tiles, those of a request in a row;
+// Tiles first_tile .. first_tile + 511 of all requests' tiles, those of a request in a row;
 // returns how many there are.  A few round trips to memory and barriers, about 3 us, where a
 // launch of its own that wrote the list for the next one took 7.  Loops are kept rolled: a
 // launch this short waits for its instructions as much as for its data.
@@ -194,13 +190,14 @@ __device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
         const int k = max(before, 0), first = s.first[k], r = s.r[k];
         const Request q = request_of(a.cu_new, a.seq_len, r, a.T, a.room);
         const int q0 = (a.first_tile + i - first) * a.tile_tokens;
-        const int base = q.seq - q.n, q1 = min(q0 + a.tile_tokens, q.n);
+        const int p = q.seq - q.n + q0, tokens = min(a.tile_tokens, q.n - q0);
         // a tile that sees nothing still has a unit: its rows are written
-        sum += max(span_of<UP>(max(base + q0, 0), base + q1 - 1, a.window, a.sinks).units, 1);
+        sum += max(span_of<UP>(max(p, 0), p + tokens - 1, a.window, a.sinks).units, 1);
         s.cu[i + 1] = sum;
-        // (a named tile's own entries do not change, and no others are read)
-        s.first[i] = first;
-        s.r[i] = uint16_t(r);
+        s.row[i] = q.row0 + q0;
+        s.p[i] = p;
+        s.tokens[i] = uint8_t(tokens);
+        s.r[i] = uint16_t(r);   // (of a named tile, the only ones others read: what it was)
     }
     block_scan<false>(sum, s.wave_end, &before, &all);
     if (t == 0) s.cu[0] = 0;
@@ -230,10 +227,10 @@ struct Shares {
     }
 };
 
-// A tile that begins in a worker's share and goes on in those of the next `more` workers: its
-// rows, and which of the worker's two parts it is (-1: there is none).
+// Where a tile's rows come from, written by the worker whose share it begins in: that worker's
+// part `part` and the first parts of the next `more` ones (more = 0: they are written already).
 struct Split {
-    int row, rows, part, more;
+    int row, rows, part, more;      // part: of all [worker][G][2]
 };
 
 // -------------------------------------------------------------------------------- device
@@ -248,9 +245,10 @@ struct AttendArgs {
     int G, GR, max_blocks, shift, page_size, n_pages;
     int workers;           // workgroups that share out a head's units
     float scale_log2;      // the softmax scale times log2(e)
-    Split *split;          // [workers][G]
-    float *part_o;         // [workers][G][2][rows][hd]
-    float2 *part_ml;       // [workers][G][2][rows]: maximum (of scores in powers of two), normaliser
+    int *tiles;            // how many the launch has
+    Split *split;          // [tile][G]
+    float *part_o;         // [worker][G][2][rows][hd]
+    float2 *part_ml;       // [worker][G][2][rows]: maximum (of scores in powers of two), normaliser
 };
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
@@ -504,9 +502,8 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n = lane & 15, lg = lane >> 4;
-    Split *split = a.split + size_t(w) * a.G + g;
-    if (threadIdx.x == 0) split->part = -1;
     const int tiles = build_list<kTokenUnit>(a.list, list);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.tiles[0] = tiles;
     const int all_units = uniform(list.cu[tiles]);
     if (all_units == 0) return;
     const int workers = min(a.workers, all_units);   // none without a unit
@@ -544,13 +541,11 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     for (int z = share_lo; z < share_hi; ++tile) {
     const int tile_lo = uniform(list.cu[tile]), tile_hi = uniform(list.cu[tile + 1]);
     const int u_lo = uniform(z - tile_lo), steps = uniform(min(tile_hi, share_hi) - z);
-    const int req = uniform(list.r[tile]), q0 = uniform(a.list.first_tile + tile - list.first[tile]);
-    const Request rq = scalar_request(a.list.cu_new, a.list.seq_len, req, a.list.T, a.list.room);
-    const int p = uniform(rq.seq - rq.n + q0), hi = p + 1;
+    const int req = uniform(list.r[tile]), p = uniform(list.p[tile]), hi = p + 1;
     const int low = a.list.window > 0 ? max(0, p - a.list.window + 1) : 0;
     const Span span = span_of<kTokenUnit>(max(p, 0), p, a.list.window, a.list.sinks);
     const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
-    const int64_t row = rq.row0 + q0;
+    const int64_t row = uniform(list.row[tile]);
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
 
     Pieces<F32> qf[KS];
@@ -732,8 +727,9 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
             if (dim == 0) a.part_ml[at] = make_float2(m, den);
         }
     }
-    if (part >= 0 && z == tile_lo && threadIdx.x == 0)
-        *split = {int(row), a.GR, part, shares.worker_of(tile_hi - 1) - w};
+    if (z == tile_lo && threadIdx.x == 0)
+        a.split[size_t(tile) * a.G + g] = {int(row), a.GR, 2 * (w * a.G + g) + part,
+                                           part < 0 ? 0 : shares.worker_of(tile_hi - 1) - w};
     z += steps;
     if (z < share_hi) __syncthreads();   // the stages are free again
     }
@@ -747,15 +743,19 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // scores of row q at positions 32 m + 8 (i / 4) + 4 h + i % 4.
 constexpr int kTileUnit = 64;
 constexpr int kTileRows = 128;
+constexpr int kMinShare = 4;          // units of a share: a part is 64 KB
 constexpr int kBadPage = 1, kOdd = 2;
 
-template <bool F32>
+template <int HD, bool F8, bool F32>
 struct TileShape {
     static constexpr int kPerCu = F32 ? 1 : 2;   // workgroups that a CU's registers hold
+    // What parts and their merge cost a call, about 25 us, in the time of a unit (us, with a CU
+    // full of workgroups: 2.1, E4M3 2.6, fp32 2.9; heads of 64 1.5, 1.9 and 1.9).
+    static constexpr float kSplitCost = HD == 128 ? (F32 ? 8.f : F8 ? 9.f : 12.f) : (F32 || F8 ? 13.f : 16.f);
 };
 
 template <int HD, bool F8, bool F32>
-__global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void attend_tile(AttendArgs a) {
     constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32, NP = Pieces<F32>::N;
     using KSw = KSwizzle<RB>;
     using VSw = TileVSwizzle<RB>;
@@ -767,16 +767,26 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
     const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n = lane & 31, h = lane >> 5;
-    Split *split = a.split + size_t(w) * a.G + g;
-    if (threadIdx.x == 0 && w < a.workers) split->part = -1;
     const int tiles = build_list<kTileUnit>(a.list, list);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.tiles[0] = tiles;
     const int all_units = uniform(list.cu[tiles]);
     if (all_units == 0) return;
-    // Many tiles: one each, the last ones (of a request: the longest) first, if the last round
-    // of workgroups is full enough.  Fewer: even shares of the units.
-    const int workers = min(a.workers, all_units);   // none without a unit
-    const int rounds = (tiles + a.workers - 1) / a.workers;
-    const bool whole_tiles = rounds >= 2 && 20 * tiles >= 17 * rounds * a.workers;
+    // Whole tiles, the last ones (of a request: the longest) first, or even shares of the units.
+    // In units: even shares take all / workers and kSplitCost for the parts and their merge;
+    // whole tiles as long as the longest one (which runs faster towards the end, alone on its
+    // CU), or all / workers and what the last round, the first `rest` tiles, leaves idle.
+    const int workers = max(min(a.workers, all_units / kMinShare), 1);
+    const int rest = tiles % a.workers;
+    const float even = float(all_units) / a.workers;
+    float longest = 0.f;
+    for (int i = threadIdx.x; i < tiles; i += kThreads) longest = fmaxf(longest, float(list.cu[i + 1] - list.cu[i]));
+    longest = max_xor32(max_xor16(apex::ffn::row_max(longest)));
+    if (lane == 0) list.wave_end[wave] = int(longest);
+    __syncthreads();
+    longest = float(max(max(list.wave_end[0], list.wave_end[1]), max(list.wave_end[2], list.wave_end[3])));
+    const float idle = rest ? (1.f - float(rest) / a.workers) * list.cu[rest] / rest : 0.f;
+    const float whole = fmaxf((TileShape<HD, F8, F32>::kPerCu == 2 ? 0.75f : 1.f) * longest, even + idle);
+    const bool whole_tiles = uniform(whole <= even + TileShape<HD, F8, F32>::kSplitCost);
     const Shares shares(all_units, workers);
     int share_lo, share_hi, tile;
     if (whole_tiles) {
@@ -809,11 +819,9 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
     for (int z = share_lo; z < share_hi; ++tile) {
     const int tile_lo = uniform(list.cu[tile]), tile_hi = uniform(list.cu[tile + 1]);
     const int u_lo = uniform(z - tile_lo), steps = uniform(min(tile_hi, share_hi) - z);
-    const int req = uniform(list.r[tile]);
-    const int q0 = uniform((a.list.first_tile + tile - list.first[tile]) * a.list.tile_tokens);
-    const Request rq = scalar_request(a.list.cu_new, a.list.seq_len, req, a.list.T, a.list.room);
-    const int tokens = uniform(min(a.list.tile_tokens, rq.n - q0));
-    const int p_first = uniform(rq.seq - rq.n + q0), p_last = p_first + tokens - 1, hi = p_last + 1;
+    const int req = uniform(list.r[tile]), tokens = uniform(list.tokens[tile]);
+    const int row0 = uniform(list.row[tile]);
+    const int p_first = uniform(list.p[tile]), p_last = p_first + tokens - 1, hi = p_last + 1;
     const int low = a.list.window > 0 ? max(0, p_first - a.list.window + 1) : 0;
     const Span span = span_of<kTileUnit>(max(p_first, 0), p_last, a.list.window, a.list.sinks);
     const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
@@ -821,7 +829,7 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
     const bool row_on = tok < tokens;
     const bool wave_on = 32 * wave < tokens * a.GR;
     const int p = row_on ? p_first + tok : -1;
-    const int64_t row = rq.row0 + q0 + (row_on ? tok : 0);
+    const int64_t row = row0 + (row_on ? tok : 0);
     const int col = (g * a.GR + (row_on ? head : 0)) * HD;
 
     Pieces<F32> qf[KS];
@@ -843,7 +851,9 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
         const int from = low - j, keep = a.list.sinks - j;
         rows_ok = r.ok;
         if constexpr (F8) {
-            sc = scale_of[r.row + min(lane & 15, max(r.end - 1, 0))];
+            const int x = lane & 15;   // the scales of rows that are not read are 0
+            sc = scale_of[r.row + min(x, max(r.end - 1, 0))];
+            sc = x >= r.end || (x < from && x >= keep) ? 0.f : sc;
             const Extent kx = extent_of<HD>(a.k_pages, r), vx = extent_of<HD>(a.v_pages, r);
             const auto kr = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(kx.base), 0, kx.bytes, 0x00027000);
             const auto vr = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(vx.base), 0, vx.bytes, 0x00027000);
@@ -860,19 +870,25 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    // Chunk ch of row rr is 16 codes, two chunks of values: the second is at the first's place ^ 16
+    // (bytes); 8 rows further a key's is at ^ 128, a value's at the same.  Places are computed
+    // from one register each time: kept, they would be eight.
+    const int code_row = 16 * wave + lane / (HD / 16), code_ch = 2 * (lane % (HD / 16));
+    const int put_k = code_row * RB + 16 * (code_ch ^ KSw::of(code_row));
+    const int put_v = kV + code_row * RB + 16 * (code_ch ^ VSw::of(code_row));
     const auto commit = [&](auto which) __attribute__((always_inline)) {
         if constexpr (F8) {
+            static_assert(CPL <= 2 && (CPL == 1 || CRPI == 8), "places of the second load");
             uint8_t *lds = decltype(which)::value ? st1 : st0;
+            const int pk = settled(put_k), pv = settled(put_v);
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int c = 0; c < CPL; ++c) {
-                    const int rr = 16 * wave + CRPI * c + lane / (HD / 16), ch = 2 * (lane % (HD / 16));
-                    const int sw = x ? VSw::of(rr) : KSw::of(rr), at = x * kV + rr * RB;
-                    const uint4 v = codes[x][c];
-                    *reinterpret_cast<uint4 *>(lds + (at + 16 * (ch ^ sw))) = widen_e4m3(make_uint2(v.x, v.y));
-                    *reinterpret_cast<uint4 *>(lds + (at + 16 * ((ch + 1) ^ sw))) = widen_e4m3(make_uint2(v.z, v.w));
-                }
+            for (int c = 0; c < CPL; ++c) {
+                const uint4 k = codes[0][c], v = codes[1][c];
+                *reinterpret_cast<uint4 *>(lds + ((pk ^ 128 * c) + 8 * RB * c)) = widen_e4m3(make_uint2(k.x, k.y));
+                *reinterpret_cast<uint4 *>(lds + ((pk ^ 128 * c ^ 16) + 8 * RB * c)) = widen_e4m3(make_uint2(k.z, k.w));
+                *reinterpret_cast<uint4 *>(lds + (pv + 8 * RB * c)) = widen_e4m3(make_uint2(v.x, v.y));
+                *reinterpret_cast<uint4 *>(lds + ((pv ^ 16) + 8 * RB * c)) = widen_e4m3(make_uint2(v.z, v.w));
+            }
         }
     };
 
@@ -903,6 +919,7 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
                 for (int e = 0; e < 4; ++e)   // exponents of all ones carry into the sign's place
                     odd |= ((x[e] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
             }
+            if constexpr (F8) odd |= (__float_as_uint(sc) & 0x7f800000u) == 0x7f800000u;
             if (__ballot(odd)) flags |= kOdd;
         }
         if (lane == 0) group_flags[buf][wave] = uint8_t(flags);
@@ -981,8 +998,13 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
                 const int i = 8 * (u & 1) + e;
                 w[e] = __builtin_amdgcn_exp2f(fmaf(s[u / 2][i], a.scale_log2, -ref));
                 l += w[e];
-                if constexpr (F8)   // a scale that the row does not see may be anything
-                    w[e] = w[e] == 0.f ? 0.f : w[e] * scales[buf][1][16 * u + 8 * (e / 4) + 4 * h + e % 4];
+            }
+            if constexpr (F8) {
+                const float4 a4 = *reinterpret_cast<const float4 *>(&scales[buf][1][16 * u + 4 * h]);
+                const float4 b4 = *reinterpret_cast<const float4 *>(&scales[buf][1][16 * u + 8 + 4 * h]);
+                const float f[8] = {a4.x, a4.y, a4.z, a4.w, b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = CAREFUL && w[e] == 0.f ? 0.f : w[e] * f[e];
             }
         };
         // Where rows see different positions, a value that is no finite number must not meet the
@@ -1073,7 +1095,6 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
     };
     const auto work = [&](auto careful) __attribute__((always_inline)) {
         clear();
-        issue(Int<0>{}, 0);
         commit(Int<0>{});
         for (int i = 0; i < steps; i += 2) {
             step(Int<0>{}, careful, i);
@@ -1084,11 +1105,15 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
             }
         }
     };
+    issue(Int<0>{}, 0);
     work(Int<0>{});
     if (lane == 0) wave_odd[wave] = met_odd;
     wait_loads<0>();
     __syncthreads();
-    if (wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) work(Int<1>{});
+    if (wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) {
+        issue(Int<0>{}, 0);
+        work(Int<1>{});
+    }
     wait_loads<0>();
     l = sum_xor32(l);
     if (!row_on) {
@@ -1120,40 +1145,46 @@ __global__ __launch_bounds__(kThreads, TileShape<F32>::kPerCu) void attend_tile(
                     make_float4(o[d][4 * e4], o[d][4 * e4 + 1], o[d][4 * e4 + 2], o[d][4 * e4 + 3]);
         if (h == 0) a.part_ml[at] = make_float2(mx, l);
     }
-    if (part >= 0 && z == tile_lo && threadIdx.x == 0)
-        *split = {rq.row0 + q0, tokens * a.GR, part, shares.worker_of(tile_hi - 1) - w};
+    if (z == tile_lo && threadIdx.x == 0)
+        a.split[size_t(tile) * a.G + g] = {row0, tokens * a.GR, 2 * (w * a.G + g) + part,
+                                           part < 0 ? 0 : shares.worker_of(tile_hi - 1) - w};
     z += steps;
     if (z < share_hi) __syncthreads();   // the stages are free again
     }
 }
 
 // --------------------------------------------------------------------------------- merge
-// Tiles of one token: grid (workers * G, GR), a workgroup per row.  Groups of HD / 4 threads take
-// the parts in turn and meet in LDS.
-template <int HD, bool F32>
-__global__ __launch_bounds__(kThreads) void merge_tokens(AttendArgs a) {
-    constexpr int LPR = HD / 4, GROUPS = kThreads / LPR;
-    __shared__ float red_m[kWaves], red_d[GROUPS];
+// Part s of a split tile: the first worker's, then the next ones' first parts (even ones).
+__device__ __forceinline__ size_t part_of(const Split &sp, int G, int s) {
+    return s == 0 ? size_t(sp.part) : size_t(sp.part & ~1) + size_t(s) * 2 * G;
+}
+
+// Tiles of one token: grid (tiles * G, GR), a workgroup of N threads per row.  Groups of HD / 4
+// threads take the parts in turn and meet in LDS.
+template <int HD, bool F32, int N>
+__global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
+    constexpr int LPR = HD / 4, GROUPS = N / LPR, WAVES = N / kWave;
+    __shared__ float red_m[WAVES], red_d[GROUPS];
     __shared__ __align__(16) float red[GROUPS][HD];
-    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G, h = blockIdx.y;
-    const Split sp = a.split[size_t(w) * a.G + g];
-    if (sp.part < 0) return;
     const int t = threadIdx.x, wave = t / kWave, lane = t % kWave, group = t / LPR, at4 = t % LPR;
-    const auto slot = [&](int s) {   // part s: the first worker's, then the next ones' first parts
-        return ((size_t(w + s) * a.G + g) * 2 + (s == 0 ? sp.part : 0)) * kTokenRows + h;
-    };
+    const Split sp = a.split[blockIdx.x];
+    if (int(blockIdx.x) >= a.tiles[0] * a.G || sp.more <= 0) return;
+    const int g = blockIdx.x % a.G, h = blockIdx.y;
     float top = -INFINITY;
-    for (int s = t; s <= sp.more; s += kThreads) top = fmaxf(top, a.part_ml[slot(s)].x);
+    for (int s = t; s <= sp.more; s += N)
+        top = fmaxf(top, a.part_ml[part_of(sp, a.G, s) * kTokenRows + h].x);
     top = max_xor32(max_xor16(apex::ffn::row_max(top)));
     if (lane == 0) red_m[wave] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) top = fmaxf(top, red_m[v]);
     float den = 0.f;
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
     for (int s = group; s <= sp.more; s += GROUPS) {
-        const float2 ml = a.part_ml[slot(s)];
-        const float4 o = reinterpret_cast<const float4 *>(a.part_o + slot(s) * HD)[at4];
+        const size_t at = part_of(sp, a.G, s) * kTokenRows + h;
+        const float2 ml = a.part_ml[at];
+        const float4 o = reinterpret_cast<const float4 *>(a.part_o + at * HD)[at4];
         const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
         den = fmaf(ml.y, c, den);
         num.x = fmaf(o.x, c, num.x);
@@ -1164,37 +1195,35 @@ __global__ __launch_bounds__(kThreads) void merge_tokens(AttendArgs a) {
     *reinterpret_cast<float4 *>(&red[group][4 * at4]) = num;
     if (at4 == 0) red_d[group] = den;
     __syncthreads();
-    if (t >= HD) return;
-    float d = 0.f, v = 0.f;
+    if (t < HD) {
+        float d = 0.f, v = 0.f;
 #pragma unroll
-    for (int q = 0; q < GROUPS; ++q) {
-        d += red_d[q];
-        v += red[q][t];
+        for (int q = 0; q < GROUPS; ++q) {
+            d += red_d[q];
+            v += red[q][t];
+        }
+        store_out<F32>(a.out, sp.row * a.out_stride + (g * a.GR + h) * HD + t, d == 0.f ? 0.f : v / d);
     }
-    store_out<F32>(a.out, sp.row * a.out_stride + (g * a.GR + h) * HD + t, d == 0.f ? 0.f : v / d);
 }
 
-// Tiles of many rows: grid (workers * G, kMergeRows), HD / 4 lanes per row.
-constexpr int kMergeRows = 16;
+// Tiles of many rows: grid (tiles * G, y), HD / 4 lanes per row.
 template <int HD, bool F32>
 __global__ __launch_bounds__(kThreads) void merge_tiles(AttendArgs a) {
     constexpr int LPR = HD / 4, PER = kThreads / LPR;   // rows at a time
-    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
-    const Split sp = a.split[size_t(w) * a.G + g];
-    if (sp.part < 0) return;
-    const int at4 = threadIdx.x % LPR;
+    const Split sp = a.split[blockIdx.x];
+    if (int(blockIdx.x) >= a.tiles[0] * a.G || sp.more <= 0) return;
+    const int at4 = threadIdx.x % LPR, g = blockIdx.x % a.G;
     for (int m = blockIdx.y * PER + threadIdx.x / LPR; m < sp.rows; m += gridDim.y * PER) {
-        const auto slot = [&](int s) {
-            return ((size_t(w + s) * a.G + g) * 2 + (s == 0 ? sp.part : 0)) * kTileRows + m;
-        };
         float top = -INFINITY;
-        for (int s = 0; s <= sp.more; ++s) top = fmaxf(top, a.part_ml[slot(s)].x);
+#pragma unroll 8
+        for (int s = 0; s <= sp.more; ++s) top = fmaxf(top, a.part_ml[part_of(sp, a.G, s) * kTileRows + m].x);
         float den = 0.f;
         float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
         for (int s = 0; s <= sp.more; ++s) {
-            const float2 ml = a.part_ml[slot(s)];
-            const float4 o = reinterpret_cast<const float4 *>(a.part_o + slot(s) * HD)[at4];
+            const size_t at = part_of(sp, a.G, s) * kTileRows + m;
+            const float2 ml = a.part_ml[at];
+            const float4 o = reinterpret_cast<const float4 *>(a.part_o + at * HD)[at4];
             const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
             den = fmaf(ml.y, c, den);
             num.x = fmaf(o.x, c, num.x);
@@ -1237,8 +1266,8 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
     p.max_tiles = T / p.tile_tokens + std::min(T, R);
     p.most_workers = std::max(1, 2 * kCus / G);
     const auto up = [](size_t v) { return apex::align_up(v, 256); };
-    const size_t shares = size_t(p.most_workers) * G, parts = 2 * shares * p.rows;
-    p.at_ml = up(shares * sizeof(Split));
+    const size_t parts = 2 * size_t(p.most_workers) * G * p.rows;
+    p.at_ml = 256 + up(size_t(std::min(p.max_tiles, kListTiles)) * G * sizeof(Split));
     p.at_o = p.at_ml + up(parts * sizeof(float2));
     p.bytes = p.at_o + up(parts * hd * sizeof(float));
     return p;
@@ -1246,19 +1275,27 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
 
 template <int HD, bool F8, bool F32>
 apex_status launch_attention(const Plan &p, hipStream_t st, AttendArgs a) {
-    const int per_cu = p.token ? TokenShape<HD, F8, F32>::kPerCu : TileShape<F32>::kPerCu;
+    const int per_cu = p.token ? TokenShape<HD, F8, F32>::kPerCu : TileShape<HD, F8, F32>::kPerCu;
     a.workers = std::max(1, kCus * per_cu / a.G);
     for (int f = 0; f < p.max_tiles; f += kListTiles) {
         a.list.first_tile = f;
+        const int tiles = std::min(p.max_tiles - f, kListTiles);
+        // no more workers than there can be shares
+        const int64_t most = int64_t(tiles) * (a.list.room / (p.token ? kTokenUnit : kTileUnit) + 1) /
+                                 (p.token ? 1 : kMinShare) + 1;
+        const int workers = int(std::min(int64_t(a.workers), most)), x = tiles * a.G;
         if (p.token) {
-            hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3(a.workers * a.G), dim3(kThreads), 0, st, a);
-            hipLaunchKernelGGL((merge_tokens<HD, F32>), dim3(a.workers * a.G, a.GR), dim3(kThreads), 0, st, a);
+            hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3(workers * a.G), dim3(kThreads), 0, st, a);
+            // few tiles have many parts
+            if (x <= 64)
+                hipLaunchKernelGGL((merge_tokens<HD, F32, 512>), dim3(x, a.GR), dim3(512), 0, st, a);
+            else
+                hipLaunchKernelGGL((merge_tokens<HD, F32, 256>), dim3(x, a.GR), dim3(256), 0, st, a);
         } else {
-            const int tiles = std::min(p.max_tiles - f, kListTiles);
-            hipLaunchKernelGGL((attend_tile<HD, F8, F32>), dim3(std::max(a.workers, tiles) * a.G),
+            hipLaunchKernelGGL((attend_tile<HD, F8, F32>), dim3(std::max(workers, tiles) * a.G), dim3(kThreads),
+                               0, st, a);
+            hipLaunchKernelGGL((merge_tiles<HD, F32>), dim3(x, std::max(1, std::min(8192 / x, 16))),
                                dim3(kThreads), 0, st, a);
-            hipLaunchKernelGGL((merge_tiles<HD, F32>), dim3(a.workers * a.G, kMergeRows), dim3(kThreads), 0,
-                               st, a);
         }
         APEX_HIP(hipGetLastError());
     }
@@ -1339,7 +1376,8 @@ extern "C" apex_status apex_attention_paged(const apex_paged_cache *cache, const
     a.n_pages = cache->n_pages;
     a.workers = 1;
     a.scale_log2 = scale * kLog2e;
-    a.split = reinterpret_cast<Split *>(ws);
+    a.tiles = reinterpret_cast<int *>(ws);
+    a.split = reinterpret_cast<Split *>(ws + 256);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.at_ml);
     a.part_o = reinterpret_cast<float *>(ws + p.at_o);
     const bool f32 = dtype == APEX_TYPE_FP32, f8 = cache->format == APEX_KV_FP8_E4M3;

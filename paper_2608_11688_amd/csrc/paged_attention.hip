@@ -748,7 +748,8 @@ constexpr int kBadPage = 1, kOdd = 2;
 
 template <int HD, bool F8, bool F32>
 struct TileShape {
-    static constexpr int kPerCu = F32 ? 1 : 2;   // workgroups that a CU's registers hold
+    // workgroups that a CU's registers hold
+    static constexpr int kPerCu = HD == 128 ? (F32 ? 1 : 2) : (F8 || F32 ? 2 : 3);
     // What parts and their merge cost a call, about 25 us, in the time of a unit (us, with a CU
     // full of workgroups: 2.1, E4M3 2.6, fp32 2.9; heads of 64 1.5, 1.9 and 1.9).
     static constexpr float kSplitCost = HD == 128 ? (F32 ? 8.f : F8 ? 9.f : 12.f) : (F32 || F8 ? 13.f : 16.f);
@@ -792,6 +793,9 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     if (whole_tiles) {
         if (w >= tiles) return;
         tile = tiles - 1 - w;
+        // one round: workgroup i + 256 comes to workgroup i's CU, so a long one meets a short one
+        if (TileShape<HD, F8, F32>::kPerCu == 2 && tiles <= a.workers && w >= a.workers / 2)
+            tile = w - a.workers / 2;
         share_lo = uniform(list.cu[tile]);
         share_hi = uniform(list.cu[tile + 1]);
     } else {
@@ -1264,7 +1268,7 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
     p.tile_tokens = p.token ? 1 : kTileRows / p.GR;
     p.rows = p.token ? kTokenRows : kTileRows;
     p.max_tiles = T / p.tile_tokens + std::min(T, R);
-    p.most_workers = std::max(1, 2 * kCus / G);
+    p.most_workers = std::max(1, (p.token || hd == 128 ? 2 : 3) * kCus / G);
     const auto up = [](size_t v) { return apex::align_up(v, 256); };
     const size_t parts = 2 * size_t(p.most_workers) * G * p.rows;
     p.at_ml = 256 + up(size_t(std::min(p.max_tiles, kListTiles)) * G * sizeof(Split));

@@ -178,12 +178,14 @@ def plan_lib():
 
 
 def ptr(a):
-    if a is None:
-        return None
+    if a is None or type(a) is int:
+        return a
+    try:
+        return a.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(a, int):
         return a
-    if hasattr(a, "data_ptr"):
-        return a.data_ptr()
     if hasattr(a, "ctypes"):
         return a.ctypes.data
     if isinstance(a, C.c_void_p):

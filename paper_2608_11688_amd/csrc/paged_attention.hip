@@ -344,15 +344,16 @@ struct Rows16 {
     int end;            // rows 0..end-1 exist for the tile
     bool ok;            // the page id is in range
 };
-__device__ __forceinline__ Rows16 rows16(const AttendArgs &a, const int32_t *table, int g, int j0,
-                                         int hi) {
+__device__ __forceinline__ Rows16 rows_of_page(const AttendArgs &a, int page, int g, int j0, int hi) {
     Rows16 r;
-    const int b = min(j0 >> a.shift, a.max_blocks - 1);
-    const int page = j0 < hi ? scalar_load(table, b) : -1;
-    r.ok = page >= 0 && page < a.n_pages;
+    r.ok = page >= 0 && page < a.n_pages && j0 < hi;
     r.row = r.ok ? (int64_t(page) * a.G + g) * a.page_size + (j0 & (a.page_size - 1)) : 0;
     r.end = r.ok ? min(max(hi - j0, 0), 16) : 0;
     return r;
+}
+__device__ __forceinline__ Rows16 rows16(const AttendArgs &a, const int32_t *table, int g, int j0, int hi) {
+    const int b = min(j0 >> a.shift, a.max_blocks - 1);
+    return rows_of_page(a, j0 < hi ? scalar_load(table, b) : -1, g, j0, hi);
 }
 
 template <int N>
@@ -420,6 +421,7 @@ __device__ __forceinline__ uint2 lds_tr8(const uint8_t *p, int at) {
 // One of two pointers by the lane, chosen here and now (the compiler would rather load it from the
 // arguments each time).
 typedef const __attribute__((address_space(1))) float *GlobalFloats;   // of memory, not LDS
+typedef const __attribute__((address_space(1))) int *GlobalInts;
 __device__ __forceinline__ GlobalFloats lane_pointer(const float *p, const float *q, bool second) {
     const uint64_t x = reinterpret_cast<uint64_t>(p), y = reinterpret_cast<uint64_t>(q);
     const int lo = settled(second ? int(y) : int(x)), hi = settled(second ? int(y >> 32) : int(x >> 32));
@@ -722,7 +724,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
         if (part < 0) {
             store_out<F32>(a.out, row * a.out_stride + (g * a.GR + h) * HD + dim, den == 0.f ? 0.f : num / den);
         } else {
-            const size_t at = ((size_t(w) * a.G + g) * 2 + part) * kTokenRows + h;
+            const size_t at = unsigned((2 * (w * a.G + g) + part) * kTokenRows + h);
             a.part_o[at * HD + dim] = num;
             if (dim == 0) a.part_ml[at] = make_float2(m, den);
         }
@@ -847,11 +849,19 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     float sc = 0.f;
     bool rows_ok = false;
     uint4 codes[2][CPL];
+    // A unit's page id is loaded a unit ahead, as a vector load: a scalar one would be waited for
+    // with the reads of LDS.
+    int page = -1;
+    const auto rows_at = [&](int i) { return span.base(u_lo + min(i, steps - 1), kTileUnit) + 16 * wave; };
+    const auto load_page = [&](int i) {
+        page = ((GlobalInts)(table))[min(rows_at(i) >> a.shift, a.max_blocks - 1)];
+    };
     const auto issue = [&](auto which, int i) __attribute__((always_inline)) {
         uint8_t *lds = decltype(which)::value ? st1 : st0;
         const int at = 16 * wave * RB;
-        const int j = span.base(u_lo + min(i, steps - 1), kTileUnit) + 16 * wave;
-        const Rows16 r = rows16(a, table, g, j, i < steps ? hi : 0);
+        const int j = rows_at(i);
+        const Rows16 r = rows_of_page(a, uniform(page), g, j, i < steps ? hi : 0);
+        load_page(i + 1);
         const int from = low - j, keep = a.list.sinks - j;
         rows_ok = r.ok;
         if constexpr (F8) {
@@ -872,8 +882,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
             load_rows16<RB, KSw>(a.k_pages, r, from, keep, lds, at, 16 * wave);
             load_rows16<RB, VSw>(a.v_pages, r, from, keep, lds, kV + at, 16 * wave);
         }
-        __builtin_amdgcn_sched_barrier(0);
     };
+    constexpr int kIssued = F8 ? 2 * CPL + 2 : RB / 32 + 1;   // loads of an issue
     // Chunk ch of row rr is 16 codes, two chunks of values: the second is at the first's place ^ 16
     // (bytes); 8 rows further a key's is at ^ 128, a value's at the same.  Places are computed
     // from one register each time: kept, they would be eight.
@@ -928,11 +938,14 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         }
         if (lane == 0) group_flags[buf][wave] = uint8_t(flags);
         lds_barrier();
+        if (!wave_on) {
+            issue(Int<1 - buf>{}, i + 1);
+            return;
+        }
+        const int flags_read = *reinterpret_cast<const int *>(group_flags[buf]);
+        // Keys are read AHEAD products before their own; the next unit's loads go out between the
+        // products (all at once, the four wavefronts' queue up at the CU's address unit: 800 cycles).
         issue(Int<1 - buf>{}, i + 1);
-        if (!wave_on) return;
-        const int all_flags = uniform(*reinterpret_cast<const int *>(group_flags[buf]));
-        __builtin_amdgcn_sched_barrier(0);
-        // keys are read AHEAD products before their own
         constexpr int NK = 2 * KS, AHEAD = 4;
         const auto load_k = [&](int x) { return lds_u4(lds, k_at[x % KS] + 32 * (x / KS) * RB); };
         uint4 kf[AHEAD];
@@ -961,8 +974,10 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         for (int x = 0; x < NK; ++x) {
             __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);  // matrix products
             if (x + AHEAD < NK) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (x < kIssued) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // loads
         }
         __builtin_amdgcn_sched_barrier(0);
+        const int all_flags = uniform(flags_read);
         if constexpr (F8)
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -1109,12 +1124,14 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
             }
         }
     };
+    load_page(0);
     issue(Int<0>{}, 0);
     work(Int<0>{});
     if (lane == 0) wave_odd[wave] = met_odd;
     wait_loads<0>();
     __syncthreads();
     if (wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) {
+        load_page(0);
         issue(Int<0>{}, 0);
         work(Int<1>{});
     }
@@ -1140,7 +1157,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                         make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
             }
     } else {
-        const size_t at = ((size_t(w) * a.G + g) * 2 + part) * kTileRows + m_row;
+        const size_t at = unsigned((2 * (w * a.G + g) + part) * kTileRows + settled(m_row));
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll

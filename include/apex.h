@@ -430,7 +430,7 @@ apex_status apex_paged_plan(const int32_t *cached, const int32_t *n_new, int R, 
  *   k, v        device, type `dtype` (apex_type): token t's row [G, hd] at k + t * k_stride;
  *               strides in values, at least G * hd and multiples of 16 bytes
  *   slot_map    device int32 [T]: tokens whose slot is outside [0, n_pages * page_size) are
- *               left out.  Slots must differ: of tokens with one slot, any may stay there.
+ *               left out.  Slots must differ: what one that two tokens name holds is undefined.
  */
 apex_status apex_paged_store(const apex_paged_cache *cache, const void *k, const void *v, int dtype,
                              int T, int64_t k_stride, int64_t v_stride, const int32_t *slot_map,

@@ -21,6 +21,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "common.h"
@@ -77,7 +78,7 @@ __device__ __forceinline__ Span span_of(int p_first, int p_last, int window, int
     Span s;
     const int low = window > 0 ? max(0, p_first - window + 1) : 0;
     s.first = low / UP;
-    s.sinks = window > 0 ? min((min(sinks, p_last + 1) + UP - 1) / UP, s.first) : 0;
+    s.sinks = window > 0 ? min(int((unsigned(min(sinks, p_last + 1)) + UP - 1) / UP), s.first) : 0;
     s.units = p_last < 0 ? 0 : p_last / UP + 1 - s.first + s.sinks;
     return s;
 }
@@ -141,11 +142,11 @@ __device__ __forceinline__ int block_scan(int v, int *wave_end, int *before, int
 
 struct ListArgs {
     const int32_t *cu_new, *seq_len;
-    int R, T, room, tile_tokens, first_tile, window, sinks;
+    int R, T, room, tile_tokens, first_tile, most_tiles, window, sinks;
 };
 
-// Tiles first_tile .. first_tile + 511 of all requests' tiles, those of a request in a row;
-// returns how many there are.  A few round trips to memory and barriers, about 3 us, where a
+// Tiles first_tile .. first_tile + most_tiles - 1 of all requests' tiles, those of a request in a
+// row; returns how many there are.  A few round trips to memory and barriers, about 3 us, where a
 // launch of its own that wrote the list for the next one took 7.  Loops are kept rolled: a
 // launch this short waits for its instructions as much as for its data.
 template <int UP>
@@ -174,7 +175,7 @@ __device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
         }
         at += n;
     }
-    const int tiles = min(max(total - a.first_tile, 0), kListTiles);
+    const int tiles = min(max(total - a.first_tile, 0), a.most_tiles);
     __syncthreads();
     // a thread's tiles, in a row; the tiles between two named ones are the first one's
     const int each = (tiles + kThreads - 1) / kThreads, i0 = t * each, i1 = min(i0 + each, tiles);
@@ -471,11 +472,16 @@ __device__ __forceinline__ void store_out(void *out, int64_t at, float v) {
 
 // ------------------------------------------------------------------------- one token's tile
 // A tile is one token and the query heads of a group: up to 16 rows, columns of the 16x16x32
-// products.  Each of four wavefronts takes 32 of a unit's 128 positions, with a ring of stages
-// of its own in LDS: no barrier stands in the loop, only the wavefront's own count of loads.
+// products.  Each wavefront is a worker of its own, on units of 32 positions, with a ring of
+// stages in LDS: behind the list no barrier, only the wavefront's own count of loads.  (Four
+// wavefronts on one tile, joined in LDS: 256 requests of 64 to 256 positions 60 us instead of
+// 42, where a tile is over before its loads are under way; long contexts the same.)
 // Lane (q = lane % 16, lg = lane / 16) holds the scores of row q at positions 16 m + 4 lg + i.
-constexpr int kTokenUnit = 128;
-constexpr int kTokenRows = 16;
+// Bound by the stream of keys and values: 64 tokens under a window of 4096 (1.08 GB) 187 us,
+// 5.75 TB/s, of 5.8 that a kernel that only reads gets.
+constexpr int kTokenUnit = 32;
+constexpr int kMostParts = 512;   // of a launch's tiles, on average: one request of 60000 positions
+                                  // in one group 21 us; in 1024 parts, as many as fit, 24, in 128 28
 
 template <int HD, bool F8, bool F32>
 struct TokenShape {
@@ -498,21 +504,31 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     __shared__ __align__(1024) uint8_t st2[NS > 2 ? kWaves : 1][NS > 2 ? S::kStage : 16];
     __shared__ __align__(1024) uint8_t st3[NS > 2 ? kWaves : 1][NS > 2 ? S::kStage : 16];
     __shared__ __align__(16) float scales[kWaves][64];
-    __shared__ float red_m[kWaves][kTokenRows], red_l[kWaves][kTokenRows];
     __shared__ TileList list;
-    static_assert(sizeof(st0) >= kWaves * kTokenRows * HD * sizeof(float), "merge room");
-    const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
+    const int wg = uniform(blockIdx.x / a.G), g = blockIdx.x - wg * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int w = wg * kWaves + wave;
     const int n = lane & 15, lg = lane >> 4;
     const int tiles = build_list<kTokenUnit>(a.list, list);
     if (blockIdx.x == 0 && threadIdx.x == 0) a.tiles[0] = tiles;
     const int all_units = uniform(list.cu[tiles]);
     if (all_units == 0) return;
-    const int workers = min(a.workers, all_units);   // none without a unit
+    // none without a unit
+    const int workers = min(a.workers, min(all_units, kMostParts * tiles));
     if (w >= workers) return;
     const Shares shares(all_units, workers);
     const int share_lo = uniform(shares.begin(w)), share_hi = uniform(shares.begin(w + 1));
-    int tile = tile_of(list, tiles, share_lo);
+    int tile = 0;
+    for (int i0 = 0; i0 < tiles; i0 += kWave) {
+        const int i = i0 + lane;
+        const unsigned long long here =
+            __ballot(i < tiles && list.cu[min(i, tiles - 1)] <= share_lo && share_lo < list.cu[min(i, tiles - 1) + 1]);
+        if (here) {
+            tile = i0 + __ffsll(static_cast<long long>(here)) - 1;
+            break;
+        }
+    }
+    tile = uniform(tile);
 
     // where this lane reads, in a stage: keys of row n (and n + 16), values of row v_row (and,
     // bf16, v_row + 16); both swizzles are the same 16 rows further
@@ -558,7 +574,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 
     const auto issue = [&](auto which, int i) __attribute__((always_inline)) {
         constexpr int st = decltype(which)::value;
-        const int j0 = span.base(u_lo + min(i, steps - 1), kTokenUnit) + 32 * wave;
+        const int j0 = span.base(u_lo + min(i, steps - 1), kTokenUnit);
         const int end = i < steps ? hi : 0;
         Rows16 r[2];
 #pragma unroll
@@ -594,7 +610,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
         constexpr int ahead = (st + NS - 1) % NS;
         issue(Int<ahead>{}, i + NS - 1);
         wait_loads<S::kLoads *(NS - 1)>();
-        const int j0 = span.base(u_lo + i, kTokenUnit) + 32 * wave;
+        const int j0 = span.base(u_lo + i, kTokenUnit);
         const uint8_t *lds = stage(which);
         float ks[8], vs[8];
         if constexpr (F8) {
@@ -696,45 +712,36 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
             if (++i == steps) break;
         }
     }
-    // the wavefronts' shares joined in LDS, over the first stage
-    wait_loads<0>();
-    __syncthreads();
-    float(*red)[kTokenRows][HD] = reinterpret_cast<float(*)[kTokenRows][HD]>(&st0[0][0]);
     l = sum_xor32(sum_xor16(l));
-    if (lg == 0) {
-        red_m[wave][n] = mx;
-        red_l[wave][n] = l;
-    }
+    if (n < a.GR) {
+        const size_t at = unsigned((2 * (w * a.G + g) + max(part, 0)) * a.GR + n);
+        const int64_t out = row * a.out_stride + (g * a.GR + n) * HD;
+        const float inv = 1.f / l;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<floatx4 *>(&red[wave][n][16 * d + 4 * lg]) = o[d];
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < a.GR * HD; idx += kThreads) {
-        const int h = idx / HD, dim = idx % HD;
-        float m = red_m[0][h];
+        for (int d = 0; d < DT; ++d) {
+            const int dim = 16 * d + 4 * lg;
+            if (part >= 0) {
+                *reinterpret_cast<floatx4 *>(a.part_o + at * HD + dim) = o[d];
+                continue;
+            }
+            float v[4];
 #pragma unroll
-        for (int v = 1; v < kWaves; ++v) m = fmaxf(m, red_m[v][h]);
-        float den = 0.f, num = 0.f;
-#pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-            const float c = red_m[v][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[v][h] - m);
-            den = fmaf(red_l[v][h], c, den);
-            num = fmaf(red[v][h][dim], c, num);
+            for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[d][e] * inv;
+            if constexpr (F32)
+                *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + out + dim) =
+                    make_float4(v[0], v[1], v[2], v[3]);
+            else
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + out + dim) =
+                    make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
         }
-        if (part < 0) {
-            store_out<F32>(a.out, row * a.out_stride + (g * a.GR + h) * HD + dim, den == 0.f ? 0.f : num / den);
-        } else {
-            const size_t at = unsigned((2 * (w * a.G + g) + part) * kTokenRows + h);
-            a.part_o[at * HD + dim] = num;
-            if (dim == 0) a.part_ml[at] = make_float2(m, den);
-        }
+        if (part >= 0 && lg == 0) a.part_ml[at] = make_float2(mx, l);
     }
-    if (z == tile_lo && threadIdx.x == 0)
+    if (z == tile_lo && lane == 0)
         a.split[size_t(tile) * a.G + g] = {int(row), a.GR, 2 * (w * a.G + g) + part,
                                            part < 0 ? 0 : shares.worker_of(tile_hi - 1) - w};
     z += steps;
-    if (z < share_hi) __syncthreads();   // the stages are free again
     }
+    wait_loads<0>();   // no load into LDS outlives the workgroup
 }
 
 // ---------------------------------------------------------------------- tiles of many rows
@@ -1193,7 +1200,7 @@ __global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
     const int g = blockIdx.x % a.G, h = blockIdx.y;
     float top = -INFINITY;
     for (int s = t; s <= sp.more; s += N)
-        top = fmaxf(top, a.part_ml[part_of(sp, a.G, s) * kTokenRows + h].x);
+        top = fmaxf(top, a.part_ml[part_of(sp, a.G, s) * a.GR + h].x);
     top = max_xor32(max_xor16(apex::ffn::row_max(top)));
     if (lane == 0) red_m[wave] = top;
     __syncthreads();
@@ -1203,7 +1210,7 @@ __global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (int s = group; s <= sp.more; s += GROUPS) {
-        const size_t at = part_of(sp, a.G, s) * kTokenRows + h;
+        const size_t at = part_of(sp, a.G, s) * a.GR + h;
         const float2 ml = a.part_ml[at];
         const float4 o = reinterpret_cast<const float4 *>(a.part_o + at * HD)[at4];
         const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
@@ -1283,9 +1290,10 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
     // is worked on token by token
     p.token = T <= R;
     p.tile_tokens = p.token ? 1 : kTileRows / p.GR;
-    p.rows = p.token ? kTokenRows : kTileRows;
-    p.max_tiles = T / p.tile_tokens + std::min(T, R);
-    p.most_workers = std::max(1, (p.token || hd == 128 ? 2 : 3) * kCus / G);
+    p.rows = p.token ? p.GR : kTileRows;
+    // the sum of ceil(n / tile_tokens) over min(T, R) requests that have any of T tokens
+    p.max_tiles = int((T + int64_t(p.tile_tokens - 1) * std::min(T, R)) / p.tile_tokens);
+    p.most_workers = p.token ? kWaves * std::max(1, 2 * kCus / G) : std::max(1, (hd == 128 ? 2 : 3) * kCus / G);
     const auto up = [](size_t v) { return apex::align_up(v, 256); };
     const size_t parts = 2 * size_t(p.most_workers) * G * p.rows;
     p.at_ml = 256 + up(size_t(std::min(p.max_tiles, kListTiles)) * G * sizeof(Split));
@@ -1297,19 +1305,26 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
 template <int HD, bool F8, bool F32>
 apex_status launch_attention(const Plan &p, hipStream_t st, AttendArgs a) {
     const int per_cu = p.token ? TokenShape<HD, F8, F32>::kPerCu : TileShape<HD, F8, F32>::kPerCu;
-    a.workers = std::max(1, kCus * per_cu / a.G);
-    for (int f = 0; f < p.max_tiles; f += kListTiles) {
+    a.workers = std::max(1, kCus * per_cu / a.G) * (p.token ? kWaves : 1);
+    // a launch's units are counted in 32 bits
+    const int unit = p.token ? kTokenUnit : kTileUnit;
+    const int at_once = std::min(kListTiles, INT_MAX / (a.list.room / unit + 2));
+    for (int f = 0; f < p.max_tiles; f += at_once) {
+        const int tiles = std::min(p.max_tiles - f, at_once);
         a.list.first_tile = f;
-        const int tiles = std::min(p.max_tiles - f, kListTiles);
+        a.list.most_tiles = tiles;
         // no more workers than there can be shares
-        const int64_t most = int64_t(tiles) * (a.list.room / (p.token ? kTokenUnit : kTileUnit) + 1) /
+        const int64_t most = int64_t(tiles) * (a.list.room / unit + 1) /
                                  (p.token ? 1 : kMinShare) + 1;
         const int workers = int(std::min(int64_t(a.workers), most)), x = tiles * a.G;
         if (p.token) {
-            hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3(workers * a.G), dim3(kThreads), 0, st, a);
-            // few tiles have many parts
+            hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3((workers + kWaves - 1) / kWaves * a.G),
+                               dim3(kThreads), 0, st, a);
+            // Few tiles have many parts: 4 requests of 24000 positions in 8 groups 4.8 us with 1024
+            // threads, 6.1 with 512; 256 requests' tiles of a few parts each 5.5 with 256, 18.9
+            // with 1024.
             if (x <= 64)
-                hipLaunchKernelGGL((merge_tokens<HD, F32, 512>), dim3(x, a.GR), dim3(512), 0, st, a);
+                hipLaunchKernelGGL((merge_tokens<HD, F32, 1024>), dim3(x, a.GR), dim3(1024), 0, st, a);
             else
                 hipLaunchKernelGGL((merge_tokens<HD, F32, 256>), dim3(x, a.GR), dim3(256), 0, st, a);
         } else {
@@ -1388,7 +1403,7 @@ extern "C" apex_status apex_attention_paged(const apex_paged_cache *cache, const
     a.k_scales = cache->k_scales;
     a.v_scales = cache->v_scales;
     a.block_table = block_table;
-    a.list = {cu_new, seq_len, R, T, max_blocks * page_size, p.tile_tokens, 0, window, sinks};
+    a.list = {cu_new, seq_len, R, T, max_blocks * page_size, p.tile_tokens, 0, 0, window, sinks};
     a.G = G;
     a.GR = p.GR;
     a.max_blocks = max_blocks;

@@ -200,7 +200,8 @@ __global__ __launch_bounds__(N) void paged_plan(PlanArgs a) {
     }
     const int first = blockIdx.x * N + t, step = gridDim.x * N;
 #pragma unroll 1
-    for (int s = first; s < a.T; s += step) {
+    for (unsigned u = first; u < unsigned(a.T); u += step) {   // (T + step may pass 2^31)
+        const int s = int(u);
         int slot = -1, p = -1;
         if (s < last_tok) {
             const int r = owner(cu_tok, a.R, s);
@@ -419,7 +420,7 @@ extern "C" apex_status apex_paged_store(const apex_paged_cache *cache, const voi
                       cache->page_size, apex::log2_of(cache->page_size),
                       cache->n_pages * cache->page_size};
     const int64_t blocks = (a.rows * (hd / 8) + kStoreThreads - 1) / kStoreThreads;
-    if (blocks > INT_MAX)
+    if (blocks > UINT32_MAX / kStoreThreads)   // a grid has fewer than 2^32 threads
         return apex::fail(APEX_E_UNSUPPORTED, "%s: T=%d tokens of %d heads are too many", fn, T, G);
     const dim3 grid(unsigned(blocks), 2);
     const bool f32 = dtype == APEX_TYPE_FP32, f8 = cache->format == APEX_KV_FP8_E4M3;

@@ -176,6 +176,45 @@ def test_chunks(torch, reqs, H, G, hd, page, window, sinks, pad, fmt, dtype):
     print(c.check(window, sinks))
 
 
+# more than the 512 tiles of a launch, groups that do not divide the workgroups, one request's
+# tokens among requests without any: requests, new tokens of a request, longest, H, G, hd
+MANY = [
+    (700, lambda rng, R: np.ones(R, int), 90, 4, 2, 64),
+    (1100, lambda rng, R: rng.integers(0, 2, R), 70, 2, 1, 128),
+    (600, lambda rng, R: rng.integers(8, 10, R), 40, 16, 1, 64),        # 8 tokens a tile: a second tile of one
+    (40, lambda rng, R: np.where(np.arange(R) == 17, 30, 0), 300, 6, 3, 128),
+    (3, lambda rng, R: np.ones(R, int), 500, 66, 33, 64),
+    (2, lambda rng, R: np.ones(R, int), 600, 520, 520, 64),             # fewer workgroups than groups
+    (2, lambda rng, R: np.array([70, 3]), 100, 300, 300, 64),
+    (1, lambda rng, R: np.ones(R, int), 40000, 8, 1, 128),              # one tile in very many parts
+]
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("R,new,longest,H,G,hd", MANY, ids=[f"R{c[0]}-{c[2]}-H{c[3]}-G{c[4]}" for c in MANY])
+def test_many_tiles_groups_and_parts(torch, R, new, longest, H, G, hd, fmt, dtype):
+    rng = np.random.default_rng(R)
+    n = new(rng, R)
+    lens = [longest if r == 0 else int(x + rng.integers(0, max(longest - x, 1))) for r, x in enumerate(n)]
+    c = Case(torch, lens, n, H, G, hd, 16, fmt, dtype, pad=1 if R > 1 else 0, seed=12)
+    print(c.check())
+
+
+@pytest.mark.parametrize("H", [1, 16])
+def test_lengths_that_count_tokens_twice_stay_inside(torch, H):
+    """cu_new that goes back and forth: more tiles than T tokens have.  Which rows are written is
+    open; nothing outside of `out` and the workspace is."""
+    c = Case(torch, [40] * 6, [4] * 6, H, 1, 64, 16, "bf16", "bf16", seed=13)
+    c.device()
+    n = c.ws.numel()
+    c.ws = torch.full((n + 65536,), 0xAB, dtype=torch.uint8, device="cuda")
+    c.dcu.copy_(i32(torch, [0, 24, 0, 24, 0, 24, 0]))
+    native.apex_attention_paged(c.cache, c.dq, "bf16", c.T, c.R, H, c.dq.stride(0), c.dcu, c.dseq, c.dtable, c.nb, 0,
+                                0, 0.125, c.out, c.out.stride(0), c.ws, n)
+    torch.cuda.synchronize()
+    assert (c.ws[n:] == 0xAB).all()
+
+
 @pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
 @pytest.mark.parametrize("new", [1, 6])
 def test_pages_with_ids_out_of_range_are_left_out(torch, new, fmt, dtype):
@@ -548,3 +587,32 @@ def test_two_streams_with_workspaces_of_their_own(torch):
         b.call(stream=streams[1].cuda_stream)
     torch.cuda.synchronize()
     assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+
+
+def test_two_graphs_that_share_a_workspace(torch):
+    """Replayed in turn on one stream, with eager calls between: nothing in the workspace is kept
+    from one call for the next."""
+    a = Case(torch, [4000, 50], [1, 1], 8, 2, 128, 16, "bf16", "bf16", seed=32)
+    b = Case(torch, [2900, 400], [100, 7], 8, 2, 128, 16, "fp8", "bf16", seed=33)
+    a.device(), b.device()
+    a.ws = b.ws = max(a.ws, b.ws, key=lambda w: w.numel())
+    a.call(), b.call()
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    graphs = []
+    for c in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.call(stream=torch.cuda.current_stream().cuda_stream)
+        graphs.append(g)
+    for i in range(4):
+        a.out.zero_(), b.out.zero_()
+        if i == 2:
+            a.ws.fill_(0x55)
+        for g in graphs if i % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+        b.call(out=b.out)
+        torch.cuda.synchronize()
+        assert torch.equal(b.out, want[1])

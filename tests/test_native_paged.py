@@ -60,6 +60,10 @@ def test_store_refuses(kw):
     refused(INVAL, lambda: store(cache(), **kw))
 
 
+def test_store_of_more_rows_than_a_grid_has():
+    refused(UNSUPPORTED, lambda: store(cache(G=1024), T=2 ** 31 - 1, ks=1024 * 128, vs=1024 * 128))
+
+
 @pytest.mark.parametrize("status,kw", [
     (INVAL, dict(T=-1)), (INVAL, dict(R=-1)), (INVAL, dict(dtype=-1)), (INVAL, dict(H=20)), (INVAL, dict(H=0)),
     (UNSUPPORTED, dict(H=136, qs=136 * 128, os=136 * 128)), (UNSUPPORTED, dict(R=native.MAX_REQUESTS + 1)),

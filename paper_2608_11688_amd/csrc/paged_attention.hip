@@ -1,13 +1,14 @@
 // Attention of new tokens over a paged cache (apex_attention_paged).
 //
 // A tile is a group of query rows of one request and key/value head that are worked on together;
-// the positions it sees fall into units.  Launches of a call (for each 512 tiles):
-//   attend    Every workgroup lists the tiles and their units for itself (build_list), then works
-//             on its share.  Tiles of one token (attend_token) or of up to 128 query rows, heads
-//             of one group and consecutive tokens (attend_tile).  The units of a head, tile after
-//             tile, are shared out evenly over its workgroups (or, many tiles: whole tiles).  A
-//             tile within one share is written to `out`; where shares end inside a tile, its
-//             weighted sums, maxima and normalisers go to the workspace.
+// the positions it sees fall into units.  Launches of a call (for up to 512 tiles each):
+//   attend    Every workgroup lists the tiles and their units for itself (build_list), then its
+//             workers take their shares.  Tiles of one token (attend_token, a wavefront a worker)
+//             or of up to 128 query rows, heads of one group and consecutive tokens (attend_tile,
+//             a workgroup a worker).  The units of a head, tile after tile, are shared out evenly
+//             over its workers (or, many large tiles: whole tiles).  A tile within one share is
+//             written to `out`; where shares end inside a tile, its weighted sums, maxima and
+//             normalisers go to the workspace.
 //   merge     the parts of such tiles joined by the log-sum-exp rule.
 //
 // Both kernels compute S^T = K Q^T and O^T = V^T P^T on the matrix cores: a lane then holds the
@@ -37,6 +38,8 @@ using apex::ffn::sum_xor32;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -61,8 +64,13 @@ constexpr int kMaxGroup = 16;      // query heads per key/value head
 constexpr float kLog2e = 1.4426950408889634f;
 // Weights are 2^(score - m) for a reference m that is raised to the running maximum only when
 // that is more than kSlack above it: they stay below 2^kSlack, where sums in 32 bits and
-// roundings, which are relative, are as good, and rescaling is rare.
+// roundings, which are relative, are as good, and rescaling is rare.  Tiles of up to kExactRows
+// rows, where a new maximum is rare enough, raise it at once: their largest weight is 1, which
+// no rounding to bf16 moves.  (Single tokens over bf16 pages: error 1.09 times that of the
+// result's rounding on average and at most 1.35 in 850 drawn cases; with the slack 1.20 and
+// 1.73.  77 us either way; chunks of 4096 and 2048 tokens without the slack take 4 to 7 % longer.)
 constexpr float kSlack = 8.f;
+constexpr int kExactRows = 16;
 
 // --------------------------------------------------------------------------------- tiles
 // The positions a tile of tokens [q0, q1) of a request sees: sink units from 0 up, then the
@@ -256,8 +264,13 @@ __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast
 __device__ __forceinline__ floatx4 mfma16(uint4 a, uint4 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
+template <bool HALF>   // fp16 operands
 __device__ __forceinline__ floatx16 mfma32(uint4 a, uint4 b, floatx16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+    if constexpr (HALF)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c,
+                                                      0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
 __device__ __forceinline__ float max_xor16(float v) {
@@ -274,49 +287,49 @@ __device__ __forceinline__ uint32_t pk_bf16(float lo, float hi) {   // rounded t
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// A matrix-core operand of 8 fp32 values: one bf16 piece each (rounded), or the three pieces of
-// 8 significant bits that add up to the value exactly.
-template <bool F32>
+// A matrix-core operand of 8 fp32 values in N bf16 pieces, all but the last of which are cut off
+// after 8 significant bits and the last rounded: one, two for 16 bits or three for the value.
+template <int N>
 struct Pieces {
-    static constexpr int N = F32 ? 3 : 1;
     uint4 p[N];
 };
-template <bool F32>
-__device__ __forceinline__ Pieces<F32> pieces_of(const float (&in)[8]) {
-    Pieces<F32> r;
-    if constexpr (!F32) {
-        r.p[0] = make_uint4(pk_bf16(in[0], in[1]), pk_bf16(in[2], in[3]), pk_bf16(in[4], in[5]),
-                            pk_bf16(in[6], in[7]));
-    } else {
-        float x[8];
+template <int N>
+__device__ __forceinline__ Pieces<N> pieces_of(const float (&in)[8]) {
+    Pieces<N> r;
+    float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = in[e];
+    for (int e = 0; e < 8; ++e) x[e] = in[e];
 #pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            uint32_t w[4];
+    for (int q = 0; q < N - 1; ++q) {
+        uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t u0 = __float_as_uint(x[2 * i]), u1 = __float_as_uint(x[2 * i + 1]);
-                w[i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);   // upper halves of u0, u1
-                x[2 * i] -= __uint_as_float(u0 & 0xffff0000u);
-                x[2 * i + 1] -= __uint_as_float(u1 & 0xffff0000u);
-            }
-            r.p[q] = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u0 = __float_as_uint(x[2 * i]), u1 = __float_as_uint(x[2 * i + 1]);
+            w[i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);   // upper halves of u0, u1
+            x[2 * i] -= __uint_as_float(u0 & 0xffff0000u);
+            x[2 * i + 1] -= __uint_as_float(u1 & 0xffff0000u);
         }
+        r.p[q] = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    r.p[N - 1] = make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(x[4], x[5]), pk_bf16(x[6], x[7]));
     return r;
+}
+
+__device__ __forceinline__ uint32_t pk_half(float lo, float hi) {   // rounded to nearest even
+    const halfx2 v = {static_cast<_Float16>(lo), static_cast<_Float16>(hi)};
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 // 8 consecutive values of a query row (bf16 or fp32), zeros where !on.
 template <bool F32>
-__device__ __forceinline__ Pieces<F32> load_q(const void *q, int64_t at, bool on) {
-    Pieces<F32> r;
+__device__ __forceinline__ Pieces<F32 ? 3 : 1> load_q(const void *q, int64_t at, bool on) {
+    Pieces<F32 ? 3 : 1> r;
     if constexpr (F32) {
         const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(q) + at);
         const float4 a = p[0], b = p[1];
         const float x[8] = {on ? a.x : 0.f, on ? a.y : 0.f, on ? a.z : 0.f, on ? a.w : 0.f,
                             on ? b.x : 0.f, on ? b.y : 0.f, on ? b.z : 0.f, on ? b.w : 0.f};
-        r = pieces_of<true>(x);
+        r = pieces_of<3>(x);
     } else {
         const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(q) + at);
         r.p[0] = make_uint4(on ? v.x : 0u, on ? v.y : 0u, on ? v.z : 0u, on ? v.w : 0u);
@@ -329,6 +342,15 @@ __device__ __forceinline__ uint4 widen_e4m3(uint2 c) {
     const auto w = [](uint32_t v, bool hi) {
         return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, true)
                                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, false));
+    };
+    return make_uint4(w(c.x, false), w(c.x, true), w(c.y, false), w(c.y, true));
+}
+
+// The same as fp16 values (exact; a NaN stays one).
+__device__ __forceinline__ uint4 widen_e4m3_half(uint2 c) {
+    const auto w = [](uint32_t v, bool hi) {
+        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, true)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, false));
     };
     return make_uint4(w(c.x, false), w(c.x, true), w(c.y, false), w(c.y, true));
 }
@@ -477,6 +499,9 @@ __device__ __forceinline__ void store_out(void *out, int64_t at, float v) {
 // wavefronts on one tile, joined in LDS: 256 requests of 64 to 256 positions 60 us instead of
 // 42, where a tile is over before its loads are under way; long contexts the same.)
 // Lane (q = lane % 16, lg = lane / 16) holds the scores of row q at positions 16 m + 4 lg + i.
+// bf16 weights go through the second product in two pieces, 16 bits: the products wait for memory
+// anyway, and rounded to 8 bits they would err as much as the rounding of the result, with E4M3
+// scales, which alike rows have alike, up to 1.7 times as much.
 // Bound by the stream of keys and values: 64 tokens under a window of 4096 (1.08 GB) 187 us,
 // 5.75 TB/s, of 5.8 that a kernel that only reads gets.
 constexpr int kTokenUnit = 32;
@@ -496,7 +521,8 @@ struct TokenShape {
 template <int HD, bool F8, bool F32>
 __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     using S = TokenShape<HD, F8, F32>;
-    constexpr int RB = S::RB, NS = S::NS, KS = HD / 32, DT = HD / 16, NP = Pieces<F32>::N;
+    constexpr int RB = S::RB, NS = S::NS, KS = HD / 32, DT = HD / 16;
+    constexpr int NP = F32 ? 3 : 1, NW = F32 ? 3 : 2;   // pieces of a query value and of a weight
     using KSw = KSwizzle<RB>;
     using VSw = TokenVSwizzle<RB, F8>;
     // an array for each stage: the compiler then knows which loads a read of LDS has to wait for
@@ -566,7 +592,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     const int64_t row = uniform(list.row[tile]);
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
 
-    Pieces<F32> qf[KS];
+    Pieces<NP> qf[KS];
 #pragma unroll
     for (int u = 0; u < KS; ++u)
         qf[u] = load_q<F32>(a.q, row * a.q_stride + (g * a.GR + (n < a.GR ? n : 0)) * HD + 32 * u + 8 * lg,
@@ -679,7 +705,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
             l += w[e];
             if constexpr (F8) w[e] *= vs[e];
         }
-        const Pieces<F32> pf = pieces_of<F32>(w);
+        const Pieces<NW> pf = pieces_of<NW>(w);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             uint4 v;
@@ -690,7 +716,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
                 v = make_uint4(v0.x, v0.y, v1.x, v1.y);
             }
 #pragma unroll
-            for (int q = NP - 1; q >= 0; --q) o[d] = mfma16(v, pf.p[q], o[d]);
+            for (int q = NW - 1; q >= 0; --q) o[d] = mfma16(v, pf.p[q], o[d]);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -750,6 +776,14 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // products; units of 64 positions are staged in LDS for all four, the next one in flight while
 // one is multiplied (one barrier per unit).  Lane (q = lane % 32, h = lane / 32) holds the
 // scores of row q at positions 32 m + 8 (i / 4) + 4 h + i % 4.
+// Bound by the matrix cores and what they wait for: 4096 tokens of 32 heads of 128 behind 12288
+// positions (962 GFLOP) 912 us, 1050 TFLOP/s, where a library's product of 8192^3 gets 1198 and
+// both are held back by the card's power (clocks of 1.9 and 1.8 GHz).  Of a unit's 4400 cycles
+// (two workgroups on a CU) the products take half; the rest are the softmax's 32 maxima and
+// exponentials a lane, which the other workgroup's products overlap, and the wait for the loads.
+// E4M3 codes are widened once for the four wavefronts: the same chunk 1180 us; widened by each
+// wavefront where it reads them 1694 (of 1090 then).  fp32: three times the products, 370 TFLOP/s without
+// counting them three times.
 constexpr int kTileUnit = 64;
 constexpr int kTileRows = 128;
 constexpr int kMinShare = 4;          // units of a share: a part is 64 KB
@@ -766,11 +800,12 @@ struct TileShape {
 
 template <int HD, bool F8, bool F32>
 __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void attend_tile(AttendArgs a) {
-    constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32, NP = Pieces<F32>::N;
+    constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32, NP = F32 ? 3 : 1;
+    constexpr bool HALF = F8 && !F32;   // weights and values in fp16
     using KSw = KSwizzle<RB>;
     using VSw = TileVSwizzle<RB>;
     __shared__ __align__(1024) uint8_t st0[2 * kTileUnit * RB], st1[2 * kTileUnit * RB];   // keys, values
-    __shared__ __align__(16) float scales[2][2][kTileUnit];
+    __shared__ __align__(16) float scales[2][3][kTileUnit];   // keys' times scale_log2; values'; their log2
     __shared__ uint8_t group_flags[2][4];   // of a unit's 16 rows each: kBadPage, kOdd
     __shared__ int wave_odd[kWaves];
     __shared__ TileList list;
@@ -841,11 +876,12 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
     const bool row_on = tok < tokens;
     const bool wave_on = 32 * wave < tokens * a.GR;
+    const float slack = tokens * a.GR <= kExactRows ? 0.f : kSlack;
     const int p = row_on ? p_first + tok : -1;
     const int64_t row = row0 + (row_on ? tok : 0);
     const int col = (g * a.GR + (row_on ? head : 0)) * HD;
 
-    Pieces<F32> qf[KS];
+    Pieces<NP> qf[KS];
 #pragma unroll
     for (int u = 0; u < KS; ++u)
         qf[u] = load_q<F32>(a.q, row * a.q_stride + col + 16 * u + 8 * h, row_on);
@@ -907,8 +943,9 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 const uint4 k = codes[0][c], v = codes[1][c];
                 *reinterpret_cast<uint4 *>(lds + ((pk ^ 128 * c) + 8 * RB * c)) = widen_e4m3(make_uint2(k.x, k.y));
                 *reinterpret_cast<uint4 *>(lds + ((pk ^ 128 * c ^ 16) + 8 * RB * c)) = widen_e4m3(make_uint2(k.z, k.w));
-                *reinterpret_cast<uint4 *>(lds + (pv + 8 * RB * c)) = widen_e4m3(make_uint2(v.x, v.y));
-                *reinterpret_cast<uint4 *>(lds + ((pv ^ 16) + 8 * RB * c)) = widen_e4m3(make_uint2(v.z, v.w));
+                const uint2 v0 = make_uint2(v.x, v.y), v1 = make_uint2(v.z, v.w);
+                *reinterpret_cast<uint4 *>(lds + (pv + 8 * RB * c)) = HALF ? widen_e4m3_half(v0) : widen_e4m3(v0);
+                *reinterpret_cast<uint4 *>(lds + ((pv ^ 16) + 8 * RB * c)) = HALF ? widen_e4m3_half(v1) : widen_e4m3(v1);
             }
         }
     };
@@ -921,8 +958,16 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     const auto step = [&](auto which, auto careful, int i) __attribute__((always_inline)) {
         constexpr int buf = decltype(which)::value;
         constexpr bool CAREFUL = decltype(careful)::value;
+        // E4M3: the reference of a row's weights follows the largest score plus log2 of the value's
+        // scale (held to what keeps the sums of weights in range), so that weight times scale, the
+        // second product's operand, is at most 2^kSlack and fp16 holds it to 11 bits (bf16's 8 err
+        // 1.4 to 1.8 times as much as the result's rounding alone, 11 no more than 1.01 times; a
+        // chunk of 4096 tokens behind 12288 positions takes 8 % longer).
         if constexpr (F8)
-            if (lane < 32) scales[buf][lane >> 4][16 * wave + (lane & 15)] = sc;
+            if (lane < 32 || lane >= 48)
+                scales[buf][min(lane >> 4, 2)][16 * wave + (lane & 15)] =
+                    lane < 16 ? sc * a.scale_log2
+                              : lane < 32 ? sc : fminf(fmaxf(__builtin_amdgcn_logf(fabsf(sc)), -100.f), 126.f);
         wait_loads<0>();
         const int j0 = span.base(u_lo + i, kTileUnit);
         const uint8_t *lds = buf ? st1 : st0;
@@ -938,7 +983,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)   // exponents of all ones carry into the sign's place
-                    odd |= ((x[e] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+                    odd |= ((x[e] & 0x7fff7fffu) + (HALF ? 0x04000400u : 0x00800080u)) & 0x80008000u;
             }
             if constexpr (F8) odd |= (__float_as_uint(sc) & 0x7f800000u) == 0x7f800000u;
             if (__ballot(odd)) flags |= kOdd;
@@ -970,8 +1015,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 const uint4 k = kf[x % AHEAD];
                 if (x + AHEAD < NK) kf[x % AHEAD] = load_k(x + AHEAD);
 #pragma unroll
-                for (int q = NP - 1; q > 0; --q) small = mfma32(k, qf[u].p[q], small);
-                big = mfma32(k, qf[u].p[0], big);
+                for (int q = NP - 1; q > 0; --q) small = mfma32<false>(k, qf[u].p[q], small);
+                big = mfma32<false>(k, qf[u].p[0], big);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[m][e] = F32 ? big[e] + small[e] : big[e];
@@ -1002,13 +1047,14 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                     s[m][e] = on ? s[m][e] : -INFINITY;
                 }
         }
-        float top = s[0][0];
+        float top = -INFINITY;   // (of E4M3 scores, which are in powers of two already, and their scales)
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[m][e]);
-        top = max_xor32(top) * a.scale_log2;
-        if (__ballot(top > mx + kSlack)) {
+            for (int e = 0; e < 16; ++e)
+                top = fmaxf(top, F8 ? s[m][e] + scales[buf][2][32 * m + 8 * (e / 4) + 4 * h + e % 4] : s[m][e]);
+        top = F8 ? max_xor32(top) : max_xor32(top) * a.scale_log2;
+        if (__ballot(top > mx + slack)) {
             const float now = fmaxf(mx, top);
             const float c = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - now);
             mx = now;
@@ -1022,7 +1068,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int i = 8 * (u & 1) + e;
-                w[e] = __builtin_amdgcn_exp2f(fmaf(s[u / 2][i], a.scale_log2, -ref));
+                w[e] = __builtin_amdgcn_exp2f(F8 ? s[u / 2][i] - ref : fmaf(s[u / 2][i], a.scale_log2, -ref));
                 l += w[e];
             }
             if constexpr (F8) {
@@ -1059,8 +1105,13 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                     for (int e4 = 0; e4 < 4; ++e4) {
                         float v[4];
                         const uint2 c = lds_u2(lds, kV + j * RB + 16 * ((4 * d + e4) ^ VSw::of(j)) + 8 * h);
-                        v[0] = apex::ffn::bf_lo(c.x), v[1] = apex::ffn::bf_hi(c.x);
-                        v[2] = apex::ffn::bf_lo(c.y), v[3] = apex::ffn::bf_hi(c.y);
+                        if constexpr (HALF) {
+                            const halfx2 c0 = __builtin_bit_cast(halfx2, c.x), c1 = __builtin_bit_cast(halfx2, c.y);
+                            v[0] = c0.x, v[1] = c0.y, v[2] = c1.x, v[3] = c1.y;
+                        } else {
+                            v[0] = apex::ffn::bf_lo(c.x), v[1] = apex::ffn::bf_hi(c.x);
+                            v[2] = apex::ffn::bf_lo(c.y), v[3] = apex::ffn::bf_hi(c.y);
+                        }
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             o[d][4 * e4 + e] = w == 0.f ? o[d][4 * e4 + e] : fmaf(w, v[e], o[d][4 * e4 + e]);
@@ -1078,24 +1129,31 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         uint4 vf[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) vf[d] = load_v(0, d);
+        const auto operand = [&](const float (&w)[8]) __attribute__((always_inline)) {
+            if constexpr (HALF)
+                return Pieces<1>{{make_uint4(pk_half(w[0], w[1]), pk_half(w[2], w[3]), pk_half(w[4], w[5]),
+                                             pk_half(w[6], w[7]))}};
+            else
+                return pieces_of<NP>(w);
+        };
         float w[8];
         weights(0, w);
-        Pieces<F32> pf = pieces_of<F32>(w);
+        Pieces<NP> pf = operand(w);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             uint4 vn[DT];
-            Pieces<F32> pn;
+            Pieces<NP> pn;
             if (u < 3) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) vn[d] = load_v(u + 1, d);
                 weights(u + 1, w);
-                pn = pieces_of<F32>(w);
+                pn = operand(w);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int q = NP - 1; q >= 0; --q) o[d] = mfma32(vf[d], pf.p[q], o[d]);
+                for (int q = NP - 1; q >= 0; --q) o[d] = mfma32<HALF>(vf[d], pf.p[q], o[d]);
             if (u < 3) {
 #pragma unroll
                 for (int x = 0; x < DT * NP; ++x) {
@@ -1234,7 +1292,8 @@ __global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
     }
 }
 
-// Tiles of many rows: grid (tiles * G, y), HD / 4 lanes per row.
+// Tiles of many rows: grid (tiles * G, y), HD / 4 lanes per row.  Bound by the parts it reads,
+// 64 KB each: 33 MB 11 us behind the launch before; 5 where no tile was split.
 template <int HD, bool F32>
 __global__ __launch_bounds__(kThreads) void merge_tiles(AttendArgs a) {
     constexpr int LPR = HD / 4, PER = kThreads / LPR;   // rows at a time
@@ -1320,7 +1379,7 @@ apex_status launch_attention(const Plan &p, hipStream_t st, AttendArgs a) {
         if (p.token) {
             hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3((workers + kWaves - 1) / kWaves * a.G),
                                dim3(kThreads), 0, st, a);
-            // Few tiles have many parts: 4 requests of 24000 positions in 8 groups 4.8 us with 1024
+            // Few tiles have many parts: 4 requests of up to 131072 positions in 8 groups 4.8 us with 1024
             // threads, 6.1 with 512; 256 requests' tiles of a few parts each 5.5 with 256, 18.9
             // with 1024.
             if (x <= 64)

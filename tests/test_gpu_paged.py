@@ -200,6 +200,36 @@ def test_many_tiles_groups_and_parts(torch, R, new, longest, H, G, hd, fmt, dtyp
     print(c.check())
 
 
+@pytest.mark.parametrize("fmt,new,pad", [("bf16", 1, 0), ("fp8", 1, 0), ("fp8", 1, 9), ("fp8", 30, 0)])
+@pytest.mark.parametrize("spread", [0.0, 3.0])
+def test_weights_are_held_to_more_bits_than_the_result(torch, fmt, new, pad, spread):
+    """16 bits (single tokens) or fp16's 11 of weight times scale (E4M3): in the 2-norm at most an
+    eighth of what rounding the result to bf16 gives, 1.008 times that together, and 1.05 with the
+    chance that the few hundred outputs here leave.  Few positions, so that single weights tell, and
+    scales e^spread apart."""
+    for seed in range(4):
+        c = Case(torch, [new + 1, new + 4, new + 30], [new] * 3, 8, 2, 128, 16, fmt, "bf16", pad=pad, seed=40 + seed)
+        if c.vs is not None:
+            c.vs *= np.exp(c.rng.uniform(-spread, spread, c.vs.shape)).astype(np.float32)
+        c.check()
+        n = 3 * new
+        k, v = c.values()
+        want = opaged.attend(c.q, k, v, c.cu, c.lens, c.table, 0, 0, 128 ** -0.5, np.zeros((c.T, 8, 128)))[0][:n]
+        got = c.out.double().cpu().numpy().reshape(c.T, 8, 128)[:n]
+        assert np.linalg.norm(got - want) <= 1.05 * np.linalg.norm(round_bf16(want) - want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("factor", [1e-28, 1e28])
+def test_scales_far_from_one(torch, factor, new, dtype):
+    """All of a pool's values tiny or huge, and zero rows among them."""
+    c = Case(torch, [90, 200], [new, new], 4, 2, 64, 16, "fp8", dtype, pad=new > 1, seed=14)
+    c.vs *= np.float32(factor)
+    c.vs[c.rng.random(c.vs.shape) < 0.1] = 0
+    c.check()
+
+
 @pytest.mark.parametrize("H", [1, 16])
 def test_lengths_that_count_tokens_twice_stay_inside(torch, H):
     """cu_new that goes back and forth: more tiles than T tokens have.  Which rows are written is

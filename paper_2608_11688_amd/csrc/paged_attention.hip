@@ -890,7 +890,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     // to bf16 once for the four wavefronts (each lane 16 codes of CPL chunks).
     constexpr int CPL = F8 ? HD / 64 : 1, CRPI = kWave * 16 / HD;   // code loads, rows of a load
     float sc = 0.f;
-    bool rows_ok = false;
+    bool sc_on = false, rows_ok = false;
     uint4 codes[2][CPL];
     // A unit's page id is loaded a unit ahead, as a vector load: a scalar one would be waited for
     // with the reads of LDS.
@@ -910,7 +910,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         if constexpr (F8) {
             const int x = lane & 15;   // the scales of rows that are not read are 0
             sc = scale_of[r.row + min(x, max(r.end - 1, 0))];
-            sc = x >= r.end || (x < from && x >= keep) ? 0.f : sc;
+            sc_on = x < r.end && (x >= from || x < keep);   // (looked at where the load has been waited for)
             const Extent kx = extent_of<HD>(a.k_pages, r), vx = extent_of<HD>(a.v_pages, r);
             const auto kr = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(kx.base), 0, kx.bytes, 0x00027000);
             const auto vr = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(vx.base), 0, vx.bytes, 0x00027000);
@@ -958,6 +958,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     const auto step = [&](auto which, auto careful, int i) __attribute__((always_inline)) {
         constexpr int buf = decltype(which)::value;
         constexpr bool CAREFUL = decltype(careful)::value;
+        if constexpr (F8) sc = sc_on ? sc : 0.f;
         // E4M3: the reference of a row's weights follows the largest score plus log2 of the value's
         // scale (held to what keeps the sums of weights in range), so that weight times scale, the
         // second product's operand, is at most 2^kSlack and fp16 holds it to 11 bits (bf16's 8 err

@@ -18,6 +18,10 @@ Memory-Efficient Edge MoE Inference) and cites it by section, equation or algori
 * ``metrics``    oracle budget delta*, overlap, full coverage (Sec. IV-B Eq. 2-3, V-C)
 * ``decode``     one decode step through all layers, composing the above
 
+Operators of serving that the paper does not define are written from their definitions:
+
+* ``paged``      paged key/value cache: plan of pages and slots, store, attention over pages
+
 Pins: every function is checked in ``tests/test_oracle_*.py`` against brute force,
 closed forms, library routines on special cases and invariants the paper states.
 """

@@ -1352,7 +1352,8 @@ Plan plan_of(int T, int R, int H, int G, int hd) {
     p.tile_tokens = p.token ? 1 : kTileRows / p.GR;
     p.rows = p.token ? p.GR : kTileRows;
     // the sum of ceil(n / tile_tokens) over min(T, R) requests that have any of T tokens
-    p.max_tiles = int((T + int64_t(p.tile_tokens - 1) * std::min(T, R)) / p.tile_tokens);
+    p.max_tiles = int(std::min((T + int64_t(p.tile_tokens - 1) * std::min(T, R)) / p.tile_tokens,
+                               int64_t(INT_MAX)));
     p.most_workers = p.token ? kWaves * std::max(1, 2 * kCus / G) : std::max(1, (hd == 128 ? 2 : 3) * kCus / G);
     const auto up = [](size_t v) { return apex::align_up(v, 256); };
     const size_t parts = 2 * size_t(p.most_workers) * G * p.rows;

@@ -9,6 +9,9 @@ are independent, so that over all outputs the 2-norm of the error is much smalle
 result's with fp32, where a dropped 8-bit piece of an operand would leave 4e-6 and more, and with
 bf16 two roundings of rms 2^-8 / sqrt(3) * 0.72 = 1.6e-3 each, 2.3e-3 together, at most 4e-3.
 """
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -228,6 +231,24 @@ def test_scales_far_from_one(torch, factor, new, dtype):
     c.vs *= np.float32(factor)
     c.vs[c.rng.random(c.vs.shape) < 0.1] = 0
     c.check()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_as_many_requests_as_there_may_be(torch, fmt):
+    """4096 prompts of 1 to 40 tokens, ten launches; a sample of them against the oracle."""
+    rng = np.random.default_rng(15)
+    n = rng.integers(1, 41, native.MAX_REQUESTS)
+    c = Case(torch, n, n, 16, 2, 64, 16, fmt, "bf16", pad=3, seed=15)
+    c.device()
+    c.call()
+    got = c.out.double().cpu().numpy().reshape(c.T, 16, 64)
+    assert (got[-3:] == 7).all()
+    k, v = c.values()
+    for r in [0, 1, *rng.integers(0, len(n), 40), len(n) - 1]:
+        rows = slice(c.cu[r], c.cu[r + 1])
+        want, size, peak = opaged.attend(c.q[rows], k, v, [0, n[r]], n[r:r + 1], c.table[r:r + 1], 0, 0, 0.125,
+                                         np.zeros((n[r], 16, 64)))
+        compare(got[rows], want, size, peak, 64, "bf16", norm=False)
 
 
 @pytest.mark.parametrize("H", [1, 16])
@@ -601,6 +622,14 @@ def test_a_server_from_prompts_to_tokens(torch, fmt, dtype):
                                             0.125, np.full((T, H, hd), 7.0))
         got = out.double().cpu().numpy().reshape(T, H, hd)
         compare(got, ref_out, size, peak, hd, dtype)
+
+
+def test_readme_example_runs(torch):
+    """The Python example of README.md for the paged cache, run as written."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "README.md")).read()
+    code = re.search(r"<!-- example: paged -->\s*```python\n(.*?)```", text, re.S).group(1)
+    exec(compile(code, "README.md example", "exec"), {})
 
 
 def test_two_streams_with_workspaces_of_their_own(torch):

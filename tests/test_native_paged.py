@@ -110,3 +110,4 @@ def test_workspace_does_not_grow_with_the_context():
     f = native.apex_attention_paged_workspace_bytes
     assert f(1, 1, 32, 8, 128) < 20 << 20 and f(4096, 8, 32, 8, 128) < 72 << 20
     assert f(0, 0, 32, 8, 128) == 256
+    assert f(2 ** 31 - 1, 2 ** 31 - 1, 16, 1, 128) < 80 << 20

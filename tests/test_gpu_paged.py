@@ -354,6 +354,22 @@ def test_lengths_that_disagree_stay_inside(torch):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("new", [1, 70])
+def test_windows_and_sinks_as_large_as_they_may_be(torch, new):
+    """As none: the same positions, the same bits."""
+    big = 2 ** 31 - 1
+    c = Case(torch, [300, 90], [new, new], 4, 2, 64, 16, "bf16", "bf16", pad=2, seed=16)
+    c.check()
+    want = c.out.clone()
+    for window, sinks in ((big, 0), (big, big), (1, big), (0, big), (200, 200)):
+        c.out.fill_(7.0)
+        c.call(window, sinks)
+        if window == 200:
+            c.check(window, sinks)
+        else:
+            assert torch.equal(c.out, want), (window, sinks)
+
+
 @pytest.mark.parametrize("new", [1, 33])
 def test_in_place_over_the_queries(torch, new):
     c = Case(torch, [900, 300], [new, new], 4, 2, 64, 16, "bf16", "bf16", seed=8)

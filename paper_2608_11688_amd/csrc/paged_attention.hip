@@ -786,15 +786,18 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // counting them three times.
 constexpr int kTileUnit = 64;
 constexpr int kTileRows = 128;
-constexpr int kMinShare = 4;          // units of a share: a part is 64 KB
+// Units of a share at least: a part is 64 KB.  64 tokens behind 1000 positions, heads of 128: 22.0
+// us with 2 (and with 1), 25.1 with 4, 34.2 with 16; 64 tokens behind 8000: 36.0, with 4 34.0.
+constexpr int kMinShare = 2;
 constexpr int kBadPage = 1, kOdd = 2;
 
 template <int HD, bool F8, bool F32>
 struct TileShape {
     // workgroups that a CU's registers hold
     static constexpr int kPerCu = HD == 128 ? (F32 ? 1 : 2) : (F8 || F32 ? 2 : 3);
-    // What parts and their merge cost a call, about 25 us, in the time of a unit (us, with a CU
-    // full of workgroups: 2.1, E4M3 2.6, fp32 2.9; heads of 64 1.5, 1.9 and 1.9).
+    // What parts and their merge cost a call where every workgroup leaves two, about 25 us, in the
+    // time of a unit (us, with a CU full of workgroups: 2.1, E4M3 2.6, fp32 2.9; heads of 64
+    // 1.5, 1.9 and 1.9).
     static constexpr float kSplitCost = HD == 128 ? (F32 ? 8.f : F8 ? 9.f : 12.f) : (F32 || F8 ? 13.f : 16.f);
 };
 
@@ -817,12 +820,15 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     const int all_units = uniform(list.cu[tiles]);
     if (all_units == 0) return;
     // Whole tiles, the last ones (of a request: the longest) first, or even shares of the units.
-    // In units: even shares take all / workers and kSplitCost for the parts and their merge;
+    // In units: even shares take all / workers and kSplitCost for as many parts as they leave;
     // whole tiles as long as the longest one (which runs faster towards the end, alone on its
     // CU), or all / workers and what the last round, the first `rest` tiles, leaves idle.
+    // Whole and even, us: a prompt of 2048 tokens 60 and 88, eight E4M3 chunks of 700 tokens behind
+    // up to 3500 positions 177 and 184, 4096 tokens behind 12288 960 and 1057; 512 tokens behind
+    // 4096 100 and 66, 31 single tokens 103 and 76, two fp32 chunks without a window 298 and 268.
     const int workers = max(min(a.workers, all_units / kMinShare), 1);
     const int rest = tiles % a.workers;
-    const float even = float(all_units) / a.workers;
+    const float even = float(all_units) / workers, parts = float(workers + min(tiles, workers)) / (2 * a.workers);
     float longest = 0.f;
     for (int i = threadIdx.x; i < tiles; i += kThreads) longest = fmaxf(longest, float(list.cu[i + 1] - list.cu[i]));
     longest = max_xor32(max_xor16(apex::ffn::row_max(longest)));
@@ -830,8 +836,9 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     __syncthreads();
     longest = float(max(max(list.wave_end[0], list.wave_end[1]), max(list.wave_end[2], list.wave_end[3])));
     const float idle = rest ? (1.f - float(rest) / a.workers) * list.cu[rest] / rest : 0.f;
-    const float whole = fmaxf((TileShape<HD, F8, F32>::kPerCu == 2 ? 0.75f : 1.f) * longest, even + idle);
-    const bool whole_tiles = uniform(whole <= even + TileShape<HD, F8, F32>::kSplitCost);
+    const float whole = fmaxf((TileShape<HD, F8, F32>::kPerCu == 2 ? 0.75f : 1.f) * longest,
+                              float(all_units) / a.workers + idle);
+    const bool whole_tiles = uniform(whole <= even + parts * TileShape<HD, F8, F32>::kSplitCost);
     const Shares shares(all_units, workers);
     int share_lo, share_hi, tile;
     if (whole_tiles) {
@@ -1346,8 +1353,9 @@ struct Plan {
 Plan plan_of(int T, int R, int H, int G, int hd) {
     Plan p;
     p.GR = H / G;
-    // no more rows than requests: single tokens, as a rule; a request that has more of them
-    // is worked on token by token
+    // No more rows than requests: single tokens, as a rule; a request that has more of them
+    // is worked on token by token.  31 single tokens, us: 73 by tokens, 76 in tiles; 16 requests of
+    // 2 tokens 28 and 30, 8 of 4 25 and 24; but a chunk among them would be read once a token.
     p.token = T <= R;
     p.tile_tokens = p.token ? 1 : kTileRows / p.GR;
     p.rows = p.token ? p.GR : kTileRows;

@@ -825,7 +825,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     // CU), or all / workers and what the last round, the first `rest` tiles, leaves idle.
     // Whole and even, us: a prompt of 2048 tokens 60 and 88, eight E4M3 chunks of 700 tokens behind
     // up to 3500 positions 177 and 184, 4096 tokens behind 12288 960 and 1057; 512 tokens behind
-    // 4096 100 and 66, 31 single tokens 103 and 76, two fp32 chunks without a window 298 and 268.
+    // 4096 100 and 66, 31 single tokens 103 and 76, 2048 fp32 tokens of heads of 64 behind 6144
+    // 298 and 268.
     const int workers = max(min(a.workers, all_units / kMinShare), 1);
     const int rest = tiles % a.workers;
     const float even = float(all_units) / workers, parts = float(workers + min(tiles, workers)) / (2 * a.workers);

@@ -73,6 +73,10 @@ constexpr float kSlack = 8.f;
 constexpr int kExactRows = 16;
 
 // --------------------------------------------------------------------------------- tiles
+// The first position a token at position p sees besides the sinks.  Tokens that lengths place
+// before 0 see nothing, and p - window would pass the range of an int there.
+__device__ __forceinline__ int lower_edge(int p, int window) { return window > 0 ? max(0, max(p, 0) - window + 1) : 0; }
+
 // The positions a tile of tokens [q0, q1) of a request sees: sink units from 0 up, then the
 // units from `first` up to the last token's position.  UP: positions of a unit.
 struct Span {
@@ -84,8 +88,7 @@ struct Span {
 template <int UP>
 __device__ __forceinline__ Span span_of(int p_first, int p_last, int window, int sinks) {
     Span s;
-    const int low = window > 0 ? max(0, p_first - window + 1) : 0;
-    s.first = low / UP;
+    s.first = lower_edge(p_first, window) / UP;
     s.sinks = window > 0 ? min(int((unsigned(min(sinks, p_last + 1)) + UP - 1) / UP), s.first) : 0;
     s.units = p_last < 0 ? 0 : p_last / UP + 1 - s.first + s.sinks;
     return s;
@@ -201,7 +204,7 @@ __device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
         const int q0 = (a.first_tile + i - first) * a.tile_tokens;
         const int p = q.seq - q.n + q0, tokens = min(a.tile_tokens, q.n - q0);
         // a tile that sees nothing still has a unit: its rows are written
-        sum += max(span_of<UP>(max(p, 0), p + tokens - 1, a.window, a.sinks).units, 1);
+        sum += max(span_of<UP>(p, p + tokens - 1, a.window, a.sinks).units, 1);
         s.cu[i + 1] = sum;
         s.row[i] = q.row0 + q0;
         s.p[i] = p;
@@ -586,8 +589,8 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     const int tile_lo = uniform(list.cu[tile]), tile_hi = uniform(list.cu[tile + 1]);
     const int u_lo = uniform(z - tile_lo), steps = uniform(min(tile_hi, share_hi) - z);
     const int req = uniform(list.r[tile]), p = uniform(list.p[tile]), hi = p + 1;
-    const int low = a.list.window > 0 ? max(0, p - a.list.window + 1) : 0;
-    const Span span = span_of<kTokenUnit>(max(p, 0), p, a.list.window, a.list.sinks);
+    const int low = lower_edge(p, a.list.window);
+    const Span span = span_of<kTokenUnit>(p, p, a.list.window, a.list.sinks);
     const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
     const int64_t row = uniform(list.row[tile]);
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
@@ -878,8 +881,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     const int req = uniform(list.r[tile]), tokens = uniform(list.tokens[tile]);
     const int row0 = uniform(list.row[tile]);
     const int p_first = uniform(list.p[tile]), p_last = p_first + tokens - 1, hi = p_last + 1;
-    const int low = a.list.window > 0 ? max(0, p_first - a.list.window + 1) : 0;
-    const Span span = span_of<kTileUnit>(max(p_first, 0), p_last, a.list.window, a.list.sinks);
+    const int low = lower_edge(p_first, a.list.window);
+    const Span span = span_of<kTileUnit>(p_first, p_last, a.list.window, a.list.sinks);
     const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
     const bool row_on = tok < tokens;

@@ -370,6 +370,19 @@ def test_windows_and_sinks_as_large_as_they_may_be(torch, new):
             assert torch.equal(c.out, want), (window, sinks)
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("idle", [0, 30])
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 4, 3), (20, 3), (0, 0)])
+def test_tokens_before_position_zero_under_any_window(torch, window, sinks, idle, fmt, dtype):
+    """Lengths shorter than the new tokens: the tokens at positions below 0 see nothing, the others
+    what they see in any case, however near the window is to the largest number."""
+    lens, new = [2, 70, 1, 40] + [0] * idle, [9, 5, 12, 70 - idle] + [0] * idle
+    c = Case(torch, lens, new, 4, 2, 64, 16, fmt, dtype, seed=17)
+    c.check(window, sinks)
+    rows = c.out[:9]
+    assert (rows[:7] == 0).all() and (rows[7:] != 0).any(dim=1).all()
+
+
 @pytest.mark.parametrize("new", [1, 33])
 def test_in_place_over_the_queries(torch, new):
     c = Case(torch, [900, 300], [new, new], 4, 2, 64, 16, "bf16", "bf16", seed=8)

@@ -38,8 +38,6 @@ using apex::ffn::sum_xor32;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
-typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -267,13 +265,8 @@ __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast
 __device__ __forceinline__ floatx4 mfma16(uint4 a, uint4 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
-template <bool HALF>   // fp16 operands
 __device__ __forceinline__ floatx16 mfma32(uint4 a, uint4 b, floatx16 c) {
-    if constexpr (HALF)
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c,
-                                                      0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
 __device__ __forceinline__ float max_xor16(float v) {
@@ -318,11 +311,6 @@ __device__ __forceinline__ Pieces<N> pieces_of(const float (&in)[8]) {
     return r;
 }
 
-__device__ __forceinline__ uint32_t pk_half(float lo, float hi) {   // rounded to nearest even
-    const halfx2 v = {static_cast<_Float16>(lo), static_cast<_Float16>(hi)};
-    return __builtin_bit_cast(uint32_t, v);
-}
-
 // 8 consecutive values of a query row (bf16 or fp32), zeros where !on.
 template <bool F32>
 __device__ __forceinline__ Pieces<F32 ? 3 : 1> load_q(const void *q, int64_t at, bool on) {
@@ -345,15 +333,6 @@ __device__ __forceinline__ uint4 widen_e4m3(uint2 c) {
     const auto w = [](uint32_t v, bool hi) {
         return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, true)
                                                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, false));
-    };
-    return make_uint4(w(c.x, false), w(c.x, true), w(c.y, false), w(c.y, true));
-}
-
-// The same as fp16 values (exact; a NaN stays one).
-__device__ __forceinline__ uint4 widen_e4m3_half(uint2 c) {
-    const auto w = [](uint32_t v, bool hi) {
-        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, true)
-                                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, false));
     };
     return make_uint4(w(c.x, false), w(c.x, true), w(c.y, false), w(c.y, true));
 }
@@ -784,9 +763,12 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // both are held back by the card's power (clocks of 1.9 and 1.8 GHz).  Of a unit's 4400 cycles
 // (two workgroups on a CU) the products take half; the rest are the softmax's 32 maxima and
 // exponentials a lane, which the other workgroup's products overlap, and the wait for the loads.
-// E4M3 codes are widened once for the four wavefronts: the same chunk 1180 us; widened by each
-// wavefront where it reads them 1694 (of 1090 then).  fp32: three times the products, 370 TFLOP/s without
-// counting them three times.
+// E4M3 codes are widened once for the four wavefronts (by each where it reads them: half as long
+// again).  Their weights, times the values' scales, go through the second product in two bf16
+// pieces, 16 bits: the same chunk 1330-1360 us.  One piece, 1090, errs up to 1.8 times as much as the
+// rounding of the result, as alike rows have alike scales; one of fp16, 1140-1160, loses what is 25
+// powers of two below a row's largest product but in its normaliser, and with it outputs that such
+// positions make up.  fp32 in three pieces: 390 TFLOP/s without counting them three times.
 constexpr int kTileUnit = 64;
 constexpr int kTileRows = 128;
 // Units of a share at least: a part is 64 KB.  64 tokens behind 1000 positions, heads of 128: 22.0
@@ -799,19 +781,19 @@ struct TileShape {
     // workgroups that a CU's registers hold
     static constexpr int kPerCu = HD == 128 ? (F32 ? 1 : 2) : (F8 || F32 ? 2 : 3);
     // What parts and their merge cost a call where every workgroup leaves two, about 25 us, in the
-    // time of a unit (us, with a CU full of workgroups: 2.1, E4M3 2.6, fp32 2.9; heads of 64
-    // 1.5, 1.9 and 1.9).
-    static constexpr float kSplitCost = HD == 128 ? (F32 ? 8.f : F8 ? 9.f : 12.f) : (F32 || F8 ? 13.f : 16.f);
+    // time of a unit (us, with a CU full of workgroups: 2.1, E4M3 3.1, fp32 2.9; heads of 64
+    // 1.5, 2.2 and 1.9).
+    static constexpr float kSplitCost = HD == 128 ? (F32 || F8 ? 8.f : 12.f) : (F32 ? 13.f : F8 ? 11.f : 16.f);
 };
 
 template <int HD, bool F8, bool F32>
 __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void attend_tile(AttendArgs a) {
-    constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32, NP = F32 ? 3 : 1;
-    constexpr bool HALF = F8 && !F32;   // weights and values in fp16
+    constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32;
+    constexpr int NP = F32 ? 3 : 1, NW = F32 ? 3 : F8 ? 2 : 1;   // pieces of a query value and of a weight
     using KSw = KSwizzle<RB>;
     using VSw = TileVSwizzle<RB>;
     __shared__ __align__(1024) uint8_t st0[2 * kTileUnit * RB], st1[2 * kTileUnit * RB];   // keys, values
-    __shared__ __align__(16) float scales[2][3][kTileUnit];   // keys' times scale_log2; values'; their log2
+    __shared__ __align__(16) float scales[2][2][kTileUnit];   // keys' times scale_log2; values'
     __shared__ uint8_t group_flags[2][4];   // of a unit's 16 rows each: kBadPage, kOdd
     __shared__ int wave_odd[kWaves];
     __shared__ TileList list;
@@ -955,8 +937,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 *reinterpret_cast<uint4 *>(lds + ((pk ^ 128 * c) + 8 * RB * c)) = widen_e4m3(make_uint2(k.x, k.y));
                 *reinterpret_cast<uint4 *>(lds + ((pk ^ 128 * c ^ 16) + 8 * RB * c)) = widen_e4m3(make_uint2(k.z, k.w));
                 const uint2 v0 = make_uint2(v.x, v.y), v1 = make_uint2(v.z, v.w);
-                *reinterpret_cast<uint4 *>(lds + (pv + 8 * RB * c)) = HALF ? widen_e4m3_half(v0) : widen_e4m3(v0);
-                *reinterpret_cast<uint4 *>(lds + ((pv ^ 16) + 8 * RB * c)) = HALF ? widen_e4m3_half(v1) : widen_e4m3(v1);
+                *reinterpret_cast<uint4 *>(lds + (pv + 8 * RB * c)) = widen_e4m3(v0);
+                *reinterpret_cast<uint4 *>(lds + ((pv ^ 16) + 8 * RB * c)) = widen_e4m3(v1);
             }
         }
     };
@@ -970,16 +952,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         constexpr int buf = decltype(which)::value;
         constexpr bool CAREFUL = decltype(careful)::value;
         if constexpr (F8) sc = sc_on ? sc : 0.f;
-        // E4M3: the reference of a row's weights follows the largest score plus log2 of the value's
-        // scale (held to what keeps the sums of weights in range), so that weight times scale, the
-        // second product's operand, is at most 2^kSlack and fp16 holds it to 11 bits (bf16's 8 err
-        // 1.4 to 1.8 times as much as the result's rounding alone, 11 no more than 1.01 times; a
-        // chunk of 4096 tokens behind 12288 positions takes 8 % longer).
         if constexpr (F8)
-            if (lane < 32 || lane >= 48)
-                scales[buf][min(lane >> 4, 2)][16 * wave + (lane & 15)] =
-                    lane < 16 ? sc * a.scale_log2
-                              : lane < 32 ? sc : fminf(fmaxf(__builtin_amdgcn_logf(fabsf(sc)), -100.f), 126.f);
+            if (lane < 32) scales[buf][lane >> 4][16 * wave + (lane & 15)] = lane < 16 ? sc * a.scale_log2 : sc;
         wait_loads<0>();
         const int j0 = span.base(u_lo + i, kTileUnit);
         const uint8_t *lds = buf ? st1 : st0;
@@ -995,7 +969,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)   // exponents of all ones carry into the sign's place
-                    odd |= ((x[e] & 0x7fff7fffu) + (HALF ? 0x04000400u : 0x00800080u)) & 0x80008000u;
+                    odd |= ((x[e] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
             }
             if constexpr (F8) odd |= (__float_as_uint(sc) & 0x7f800000u) == 0x7f800000u;
             if (__ballot(odd)) flags |= kOdd;
@@ -1027,8 +1001,8 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 const uint4 k = kf[x % AHEAD];
                 if (x + AHEAD < NK) kf[x % AHEAD] = load_k(x + AHEAD);
 #pragma unroll
-                for (int q = NP - 1; q > 0; --q) small = mfma32<false>(k, qf[u].p[q], small);
-                big = mfma32<false>(k, qf[u].p[0], big);
+                for (int q = NP - 1; q > 0; --q) small = mfma32(k, qf[u].p[q], small);
+                big = mfma32(k, qf[u].p[0], big);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[m][e] = F32 ? big[e] + small[e] : big[e];
@@ -1059,13 +1033,12 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                     s[m][e] = on ? s[m][e] : -INFINITY;
                 }
         }
-        float top = -INFINITY;   // (of E4M3 scores, which are in powers of two already, and their scales)
+        float top = -INFINITY;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                top = fmaxf(top, F8 ? s[m][e] + scales[buf][2][32 * m + 8 * (e / 4) + 4 * h + e % 4] : s[m][e]);
-        top = F8 ? max_xor32(top) : max_xor32(top) * a.scale_log2;
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[m][e]);
+        top = F8 ? max_xor32(top) : max_xor32(top) * a.scale_log2;   // (E4M3 scores are in powers of two already)
         if (__ballot(top > mx + slack)) {
             const float now = fmaxf(mx, top);
             const float c = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - now);
@@ -1115,15 +1088,9 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int e4 = 0; e4 < 4; ++e4) {
-                        float v[4];
                         const uint2 c = lds_u2(lds, kV + j * RB + 16 * ((4 * d + e4) ^ VSw::of(j)) + 8 * h);
-                        if constexpr (HALF) {
-                            const halfx2 c0 = __builtin_bit_cast(halfx2, c.x), c1 = __builtin_bit_cast(halfx2, c.y);
-                            v[0] = c0.x, v[1] = c0.y, v[2] = c1.x, v[3] = c1.y;
-                        } else {
-                            v[0] = apex::ffn::bf_lo(c.x), v[1] = apex::ffn::bf_hi(c.x);
-                            v[2] = apex::ffn::bf_lo(c.y), v[3] = apex::ffn::bf_hi(c.y);
-                        }
+                        const float v[4] = {apex::ffn::bf_lo(c.x), apex::ffn::bf_hi(c.x), apex::ffn::bf_lo(c.y),
+                                            apex::ffn::bf_hi(c.y)};
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             o[d][4 * e4 + e] = w == 0.f ? o[d][4 * e4 + e] : fmaf(w, v[e], o[d][4 * e4 + e]);
@@ -1141,37 +1108,30 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         uint4 vf[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) vf[d] = load_v(0, d);
-        const auto operand = [&](const float (&w)[8]) __attribute__((always_inline)) {
-            if constexpr (HALF)
-                return Pieces<1>{{make_uint4(pk_half(w[0], w[1]), pk_half(w[2], w[3]), pk_half(w[4], w[5]),
-                                             pk_half(w[6], w[7]))}};
-            else
-                return pieces_of<NP>(w);
-        };
         float w[8];
         weights(0, w);
-        Pieces<NP> pf = operand(w);
+        Pieces<NW> pf = pieces_of<NW>(w);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             uint4 vn[DT];
-            Pieces<NP> pn;
+            Pieces<NW> pn;
             if (u < 3) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) vn[d] = load_v(u + 1, d);
                 weights(u + 1, w);
-                pn = operand(w);
+                pn = pieces_of<NW>(w);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int q = NP - 1; q >= 0; --q) o[d] = mfma32<HALF>(vf[d], pf.p[q], o[d]);
+                for (int q = NW - 1; q >= 0; --q) o[d] = mfma32(vf[d], pf.p[q], o[d]);
             if (u < 3) {
 #pragma unroll
-                for (int x = 0; x < DT * NP; ++x) {
+                for (int x = 0; x < DT * NW; ++x) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // a product
                     if (x < DT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // values of the next step
-                    __builtin_amdgcn_sched_group_barrier(0x002, F32 ? 9 : 28 / DT, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, F32 ? 9 : NW == 2 ? 32 / DT : 28 / DT, 0);
                     __builtin_amdgcn_sched_group_barrier(0x400, 8 / DT, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);

@@ -233,6 +233,45 @@ def test_scales_far_from_one(torch, factor, new, dtype):
     c.check()
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("gap", [8, 25.2, 33, 60, 90])
+def test_small_weights_beside_a_very_large_one(torch, gap, new, fmt, dtype):
+    """The first position's weight stands `gap` powers of two above those of all others, and half of
+    its values are 0: these outputs are made up by the others and held to the same bound."""
+    c = Case(torch, [300, 150], [new, new], 4, 2, 64, 16, fmt, dtype, seed=18)
+    encode = fp8.encode if fmt == "fp8" else round_bf16
+    c.q[:], c.q[..., 0] = 0, gap * np.log(2)
+    c.q = round_bf16(c.q) if dtype == "bf16" else c.q.astype(np.float32).astype(np.float64)
+    c.k[..., 0] = encode(np.zeros(c.k.shape[:3]))
+    first = c.table[:2, 0]
+    c.k[first, :, 0, 0] = encode(np.full((2, 2), 8.0))       # scale 1/8: a score of gap * ln 2
+    c.v[first, :, 0, 32:] = encode(np.zeros((2, 2, 32)))
+    if c.ks is not None:
+        c.ks[first, :, 0] = 1.0
+    c.check()
+    assert (c.out.view(c.T, 4, 64)[:, :, 32:] != 0).float().mean() > 0.9
+
+
+@pytest.mark.parametrize("power,dtype", [(-100, "bf16"), (112, "bf16"), (112, "fp32")])
+@pytest.mark.parametrize("new", [1, 40])
+def test_scales_as_far_from_one_as_values_go(torch, power, new, dtype):
+    """All value scales of a request near the ends of the type's range, zeros among them.  Pieces of
+    weight times scale below 2^-126 may be lost: with scales of 2^-107 the second pieces of weights
+    under 2^-11, 2^-18 of a weight of 1 each, where the bound has 2^-8 of all weights."""
+    c = Case(torch, [90, 200], [new, new], 4, 2, 64, 16, "fp8", dtype, pad=new > 1, seed=19)
+    c.vs *= np.float32(2.0 ** power)
+    c.vs[c.rng.random(c.vs.shape) < 0.1] = 0
+    c.device()
+    c.call()
+    k, v = c.values()
+    got = c.out.double().cpu().numpy().reshape(c.T, 4, 64)
+    rows = slice(0, 2 * new)
+    want, size, peak = opaged.attend(c.q, k, v, c.cu, c.lens, c.table, 0, 0, 0.125, np.zeros_like(got))
+    up = 2.0 ** -power
+    compare(got[rows] * up, want[rows] * up, size[rows] * up, peak[rows], 64, dtype)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "fp8"])
 def test_as_many_requests_as_there_may_be(torch, fmt):
     """4096 prompts of 1 to 40 tokens, ten launches; a sample of them against the oracle."""

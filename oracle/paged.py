@@ -110,7 +110,7 @@ def visible_positions(p, window, sinks):
 
 def attend(q, k_pages, v_pages, cu_new, seq_len, table, window, sinks, scale, out):
     """q [T, H, hd]; pages [n_pages, G, page, hd] as float64 values.  Returns (out, size, peak): out
-    [T, H, hd] with rows outside of the requests as given; size = sum of weight * |value| of every
+    [T, H, hd] with rows outside of the requests as given, 0 where all scores are -inf; size = sum of weight * |value| of every
     output; peak [T, H] = the largest sum of |scale q k| of a visible position."""
     n_pages, G, page, hd = k_pages.shape
     H = q.shape[1]
@@ -131,6 +131,9 @@ def attend(q, k_pages, v_pages, cu_new, seq_len, table, window, sinks, scale, ou
                 K, V = k_pages[pid, g, j % page], v_pages[pid, g, j % page]
                 for h in range(g * (H // G), (g + 1) * (H // G)):
                     s = (K @ q[t, h]) * scale
+                    if s.max() == -np.inf:
+                        out[t, h] = 0.0
+                        continue
                     w = np.exp(s - s.max())
                     w /= w.sum()
                     out[t, h] = w @ V

@@ -284,12 +284,17 @@ __device__ __forceinline__ uint32_t pk_bf16(float lo, float hi) {   // rounded t
 }
 
 // A matrix-core operand of 8 fp32 values in N bf16 pieces, all but the last of which are cut off
-// after 8 significant bits and the last rounded: one, two for 16 bits or three for the value.
+// after 8 significant bits and the last rounded: one, two for 16 bits or three for the value.  A
+// piece of 0 must not meet an infinite key or value, with which its product is NaN: where the
+// other operand `meets` infinities, pieces behind one that holds the value are 2^-40 and 2^-50 of
+// it, which no sum in 32 bits shows (from 2^-76 up; those of a smaller value may be 0).  `is`: the
+// values may be infinite themselves, all their pieces are then.
+enum class Infinity { never, meets, is };
 template <int N>
 struct Pieces {
     uint4 p[N];
 };
-template <int N>
+template <int N, Infinity INF>
 __device__ __forceinline__ Pieces<N> pieces_of(const float (&in)[8]) {
     Pieces<N> r;
     float x[8];
@@ -305,6 +310,12 @@ __device__ __forceinline__ Pieces<N> pieces_of(const float (&in)[8]) {
             x[2 * i] -= __uint_as_float(u0 & 0xffff0000u);
             x[2 * i + 1] -= __uint_as_float(u1 & 0xffff0000u);
         }
+        if constexpr (INF != Infinity::never)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(in[e], q == 0 ? 0x1p-40f : 0x1p-50f, x[e]);
+        if constexpr (INF == Infinity::is)   // (infinity less itself)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = x[e] == x[e] ? x[e] : in[e];
         r.p[q] = make_uint4(w[0], w[1], w[2], w[3]);
     }
     r.p[N - 1] = make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(x[4], x[5]), pk_bf16(x[6], x[7]));
@@ -320,7 +331,7 @@ __device__ __forceinline__ Pieces<F32 ? 3 : 1> load_q(const void *q, int64_t at,
         const float4 a = p[0], b = p[1];
         const float x[8] = {on ? a.x : 0.f, on ? a.y : 0.f, on ? a.z : 0.f, on ? a.w : 0.f,
                             on ? b.x : 0.f, on ? b.y : 0.f, on ? b.z : 0.f, on ? b.w : 0.f};
-        r = pieces_of<3>(x);
+        r = pieces_of<3, Infinity::is>(x);
     } else {
         const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(q) + at);
         r.p[0] = make_uint4(on ? v.x : 0u, on ? v.y : 0u, on ? v.z : 0u, on ? v.w : 0u);
@@ -505,6 +516,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     using S = TokenShape<HD, F8, F32>;
     constexpr int RB = S::RB, NS = S::NS, KS = HD / 32, DT = HD / 16;
     constexpr int NP = F32 ? 3 : 1, NW = F32 ? 3 : 2;   // pieces of a query value and of a weight
+    constexpr Infinity kValues = F8 ? Infinity::never : Infinity::meets;   // (no E4M3 code is infinite)
     using KSw = KSwizzle<RB>;
     using VSw = TokenVSwizzle<RB, F8>;
     // an array for each stage: the compiler then knows which loads a read of LDS has to wait for
@@ -687,7 +699,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
             l += w[e];
             if constexpr (F8) w[e] *= vs[e];
         }
-        const Pieces<NW> pf = pieces_of<NW>(w);
+        const Pieces<NW> pf = pieces_of<NW, kValues>(w);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             uint4 v;
@@ -790,6 +802,7 @@ template <int HD, bool F8, bool F32>
 __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void attend_tile(AttendArgs a) {
     constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32;
     constexpr int NP = F32 ? 3 : 1, NW = F32 ? 3 : F8 ? 2 : 1;   // pieces of a query value and of a weight
+    constexpr Infinity kValues = F8 ? Infinity::never : Infinity::meets;   // (no E4M3 code is infinite)
     using KSw = KSwizzle<RB>;
     using VSw = TileVSwizzle<RB>;
     __shared__ __align__(1024) uint8_t st0[2 * kTileUnit * RB], st1[2 * kTileUnit * RB];   // keys, values
@@ -1110,7 +1123,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         for (int d = 0; d < DT; ++d) vf[d] = load_v(0, d);
         float w[8];
         weights(0, w);
-        Pieces<NW> pf = pieces_of<NW>(w);
+        Pieces<NW> pf = pieces_of<NW, kValues>(w);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -1120,7 +1133,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
 #pragma unroll
                 for (int d = 0; d < DT; ++d) vn[d] = load_v(u + 1, d);
                 weights(u + 1, w);
-                pn = pieces_of<NW>(w);
+                pn = pieces_of<NW, kValues>(w);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d)

@@ -368,6 +368,68 @@ def test_a_nan_that_is_seen_is_nan(torch):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new,pad", [(1, 0), (1, 1), (40, 0)])
+def test_keys_of_minus_infinity_have_no_weight(torch, new, pad, dtype):
+    """Scores of -infinity are weights of 0, and rows that have no others are 0: the queries are bf16
+    numbers, so that an fp32 one is all in its first piece."""
+    c = Case(torch, [150, 90, 200], [new, new, new], 4, 2, 64, 16, "bf16", dtype, pad=pad, seed=20)
+    c.q = round_bf16(c.q)
+    c.q[..., 3] = np.abs(c.q[..., 3]) + 1
+    c.q[1, :, 11] = 1.0 + 2.0 ** -7
+    gone = c.rng.random(c.k.shape[:3]) < 0.3
+    gone[c.table[1, :cdiv(90, 16)]] = True                  # all of the second request's
+    gone[c.table[2, 12], :, 7] = False                      # the third's last is there
+    k, v = c.k.copy(), c.v
+    c.k[gone, 3] = -np.inf
+    c.device()
+    c.call()
+    got = c.out.double().cpu().numpy().reshape(c.T, 4, 64)
+    keys = k.copy()
+    keys[gone, 3] = -1e9                                    # weights of 0 in 64 bits as well
+    want, size, _ = opaged.attend(c.q, keys, v, c.cu, c.lens, c.table, 0, 0, 0.125, np.full_like(got, 7.0))
+    keys[gone, 3] = 0
+    peak = opaged.attend(c.q, keys, v, c.cu, c.lens, c.table, 0, 0, 0.125, np.full_like(got, 7.0))[2]
+    rows = slice(new, 2 * new)
+    assert (got[rows] == 0).all()
+    want[rows] = size[rows] = 0
+    compare(got, want, size, peak, 64, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new,pad", [(1, 0), (1, 1), (40, 0)])
+def test_queries_that_are_infinite(torch, new, pad, dtype):
+    """-infinity against keys of one sign: all scores -infinity, zeros; +infinity: NaN."""
+    c = Case(torch, [50, 70], [new, new], 2, 1, 64, 16, "bf16", dtype, pad=pad, seed=21)
+    c.k[..., 9] = np.abs(c.k[..., 9]) + 0.5
+    c.q[:, 0, 9], c.q[:, 1, 9] = -np.inf, np.inf
+    c.device()
+    c.call()
+    got = c.out.view(c.T, 2, 64)[:2 * new]
+    assert (got[:, 0] == 0).all() and torch.isnan(got[:, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new,pad", [(1, 0), (1, 1), (40, 0)])
+def test_values_that_are_infinite_and_seen(torch, new, pad, dtype):
+    """A weight times an infinite value is that infinity, whatever pieces the weight is held in; of
+    weight 1 (one position), and among others."""
+    c = Case(torch, [new, 90 + new, 300], [new, new, new], 4, 2, 64, 16, "bf16", dtype, pad=pad, seed=22)
+    c.v[c.table[:, 0], :, 0, 5:8] = np.inf, -np.inf, np.nan
+    c.v[c.table[2, 17], :, 0, 5] = -np.inf                  # with another sign: NaN
+    c.device()
+    c.call()
+    got = c.out.double().cpu().numpy().reshape(c.T, 4, 64)
+    with np.errstate(invalid="ignore"):
+        want, size, peak = opaged.attend(c.q, c.k, c.v, c.cu, c.lens, c.table, 0, 0, 0.125, np.full_like(got, 7.0))
+    assert np.isinf(want).any() and np.array_equal(np.isinf(got), np.isinf(want))
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    infinite = np.isinf(want)
+    for x in (got, want, size):
+        x[infinite] = 0
+    compare(got, want, size, peak, 64, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("new", [1, 40])
 def test_large_and_even_scores(torch, new, dtype):
     """Scores that stand far apart (weights of one position only) and all equal ones."""

@@ -67,6 +67,17 @@ def test_a_row_that_sees_nothing_is_zero_and_rows_behind_stay():
     assert (out[0] == 0).all() and (out[1] == 0).all() and (out[2] == 7).all()
 
 
+def test_a_row_whose_scores_are_all_minus_infinity_is_zero():
+    q = np.array([[[1.0, 2.0]], [[-1.0, 0.5]]])
+    pages = np.ones((2, 1, 1, 16, 2))
+    pages[0, 0, 0, :2, 0] = -np.inf
+    with np.errstate(invalid="ignore"):
+        out, size, _ = paged.attend(q, pages[0], pages[1], [0, 1, 2], [2, 1], np.array([[0], [0]]), 0, 0, 1.0,
+                                    np.full((2, 1, 2), 7.0))
+    assert (out[0] == 0).all() and (size[0] == 0).all()
+    assert np.isnan(out[1]).all()                   # a score of +infinity
+
+
 def test_store_rounds_rows():
     rows = np.array([[[1.0, -448.0, 2.0 ** -9, 0.0]], [[np.inf, 1, 1, 1]], [[0.0, 0, 0, 0]]])
     codes, scales = np.zeros((1, 1, 16, 4), np.uint8), np.full((1, 1, 16), 9.0, np.float32)

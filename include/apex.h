@@ -443,8 +443,10 @@ apex_status apex_paged_store(const apex_paged_cache *cache, const void *k, const
  * over the positions 0 <= j <= p with window == 0, or j > p - window, or j < sinks (a sliding
  * window of the last `window` positions besides which the first `sinks` stay visible).
  * Positions in a page whose id is outside [0, n_pages) are left out too; a row that sees
- * nothing, or whose scores are all -infinity, becomes 0.  Whatever keys and values hold at positions a row does not see (NaN
- * included) does not reach it.  Table entries and pages that no row sees are not read, so
+ * nothing, or whose scores are all -infinity, becomes 0.  Whatever keys and values hold at
+ * positions a row does not see (NaN included) does not reach it.  An infinite value that it sees
+ * makes NaN where its weight is 0 in 32 bits, and may where that is below 2^-76 of the largest.
+ * Table entries and pages that no row sees are not read, so
  * pages that left a window may be reused.  Rows before cu_new[0] and from cu_new[R] on are
  * left as they are.
  * Arithmetic: products on the matrix cores, sums, maxima and normalisers in fp32.  dtype

@@ -1074,13 +1074,15 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 const float4 b4 = *reinterpret_cast<const float4 *>(&scales[buf][1][16 * u + 8 + 4 * h]);
                 const float f[8] = {a4.x, a4.y, a4.z, a4.w, b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = CAREFUL && w[e] == 0.f ? 0.f : w[e] * f[e];
+                for (int e = 0; e < 8; ++e) w[e] *= f[e];
             }
         };
         // Where rows see different positions, a value that is no finite number must not meet the
         // zero weights of the rows that do not see it.  A tile that meets such a unit is worked
-        // on again, carefully: that unit's products then go one by one.  (Done at once, in this
-        // loop, the compiler moves all of o between registers three times a unit.)
+        // on again, carefully: that unit's products then go one by one, for the rows that see the
+        // position, whatever its weight: 0 times infinity is NaN there as in any other unit.
+        // (Done at once, in this loop, the compiler moves all of o between registers three times
+        // a unit.)
         const bool odd = all_flags & 0x01010101 * kOdd;
         met_odd = met_odd || odd;
         if (CAREFUL && odd) {
@@ -1097,6 +1099,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                         if (16 * u + 8 * (e / 4) + e % 4 == (j & ~4)) w = all_w[u][e];
                 const float other = __shfl_xor(w, 32);
                 w = ((j >> 2) & 1) == h ? w : other;
+                const bool on = visible(j0 + j, p, a.list.window, a.list.sinks);   // (rows of bad pages are 0)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -1106,7 +1109,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                                             apex::ffn::bf_hi(c.y)};
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            o[d][4 * e4 + e] = w == 0.f ? o[d][4 * e4 + e] : fmaf(w, v[e], o[d][4 * e4 + e]);
+                            o[d][4 * e4 + e] = on ? fmaf(w, v[e], o[d][4 * e4 + e]) : o[d][4 * e4 + e];
                     }
             }
             return;

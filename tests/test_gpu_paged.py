@@ -429,6 +429,44 @@ def test_values_that_are_infinite_and_seen(torch, new, pad, dtype):
     compare(got, want, size, peak, 64, dtype)
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 3)])
+@pytest.mark.parametrize("new,pad", [(1, 0), (1, 1), (90, 0)])
+def test_weights_of_zero_meet_values_that_are_not_finite(torch, new, pad, window, sinks, fmt, dtype):
+    """Seen values that are no finite numbers, with weights that are 0 in 32 bits: NaN or infinite for
+    each row that sees them, also where other rows of a tile do not, and nothing for those."""
+    c = Case(torch, [new + 200, new + 37, new], [new] * 3, 4, 2, 64, 16, fmt, dtype, pad=pad, seed=23)
+    encode = fp8.encode if fmt == "fp8" else round_bf16
+    c.q[..., 0] = 64.0
+    c.k[..., 0] = encode(np.ones(c.k.shape[:3]) * 8)
+    if c.ks is not None:
+        c.ks[:] = 1 / 8
+        c.k[..., 1:] = encode(c.rng.standard_normal(c.k.shape[:3] + (63,)) * 8)
+    spoilt = []                                             # a position of each page of each request
+    for r in range(3):
+        for j in range(5, int(c.lens[r]), 16):
+            pid = c.table[r, j // 16]
+            c.k[pid, :, j % 16, 0] = encode(np.full(2, -256.0))     # scores of -256 and less
+            c.v[pid, :, j % 16, 9] = np.inf if fmt == "bf16" else 0x7F
+            spoilt.append((r, j))
+    v = c.v.copy()
+    c.device()
+    c.call(window, sinks)
+    got = c.out.double().cpu().numpy().reshape(c.T, 4, 64)
+    for r, j in spoilt:
+        v[c.table[r, j // 16], :, j % 16, 9] = 0
+    c.v = v
+    want, size, peak = opaged.attend(c.q, *c.values(), c.cu, c.lens, c.table, window, sinks, 0.125, np.full_like(got, 7.0))
+    sees = np.zeros(c.T, bool)
+    for r in range(3):
+        for i in range(new):
+            seen = opaged.visible_positions(int(c.lens[r]) - new + i, window, sinks)
+            sees[c.cu[r] + i] = (seen % 16 == 5).any()
+    assert not np.isfinite(got[sees][..., 9]).any()
+    got[sees, :, 9] = want[sees, :, 9]
+    compare(got, want, size, peak, 64, dtype, norm=False)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("new", [1, 40])
 def test_large_and_even_scores(torch, new, dtype):

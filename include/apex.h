@@ -451,10 +451,10 @@ apex_status apex_paged_store(const apex_paged_cache *cache, const void *k, const
  * left as they are.
  * Arithmetic: products on the matrix cores, sums, maxima and normalisers in fp32.  dtype
  * APEX_TYPE_BF16: the result is rounded once to bf16, and before it the softmax weights (times the
- * value's scale) for the second product: to 16 bits or more over E4M3 pages and where T <= R, else to
- * bf16.  APEX_TYPE_FP32: no operand is rounded (fp32 values go through the matrix cores in three
- * pieces, three times the work).  Weight times scale below 2^-126 may count as 0.  No atomics:
- * results are deterministic.
+ * value's scale) for the second product: to 16 bits or more over E4M3 pages and where no request
+ * brings more than one token, else to bf16.  APEX_TYPE_FP32: no operand is rounded (fp32 values go
+ * through the matrix cores in three pieces, three times the work).  Weight times scale below 2^-126
+ * may count as 0.  No atomics: results are deterministic, and empty rows change none of their bits.
  *   q, out       device, type `dtype`: row t's [H, hd] at q + t * q_stride; strides in values,
  *                at least H * hd and multiples of 16 bytes; out may be q (same stride)
  *   cu_new, seq_len, block_table [R, max_blocks]   as apex_paged_plan leaves them

@@ -3,15 +3,15 @@
 // A tile is a group of query rows of one request and key/value head that are worked on together;
 // the positions it sees fall into units.  Launches of a call (for up to 512 tiles each):
 //   attend    Every workgroup lists the tiles and their units for itself (build_list), then its
-//             workers take their shares.  Tiles of one token (attend_token, a wavefront a worker)
-//             or of up to 128 query rows, heads of one group and consecutive tokens (attend_tile,
-//             a workgroup a worker).  The units of a head, tile after tile, are shared out evenly
-//             over its workers (or, many large tiles: whole tiles).  A tile within one share is
-//             written to `out`; where shares end inside a tile, its weighted sums, maxima and
-//             normalisers go to the workspace.
+//             workers take their shares.  By the lengths, tiles are of one token (attend_token, a
+//             wavefront a worker) or of up to 128 query rows, heads of one group and consecutive
+//             tokens (attend_tile, a workgroup a worker).  The units of a head, tile after tile,
+//             are shared out evenly over its workers (or, many large tiles: whole tiles).  A tile
+//             within one share is written to `out`; where shares end inside a tile, its weighted
+//             sums, maxima and normalisers go to the workspace.
 //   merge     the parts of such tiles joined by the log-sum-exp rule.
 //
-// Both kernels compute S^T = K Q^T and O^T = V^T P^T on the matrix cores: a lane then holds the
+// Both kinds compute S^T = K Q^T and O^T = V^T P^T on the matrix cores: a lane then holds the
 // scores of one query row in its registers, so that maxima, sums and rescaling are a lane's own
 // (but for one or two exchanges between lanes of a row), and the scores' registers are the
 // second product's operand as they stand.  The order of the positions within a step, which the
@@ -56,17 +56,18 @@ __device__ __forceinline__ T scalar_load(const T *p, int64_t i) {
     return ((Scalar)(p))[i];
 }
 
+constexpr int kCus = 256;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxGroup = 16;      // query heads per key/value head
 constexpr float kLog2e = 1.4426950408889634f;
 // Weights are 2^(score - m) for a reference m that is raised to the running maximum only when
 // that is more than kSlack above it: they stay below 2^kSlack, where sums in 32 bits and
-// roundings, which are relative, are as good, and rescaling is rare.  Tiles of up to kExactRows
-// rows, where a new maximum is rare enough, raise it at once: their largest weight is 1, which
-// no rounding to bf16 moves.  (Single tokens over bf16 pages: error 1.09 times that of the
-// result's rounding on average and at most 1.35 in 850 drawn cases; with the slack 1.20 and
-// 1.73.  77 us either way; chunks of 4096 and 2048 tokens without the slack take 4 to 7 % longer.)
+// roundings, which are relative, are as good, and rescaling is rare.  Of tiles of many rows
+// (attend_tile), those of up to kExactRows, where a new maximum is rare enough, raise it at once:
+// their largest weight is 1, which no rounding to bf16 moves.  (Tokens of a mixed batch over bf16
+// pages: error 1.09 times that of the result's rounding on average and at most 1.35 in 850 drawn
+// cases; with the slack 1.20 and 1.73.  Chunks of 4096 and 2048 tokens take 4 to 7 % longer without it.)
 constexpr float kSlack = 8.f;
 constexpr int kExactRows = 16;
 
@@ -76,21 +77,22 @@ constexpr int kExactRows = 16;
 __device__ __forceinline__ int lower_edge(int p, int window) { return window > 0 ? max(0, max(p, 0) - window + 1) : 0; }
 
 // The positions a tile of tokens [q0, q1) of a request sees: sink units from 0 up, then the
-// units from `first` up to the last token's position.  UP: positions of a unit.
+// units from `first` up to the last token's position.  A unit has 2^shift positions.
 struct Span {
     int sinks, first, units;
-    __device__ __forceinline__ int base(int u, int UP) const {
-        return (u < sinks ? u : first + u - sinks) * UP;
+    __device__ __forceinline__ int base(int u, int shift) const {
+        return (u < sinks ? u : first + u - sinks) << shift;
     }
 };
-template <int UP>
-__device__ __forceinline__ Span span_of(int p_first, int p_last, int window, int sinks) {
+__device__ __forceinline__ Span span_of(int p_first, int p_last, int window, int sinks, int shift) {
     Span s;
-    s.first = lower_edge(p_first, window) / UP;
-    s.sinks = window > 0 ? min(int((unsigned(min(sinks, p_last + 1)) + UP - 1) / UP), s.first) : 0;
-    s.units = p_last < 0 ? 0 : p_last / UP + 1 - s.first + s.sinks;
+    s.first = lower_edge(p_first, window) >> shift;
+    s.sinks = window > 0 ? min(int((unsigned(min(sinks, p_last + 1)) + (1u << shift) - 1) >> shift), s.first) : 0;
+    s.units = p_last < 0 ? 0 : (p_last >> shift) + 1 - s.first + s.sinks;
     return s;
 }
+constexpr int kTokenShift = 5, kTokenUnit = 1 << kTokenShift;   // of tiles of one token
+constexpr int kTileShift = 6, kTileUnit = 1 << kTileShift;      // of tiles of many rows
 
 // The new tokens [a, b) of request r among the rows of q, and its length, from device memory
 // and so held to their ranges.
@@ -112,6 +114,7 @@ struct TileList {                   // in LDS
     uint16_t r[kListTiles];         // its request
     uint8_t tokens[kListTiles];
     int wave_end[kWaves];
+    float tokens_all[kWaves], once[kWaves], each[kWaves];
     int found;
 };
 
@@ -154,29 +157,57 @@ struct ListArgs {
     int R, T, room, tile_tokens, first_tile, most_tiles, window, sinks;
 };
 
-// Tiles first_tile .. first_tile + most_tiles - 1 of all requests' tiles, those of a request in a
-// row; returns how many there are.  A few round trips to memory and barriers, about 3 us, where a
-// launch of its own that wrote the list for the next one took 7.  Loops are kept rolled: a
-// launch this short waits for its instructions as much as for its data.
-template <int UP>
-__device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
-    const int t = threadIdx.x;
-    const int per = (a.R + kThreads - 1) / kThreads;
+// Whether tokens are worked on one by one, and tiles first_tile .. first_tile + most_tiles - 1 of
+// all requests' tiles, those of a request in a row; returns how many there are.  A few round trips
+// to memory and barriers, about 3 us, where a launch of its own that wrote the list for the next
+// one took 7.  Loops are kept rolled: a launch this short waits for its instructions as much as
+// for its data.
+//
+// One by one: no more tokens than requests, and what each reads of its context adds up to at most
+// twice what the requests' contexts hold.  It is the tokens that count, not the rows of q, most of
+// which may be empty.  Single tokens one by one and in tiles of many rows, us (32 requests of up
+// to 4000 positions, 32 heads of 128 in 8 groups): bf16 73 and 78, E4M3 46 and 66, fp32 75 and 128,
+// fp32 over E4M3 47 and 157; 16 requests of 2 tokens 28 and 30, 8 of 4 25 and 24; one request's 64
+// tokens behind 8000 positions among 63 idle ones 166 and 35.
+__device__ __forceinline__ int build_list(const ListArgs &a, TileList &s, bool &one_by_one) {
+    const int t = threadIdx.x, wave = t / kWave;
+    const int per = (a.R + kThreads - 1) / kThreads, r_lo = t * per, r_hi = min(r_lo + per, a.R);
 #pragma unroll 1
     for (int i = t; i < kListTiles; i += kThreads) s.first[i] = -1;
-    const auto tiles_of = [&](int r) {
-        return int(unsigned(request_of(a.cu_new, a.seq_len, r, a.T, a.room).n + a.tile_tokens - 1) /
-                   unsigned(a.tile_tokens));
-    };
-    int count = 0, last = 0;
+    // (in fp32: tokens that lengths count twice pass 32 bits, and what decides is exact below 2^24)
+    float tokens_all = 0.f, once = 0.f, each = 0.f;
+    int n = 0;   // of a thread that has one request
 #pragma unroll 1
-    for (int r = t * per; r < min((t + 1) * per, a.R); ++r) count += last = tiles_of(r);
+    for (int r = r_lo; r < r_hi; ++r) {
+        const Request q = request_of(a.cu_new, a.seq_len, r, a.T, a.room);
+        n = q.n;
+        const unsigned most = a.window > 0 ? unsigned(a.window) + unsigned(a.sinks) : unsigned(INT_MAX);
+        const float context = float(min(unsigned(q.seq), most));
+        tokens_all += float(n);
+        once += n > 0 ? context : 0.f;
+        each += float(n) * context;
+    }
+    tokens_all = apex::ffn::wave_sum(tokens_all);
+    once = apex::ffn::wave_sum(once);
+    each = apex::ffn::wave_sum(each);
+    if (t % kWave == 0) s.tokens_all[wave] = tokens_all, s.once[wave] = once, s.each[wave] = each;
+    __syncthreads();
+    tokens_all = once = each = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) tokens_all += s.tokens_all[w], once += s.once[w], each += s.each[w];
+    one_by_one = uniform(tokens_all <= float(a.R) && each <= 2.f * once);
+    const int tile_tokens = one_by_one ? 1 : a.tile_tokens, shift = one_by_one ? kTokenShift : kTileShift;
+    const auto tiles_of = [&](int n) { return int(unsigned(n + tile_tokens - 1) / unsigned(tile_tokens)); };
+    const auto tokens_of = [&](int r) { return per == 1 ? n : request_of(a.cu_new, a.seq_len, r, a.T, a.room).n; };
+    int count = 0;
+#pragma unroll 1
+    for (int r = r_lo; r < r_hi; ++r) count += tiles_of(tokens_of(r));
     int at, total;
     block_scan<false>(count, s.wave_end, &at, &total);
     // the first tile of each request in the list names it
 #pragma unroll 1
-    for (int r = t * per; r < min((t + 1) * per, a.R); ++r) {
-        const int n = per == 1 ? last : tiles_of(r);
+    for (int r = r_lo; r < r_hi; ++r) {
+        const int n = tiles_of(tokens_of(r));
         if (n > 0 && at + n > a.first_tile && at < a.first_tile + kListTiles) {
             const int i = max(at - a.first_tile, 0);
             s.first[i] = at;
@@ -187,7 +218,7 @@ __device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
     const int tiles = min(max(total - a.first_tile, 0), a.most_tiles);
     __syncthreads();
     // a thread's tiles, in a row; the tiles between two named ones are the first one's
-    const int each = (tiles + kThreads - 1) / kThreads, i0 = t * each, i1 = min(i0 + each, tiles);
+    const int share = (tiles + kThreads - 1) / kThreads, i0 = t * share, i1 = min(i0 + share, tiles);
     int named = -1, before, all;
 #pragma unroll 1
     for (int i = i0; i < i1; ++i)
@@ -199,10 +230,10 @@ __device__ __forceinline__ int build_list(const ListArgs &a, TileList &s) {
         if (s.first[i] >= 0) before = i;
         const int k = max(before, 0), first = s.first[k], r = s.r[k];
         const Request q = request_of(a.cu_new, a.seq_len, r, a.T, a.room);
-        const int q0 = (a.first_tile + i - first) * a.tile_tokens;
-        const int p = q.seq - q.n + q0, tokens = min(a.tile_tokens, q.n - q0);
+        const int q0 = (a.first_tile + i - first) * tile_tokens;
+        const int p = q.seq - q.n + q0, tokens = min(tile_tokens, q.n - q0);
         // a tile that sees nothing still has a unit: its rows are written
-        sum += max(span_of<UP>(p, p + tokens - 1, a.window, a.sinks).units, 1);
+        sum += max(span_of(p, p + tokens - 1, a.window, a.sinks, shift).units, 1);
         s.cu[i + 1] = sum;
         s.row[i] = q.row0 + q0;
         s.p[i] = p;
@@ -253,9 +284,9 @@ struct AttendArgs {
     const int32_t *block_table;
     ListArgs list;
     int G, GR, max_blocks, shift, page_size, n_pages;
-    int workers;           // workgroups that share out a head's units
+    int workers, token_workers;   // that share out a head's units: workgroups, or wavefronts
     float scale_log2;      // the softmax scale times log2(e)
-    int *tiles;            // how many the launch has
+    int2 *tiles;           // how many the launch has, and whether of one token
     Split *split;          // [tile][G]
     float *part_o;         // [worker][G][2][rows][hd]
     float2 *part_ml;       // [worker][G][2][rows]: maximum (of scores in powers of two), normaliser
@@ -487,54 +518,66 @@ __device__ __forceinline__ void store_out(void *out, int64_t at, float v) {
 
 // ------------------------------------------------------------------------- one token's tile
 // A tile is one token and the query heads of a group: up to 16 rows, columns of the 16x16x32
-// products.  Each wavefront is a worker of its own, on units of 32 positions, with a ring of
-// stages in LDS: behind the list no barrier, only the wavefront's own count of loads.  (Four
+// products.  Each wavefront is a worker of its own, on units of 32 positions, with stages of its
+// own in LDS: behind the list no barrier, only the wavefront's own count of loads.  (Four
 // wavefronts on one tile, joined in LDS: 256 requests of 64 to 256 positions 60 us instead of
 // 42, where a tile is over before its loads are under way; long contexts the same.)
 // Lane (q = lane % 16, lg = lane / 16) holds the scores of row q at positions 16 m + 4 lg + i.
 // bf16 weights go through the second product in two pieces, 16 bits: the products wait for memory
 // anyway, and rounded to 8 bits they would err as much as the rounding of the result, with E4M3
 // scales, which alike rows have alike, up to 1.7 times as much.
-// Bound by the stream of keys and values: 64 tokens under a window of 4096 (1.08 GB) 187 us,
-// 5.75 TB/s, of 5.8 that a kernel that only reads gets.
-constexpr int kTokenUnit = 32;
+// Bound by the stream of keys and values: 64 tokens under a window of 4096 (1.08 GB) 190 us,
+// 5.65 TB/s, of 5.8 that a kernel that only reads gets.
 constexpr int kMostParts = 512;   // of a launch's tiles, on average: one request of 60000 positions
                                   // in one group 21 us; in 1024 parts, as many as fit, 24, in 128 28
+constexpr int kTokenShare = 8;    // units: 256 requests of 64 to 256 positions (5 units a share) 50 us with
+                                  // all workers, 47 with half; 31 of up to 4096 (12 units) 71.5 and 79.8
 
+// Stages in LDS, and how many workgroups a CU holds: of tiles of many rows by their registers.
 template <int HD, bool F8, bool F32>
-struct TokenShape {
-    static constexpr int RB = HD * (F8 ? 1 : 2);
-    static constexpr int kStage = 2 * 32 * RB;              // keys and values of 32 positions
-    static constexpr int NS = kStage > 4096 ? 2 : 4;        // stages
-    static constexpr int kRing = kWaves * NS * kStage;
-    static constexpr int kPerCu = kRing > 65536 ? 1 : 2;    // workgroups that a CU's LDS holds
-    static constexpr int kLoads = kStage / 1024 + (F8 ? 1 : 0);
+struct Shape {
+    static constexpr int kPerCu = HD == 128 ? (F32 ? 1 : 2) : (F8 || F32 ? 2 : 3);
+    // tiles of many rows: keys and values of a unit, two stages
+    static constexpr int kTileStage = 2 * kTileUnit * HD * 2;
+    // tiles of one token: the same of 32 positions for each wavefront, a ring of kTokenStages; of
+    // what the workgroups of a CU leave room for, or one stage, where keys and values take turns
+    static constexpr int kRowBytes = HD * (F8 ? 1 : 2);
+    static constexpr int kTokenStage = 2 * kTokenUnit * kRowBytes;
+    static constexpr int kRing = 1024 * (kPerCu == 1 ? 128 : kPerCu == 2 ? 64 : 32);
+    static constexpr int kTokenStages = kRing / (kWaves * kTokenStage);
+    static_assert(kTokenStages == 1 || kTokenStages == 2 || kTokenStages == 4, "a ring");
+    static constexpr int kTokenLoads = kTokenStage / 1024 + (F8 ? 1 : 0);
+    static constexpr int kTokenArray = kWaves * kTokenStage / (kTokenStages == 1 ? 2 : 1);
+    static constexpr int kStage = kTokenArray > kTileStage ? kTokenArray : kTileStage;
+    // What parts and their merge cost a call where every workgroup leaves two, about 25 us, in the
+    // time of a unit (us, with a CU full of workgroups: 2.1, E4M3 3.1, fp32 2.9; heads of 64
+    // 1.5, 2.2 and 1.9).
+    static constexpr float kSplitCost = HD == 128 ? (F32 || F8 ? 8.f : 12.f) : (F32 ? 13.f : F8 ? 11.f : 16.f);
+};
+
+// LDS of a workgroup.  An array for each stage: the compiler then knows which loads a read of LDS
+// has to wait for.
+struct Stages {
+    uint8_t *st0, *st1, *st2, *st3;
 };
 
 template <int HD, bool F8, bool F32>
-__global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
-    using S = TokenShape<HD, F8, F32>;
-    constexpr int RB = S::RB, NS = S::NS, KS = HD / 32, DT = HD / 16;
+__device__ __forceinline__ void attend_token(const AttendArgs &a, TileList &list, int tiles, const Stages &lds_stages,
+                                             float (*scales)[64]) {
+    using S = Shape<HD, F8, F32>;
+    constexpr int RB = S::kRowBytes, NS = S::kTokenStages, KS = HD / 32, DT = HD / 16;
     constexpr int NP = F32 ? 3 : 1, NW = F32 ? 3 : 2;   // pieces of a query value and of a weight
     constexpr Infinity kValues = F8 ? Infinity::never : Infinity::meets;   // (no E4M3 code is infinite)
     using KSw = KSwizzle<RB>;
     using VSw = TokenVSwizzle<RB, F8>;
-    // an array for each stage: the compiler then knows which loads a read of LDS has to wait for
-    __shared__ __align__(1024) uint8_t st0[kWaves][S::kStage], st1[kWaves][S::kStage];
-    __shared__ __align__(1024) uint8_t st2[NS > 2 ? kWaves : 1][NS > 2 ? S::kStage : 16];
-    __shared__ __align__(1024) uint8_t st3[NS > 2 ? kWaves : 1][NS > 2 ? S::kStage : 16];
-    __shared__ __align__(16) float scales[kWaves][64];
-    __shared__ TileList list;
     const int wg = uniform(blockIdx.x / a.G), g = blockIdx.x - wg * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int w = wg * kWaves + wave;
     const int n = lane & 15, lg = lane >> 4;
-    const int tiles = build_list<kTokenUnit>(a.list, list);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.tiles[0] = tiles;
     const int all_units = uniform(list.cu[tiles]);
-    if (all_units == 0) return;
-    // none without a unit
-    const int workers = min(a.workers, min(all_units, kMostParts * tiles));
+    // None without a unit; one workgroup a CU where two would have small shares.
+    const bool half = S::kTokenStages == 1 && all_units / kTokenShare < a.token_workers;
+    const int workers = min(half ? (a.token_workers + 1) / 2 : a.token_workers, min(all_units, kMostParts * tiles));
     if (w >= workers) return;
     const Shares shares(all_units, workers);
     const int share_lo = uniform(shares.begin(w)), share_hi = uniform(shares.begin(w + 1));
@@ -551,24 +594,27 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     tile = uniform(tile);
 
     // where this lane reads, in a stage: keys of row n (and n + 16), values of row v_row (and,
-    // bf16, v_row + 16); both swizzles are the same 16 rows further
+    // bf16, v_row + 16); both swizzles are the same 16 rows further.  HALVES: one stage, its keys in
+    // the first array and its values in the second.
+    constexpr bool HALVES = NS == 1;
+    constexpr int kKeys = 32 * RB, kPlace = HALVES ? kKeys : 2 * kKeys, kValuesAt = HALVES ? 0 : kKeys;
     int k_at[KS], v_at[DT];
     const int kv = n >> 1, v_row = F8 ? (kv < 4 ? 4 * lg + kv : 12 + 4 * lg + kv) : 4 * lg + (n >> 2);
 #pragma unroll
     for (int u = 0; u < KS; ++u)
-        k_at[u] = settled(wave * S::kStage + n * RB +
+        k_at[u] = settled(wave * kPlace + n * RB +
                           (F8 ? 16 * ((2 * u + lg / 2) ^ KSw::of(n)) + 8 * (lg & 1)
                               : 16 * ((4 * u + lg) ^ KSw::of(n))));
 #pragma unroll
     for (int d = 0; d < DT; ++d)
-        v_at[d] = settled(wave * S::kStage + (32 + v_row) * RB + 8 * (lane & 1) +
+        v_at[d] = settled(wave * kPlace + kValuesAt + v_row * RB + 8 * (lane & 1) +
                           16 * ((F8 ? d : 2 * d + ((lane & 3) >> 1)) ^ VSw::of(v_row)));
     const auto stage = [&](auto which) __attribute__((always_inline)) -> uint8_t * {
         constexpr int st = decltype(which)::value;
-        if constexpr (st == 0) return st0[0];
-        else if constexpr (st == 1) return st1[0];
-        else if constexpr (st == 2) return st2[0];
-        else return st3[0];
+        if constexpr (st == 0) return lds_stages.st0;
+        else if constexpr (st == 1) return lds_stages.st1;
+        else if constexpr (st == 2) return lds_stages.st2;
+        else return lds_stages.st3;
     };
     const GlobalFloats scale_of = lane_pointer(a.k_scales, a.v_scales, lane >= 32);
     float sc[NS];           // this lane's scale of a stage: keys in lanes 0..31, values behind
@@ -581,7 +627,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     const int u_lo = uniform(z - tile_lo), steps = uniform(min(tile_hi, share_hi) - z);
     const int req = uniform(list.r[tile]), p = uniform(list.p[tile]), hi = p + 1;
     const int low = lower_edge(p, a.list.window);
-    const Span span = span_of<kTokenUnit>(p, p, a.list.window, a.list.sinks);
+    const Span span = span_of(p, p, a.list.window, a.list.sinks, kTokenShift);
     const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
     const int64_t row = uniform(list.row[tile]);
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
@@ -592,32 +638,40 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
         qf[u] = load_q<F32>(a.q, row * a.q_stride + (g * a.GR + (n < a.GR ? n : 0)) * HD + 32 * u + 8 * lg,
                             n < a.GR);
 
-    const auto issue = [&](auto which, int i) __attribute__((always_inline)) {
-        constexpr int st = decltype(which)::value;
-        const int j0 = span.base(u_lo + min(i, steps - 1), kTokenUnit);
-        const int end = i < steps ? hi : 0;
-        Rows16 r[2];
+    // unit i's rows, nothing of which is to be read from the last unit on
+    const auto unit_at = [&](int i) { return span.base(u_lo + min(i, steps - 1), kTokenShift); };
+    const auto rows_of = [&](int i, Rows16 (&r)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) r[m] = rows16(a, table, g, unit_at(i) + 16 * m, i < steps ? hi : 0);
+    };
+    const auto load_keys = [&](int i, const Rows16 (&r)[2], uint8_t *at) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            r[m] = rows16(a, table, g, j0 + 16 * m, end);
-            ok[st][m] = r[m].ok;
+            const int j = unit_at(i) + 16 * m;
+            load_rows16<RB, KSw>(a.k_pages, r[m], low - j, a.list.sinks - j, at, wave * kPlace + 16 * m * RB, 16 * m);
         }
+    };
+    const auto load_values = [&](int i, const Rows16 (&r)[2], uint8_t *at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int j = unit_at(i) + 16 * m;
+            load_rows16<RB, VSw>(a.v_pages, r[m], low - j, a.list.sinks - j, at, wave * kPlace + kValuesAt + 16 * m * RB,
+                                 16 * m);
+        }
+    };
+    const auto issue = [&](auto which, int i) __attribute__((always_inline)) {
+        constexpr int st = decltype(which)::value;
+        Rows16 r[2];
+        rows_of(i, r);
+        ok[st][0] = r[0].ok;
+        ok[st][1] = r[1].ok;
         if constexpr (F8) {
             const int64_t at = lane & 16 ? r[1].row : r[0].row;
             const int last = max((lane & 16 ? r[1].end : r[0].end) - 1, 0);
             sc[st] = scale_of[at + min(n, last)];
         }
-        uint8_t *at = stage(which);
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int j = j0 + 16 * m;
-            load_rows16<RB, KSw>(a.k_pages, r[m], low - j, a.list.sinks - j, at, wave * S::kStage + 16 * m * RB, 16 * m);
-        }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int j = j0 + 16 * m;
-            load_rows16<RB, VSw>(a.v_pages, r[m], low - j, a.list.sinks - j, at, wave * S::kStage + (32 + 16 * m) * RB, 16 * m);
-        }
+        load_keys(i, r, stage(which));
+        load_values(i, r, stage(which));
         __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -625,28 +679,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
     floatx4 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const auto step = [&](auto which, int i) __attribute__((always_inline)) {
-        constexpr int st = decltype(which)::value;
-        constexpr int ahead = (st + NS - 1) % NS;
-        issue(Int<ahead>{}, i + NS - 1);
-        wait_loads<S::kLoads *(NS - 1)>();
-        const int j0 = span.base(u_lo + i, kTokenUnit);
-        const uint8_t *lds = stage(which);
-        float ks[8], vs[8];
-        if constexpr (F8) {
-            scales[wave][lane] = sc[st];
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    ks[4 * m + e] = scales[wave][16 * m + 4 * lg + e];
-                    vs[4 * m + e] = scales[wave][32 + 16 * m + 4 * lg + e];
-                }
-        }
-        float s[8];
+    const auto products = [&](const uint8_t *lds, float (&s)[8]) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             floatx4 big = floatx4{0.f, 0.f, 0.f, 0.f}, small = big;
@@ -662,19 +695,25 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
                 big = mfma16(k, qf[u].p[0], big);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[4 * m + e] = F32 ? big[e] + small[e] : big[e];
-                if constexpr (F8) s[4 * m + e] *= ks[4 * m + e];
-            }
+            for (int e = 0; e < 4; ++e) s[4 * m + e] = F32 ? big[e] + small[e] : big[e];
         }
-        const bool whole = j0 + 31 < hi && (j0 >= low || j0 + 31 < a.list.sinks) && ok[st][0] && ok[st][1];
+        if constexpr (HALVES) {   // all reads of LDS first: left to itself, each product waits for its own
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * KS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2 * KS * NP, 0);
+        }
+    };
+    // scores to weights (times the values' scales vs) of unit i, whose pages are ok
+    const auto weights = [&](int i, bool ok0, bool ok1, float (&s)[8], float (&vs)[8])
+                             __attribute__((always_inline)) {
+        const int j0 = unit_at(i);
+        const bool whole = j0 + 31 < hi && (j0 >= low || j0 + 31 < a.list.sinks) && ok0 && ok1;
         if (!whole) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + 16 * m + 4 * lg + e;
-                    const bool on = j < hi && (j >= low || j < a.list.sinks) && ok[st][m];
+                    const bool on = j < hi && (j >= low || j < a.list.sinks) && (m ? ok1 : ok0);
                     s[4 * m + e] = on ? s[4 * m + e] : -INFINITY;
                     if constexpr (F8) vs[4 * m + e] = on ? vs[4 * m + e] : 0.f;
                 }
@@ -692,14 +731,15 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
             for (int d = 0; d < DT; ++d) o[d] *= c;
         }
         const float ref = mx == -INFINITY ? 0.f : mx;
-        float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, -ref));
-            l += w[e];
-            if constexpr (F8) w[e] *= vs[e];
+            s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, -ref));
+            l += s[e];
+            if constexpr (F8) s[e] *= vs[e];
         }
-        const Pieces<NW> pf = pieces_of<NW, kValues>(w);
+        return pieces_of<NW, kValues>(s);
+    };
+    const auto accumulate = [&](const uint8_t *lds, const Pieces<NW> &pf) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             uint4 v;
@@ -712,24 +752,80 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 #pragma unroll
             for (int q = NW - 1; q >= 0; --q) o[d] = mfma16(v, pf.p[q], o[d]);
         }
+        if constexpr (HALVES) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, DT * NW, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
-    issue(Int<0>{}, 0);
-    if constexpr (NS == 4) {
-        issue(Int<1>{}, 1);
-        issue(Int<2>{}, 2);
-    }
-    int i = 0;
-    while (true) {
-        step(Int<0>{}, i);
-        if (++i == steps) break;
-        step(Int<1>{}, i);
-        if (++i == steps) break;
+    const auto step = [&](auto which, int i) __attribute__((always_inline)) {
+        constexpr int st = decltype(which)::value;
+        constexpr int ahead = (st + NS - 1) % NS;
+        issue(Int<ahead>{}, i + NS - 1);
+        wait_loads<S::kTokenLoads *(NS - 1)>();
+        float s[8], ks[8], vs[8];
+        if constexpr (F8) {
+            scales[wave][lane] = sc[st];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ks[4 * m + e] = scales[wave][16 * m + 4 * lg + e];
+                    vs[4 * m + e] = scales[wave][32 + 16 * m + 4 * lg + e];
+                }
+        }
+        products(stage(which), s);
+        if constexpr (F8)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] *= ks[e];
+        accumulate(stage(which), weights(i, ok[st][0], ok[st][1], s, vs));
+    };
+    if constexpr (HALVES) {
+        // The next unit's keys are loaded once the keys are multiplied, its values once these are:
+        // a half is always on its way, and a CU has twice the wavefronts that whole stages would
+        // leave room for.
+        Rows16 r[2], next[2];
+        rows_of(0, r);
+        load_keys(0, r, stage(Int<0>{}));
+        load_values(0, r, stage(Int<1>{}));
+        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < steps; ++i) {
+            float s[8], vs[8];
+            rows_of(i + 1, next);
+            wait_loads<S::kTokenLoads / 2>();
+            products(stage(Int<0>{}), s);
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(i + 1, next, stage(Int<0>{}));
+            __builtin_amdgcn_sched_barrier(0);
+            const Pieces<NW> pf = weights(i, r[0].ok, r[1].ok, s, vs);
+            wait_loads<S::kTokenLoads / 2>();
+            accumulate(stage(Int<1>{}), pf);
+            load_values(i + 1, next, stage(Int<1>{}));
+            __builtin_amdgcn_sched_barrier(0);
+            r[0] = next[0];
+            r[1] = next[1];
+        }
+    } else {
+        issue(Int<0>{}, 0);
         if constexpr (NS == 4) {
-            step(Int<2>{}, i);
+            issue(Int<1>{}, 1);
+            issue(Int<2>{}, 2);
+        }
+        int i = 0;
+        while (true) {
+            step(Int<0>{}, i);
             if (++i == steps) break;
-            step(Int<3>{}, i);
+            step(Int<1>{}, i);
             if (++i == steps) break;
+            if constexpr (NS == 4) {
+                step(Int<2>{}, i);
+                if (++i == steps) break;
+                step(Int<3>{}, i);
+                if (++i == steps) break;
+            }
         }
     }
     l = sum_xor32(sum_xor16(l));
@@ -771,7 +867,7 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // one is multiplied (one barrier per unit).  Lane (q = lane % 32, h = lane / 32) holds the
 // scores of row q at positions 32 m + 8 (i / 4) + 4 h + i % 4.
 // Bound by the matrix cores and what they wait for: 4096 tokens of 32 heads of 128 behind 12288
-// positions (962 GFLOP) 912 us, 1050 TFLOP/s, where a library's product of 8192^3 gets 1198 and
+// positions (962 GFLOP) 900-930 us, 1030-1070 TFLOP/s, where a library's product of 8192^3 gets 1198 and
 // both are held back by the card's power (clocks of 1.9 and 1.8 GHz).  Of a unit's 4400 cycles
 // (two workgroups on a CU) the products take half; the rest are the softmax's 32 maxima and
 // exponentials a lane, which the other workgroup's products overlap, and the wait for the loads.
@@ -781,50 +877,42 @@ __global__ __launch_bounds__(kThreads) void attend_token(AttendArgs a) {
 // rounding of the result, as alike rows have alike scales; one of fp16, 1140-1160, loses what is 25
 // powers of two below a row's largest product but in its normaliser, and with it outputs that such
 // positions make up.  fp32 in three pieces: 390 TFLOP/s without counting them three times.
-constexpr int kTileUnit = 64;
 constexpr int kTileRows = 128;
 // Units of a share at least: a part is 64 KB.  64 tokens behind 1000 positions, heads of 128: 22.0
 // us with 2 (and with 1), 25.1 with 4, 34.2 with 16; 64 tokens behind 8000: 36.0, with 4 34.0.
 constexpr int kMinShare = 2;
 constexpr int kBadPage = 1, kOdd = 2;
 
-template <int HD, bool F8, bool F32>
-struct TileShape {
-    // workgroups that a CU's registers hold
-    static constexpr int kPerCu = HD == 128 ? (F32 ? 1 : 2) : (F8 || F32 ? 2 : 3);
-    // What parts and their merge cost a call where every workgroup leaves two, about 25 us, in the
-    // time of a unit (us, with a CU full of workgroups: 2.1, E4M3 3.1, fp32 2.9; heads of 64
-    // 1.5, 2.2 and 1.9).
-    static constexpr float kSplitCost = HD == 128 ? (F32 || F8 ? 8.f : 12.f) : (F32 ? 13.f : F8 ? 11.f : 16.f);
+struct TileScratch {                // in LDS
+    float scales[2][2][kTileUnit];      // keys' times scale_log2; values'
+    uint8_t group_flags[2][4];          // of a unit's 16 rows each: kBadPage, kOdd
+    int wave_odd[kWaves];
 };
 
 template <int HD, bool F8, bool F32>
-__global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void attend_tile(AttendArgs a) {
+__device__ __forceinline__ void attend_tile(const AttendArgs &a, TileList &list, int tiles, const Stages &lds_stages,
+                                            TileScratch &scratch) {
     constexpr int RB = HD * 2, KS = HD / 16, DT = HD / 32;
     constexpr int NP = F32 ? 3 : 1, NW = F32 ? 3 : F8 ? 2 : 1;   // pieces of a query value and of a weight
     constexpr Infinity kValues = F8 ? Infinity::never : Infinity::meets;   // (no E4M3 code is infinite)
     using KSw = KSwizzle<RB>;
     using VSw = TileVSwizzle<RB>;
-    __shared__ __align__(1024) uint8_t st0[2 * kTileUnit * RB], st1[2 * kTileUnit * RB];   // keys, values
-    __shared__ __align__(16) float scales[2][2][kTileUnit];   // keys' times scale_log2; values'
-    __shared__ uint8_t group_flags[2][4];   // of a unit's 16 rows each: kBadPage, kOdd
-    __shared__ int wave_odd[kWaves];
-    __shared__ TileList list;
+    uint8_t *const st0 = lds_stages.st0, *const st1 = lds_stages.st1;   // keys, values
+    float (&scales)[2][2][kTileUnit] = scratch.scales;
+    uint8_t (&group_flags)[2][4] = scratch.group_flags;
+    int (&wave_odd)[kWaves] = scratch.wave_odd;
     const int w = uniform(blockIdx.x / a.G), g = blockIdx.x - w * a.G;
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n = lane & 31, h = lane >> 5;
-    const int tiles = build_list<kTileUnit>(a.list, list);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.tiles[0] = tiles;
     const int all_units = uniform(list.cu[tiles]);
-    if (all_units == 0) return;
     // Whole tiles, the last ones (of a request: the longest) first, or even shares of the units.
     // In units: even shares take all / workers and kSplitCost for as many parts as they leave;
     // whole tiles as long as the longest one (which runs faster towards the end, alone on its
     // CU), or all / workers and what the last round, the first `rest` tiles, leaves idle.
-    // Whole and even, us: a prompt of 2048 tokens 60 and 88, eight E4M3 chunks of 700 tokens behind
-    // up to 3500 positions 177 and 184, 4096 tokens behind 12288 960 and 1057; 512 tokens behind
-    // 4096 100 and 66, 31 single tokens 103 and 76, 2048 fp32 tokens of heads of 64 behind 6144
-    // 298 and 268.
+    // Whole and even, us: a prompt of 2048 tokens 59 and 88, eight E4M3 chunks of 700 tokens behind
+    // up to 3500 positions 181 and 182 (bf16 119 and 135), 4096 tokens behind 12288 897 and 964;
+    // 512 tokens behind 4096 94 and 64, eight requests of 4 tokens 47 and 25, 2048 fp32 tokens of
+    // heads of 64 behind 6144 304 and 276.
     const int workers = max(min(a.workers, all_units / kMinShare), 1);
     const int rest = tiles % a.workers;
     const float even = float(all_units) / workers, parts = float(workers + min(tiles, workers)) / (2 * a.workers);
@@ -835,25 +923,21 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     __syncthreads();
     longest = float(max(max(list.wave_end[0], list.wave_end[1]), max(list.wave_end[2], list.wave_end[3])));
     const float idle = rest ? (1.f - float(rest) / a.workers) * list.cu[rest] / rest : 0.f;
-    const float whole = fmaxf((TileShape<HD, F8, F32>::kPerCu == 2 ? 0.75f : 1.f) * longest,
+    const float whole = fmaxf((Shape<HD, F8, F32>::kPerCu == 2 ? 0.75f : 1.f) * longest,
                               float(all_units) / a.workers + idle);
-    const bool whole_tiles = uniform(whole <= even + parts * TileShape<HD, F8, F32>::kSplitCost);
+    const bool whole_tiles = uniform(whole <= even + parts * Shape<HD, F8, F32>::kSplitCost);
     const Shares shares(all_units, workers);
-    int share_lo, share_hi, tile;
-    if (whole_tiles) {
-        if (w >= tiles) return;
-        tile = tiles - 1 - w;
-        // one round: workgroup i + 256 comes to workgroup i's CU, so a long one meets a short one
-        if (TileShape<HD, F8, F32>::kPerCu == 2 && tiles <= a.workers && w >= a.workers / 2)
-            tile = w - a.workers / 2;
-        share_lo = uniform(list.cu[tile]);
-        share_hi = uniform(list.cu[tile + 1]);
-    } else {
-        if (w >= workers) return;
-        share_lo = uniform(shares.begin(w));
-        share_hi = uniform(shares.begin(w + 1));
-        tile = tile_of(list, tiles, share_lo);
-    }
+    // Whole tiles in turns of all workgroups.  (One round: workgroup i + 256 comes to workgroup i's
+    // CU, so that a long one meets a short one.)
+    const int groups = gridDim.x / a.G;
+    const auto whole_tile = [&](int turn) {
+        return Shape<HD, F8, F32>::kPerCu == 2 && tiles <= a.workers && turn >= a.workers / 2 ? turn - a.workers / 2
+                                                                                             : tiles - 1 - turn;
+    };
+    if (w >= (whole_tiles ? tiles : workers)) return;
+    int turn = w, tile = whole_tiles ? whole_tile(w) : tile_of(list, tiles, shares.begin(w));
+    int share_lo = uniform(whole_tiles ? list.cu[tile] : shares.begin(w));
+    int share_hi = uniform(whole_tiles ? list.cu[tile + 1] : shares.begin(w + 1));
     const int m_row = 32 * wave + n, tok = m_row / a.GR, head = m_row - tok * a.GR;
     // where this lane reads, in a stage: keys of row n (and n + 32), values of rows v_row and
     // v_row + 8 of 16; the swizzles are the same 8, 16 and 32 rows further
@@ -877,7 +961,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     const int row0 = uniform(list.row[tile]);
     const int p_first = uniform(list.p[tile]), p_last = p_first + tokens - 1, hi = p_last + 1;
     const int low = lower_edge(p_first, a.list.window);
-    const Span span = span_of<kTileUnit>(p_first, p_last, a.list.window, a.list.sinks);
+    const Span span = span_of(p_first, p_last, a.list.window, a.list.sinks, kTileShift);
     const int32_t *table = a.block_table + size_t(req) * a.max_blocks;
     const int part = z == tile_lo && tile_hi <= share_hi ? -1 : z == share_lo ? 0 : 1;
     const bool row_on = tok < tokens;
@@ -901,7 +985,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
     // A unit's page id is loaded a unit ahead, as a vector load: a scalar one would be waited for
     // with the reads of LDS.
     int page = -1;
-    const auto rows_at = [&](int i) { return span.base(u_lo + min(i, steps - 1), kTileUnit) + 16 * wave; };
+    const auto rows_at = [&](int i) { return span.base(u_lo + min(i, steps - 1), kTileShift) + 16 * wave; };
     const auto load_page = [&](int i) {
         page = ((GlobalInts)(table))[min(rows_at(i) >> a.shift, a.max_blocks - 1)];
     };
@@ -968,7 +1052,7 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         if constexpr (F8)
             if (lane < 32) scales[buf][lane >> 4][16 * wave + (lane & 15)] = lane < 16 ? sc * a.scale_log2 : sc;
         wait_loads<0>();
-        const int j0 = span.base(u_lo + i, kTileUnit);
+        const int j0 = span.base(u_lo + i, kTileShift);
         const uint8_t *lds = buf ? st1 : st0;
         // whether all rows see all positions (but for bad pages)
         const bool even = j0 + kTileUnit - 1 <= p_first &&
@@ -1036,13 +1120,16 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
                 for (int e = 0; e < 16; ++e) s[m][e] *= scales[buf][0][32 * m + 8 * (e / 4) + 4 * h + e % 4];
         const bool whole = even && !(all_flags & 0x01010101 * kBadPage);
         if (!whole) {
+            // from the lane's first position on, where the others are at constants (as indices of
+            // their own they would be kept in 28 registers)
+            const int at = settled(j0 + 4 * h), last = p - at, first = lower_edge(p, a.list.window) - at;
+            const int sinks = a.list.sinks - at;
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int jj = 32 * m + 8 * (e / 4) + 4 * h + e % 4;
-                    const bool on = visible(j0 + jj, p, a.list.window, a.list.sinks) &&
-                                    !(all_flags & kBadPage << 8 * (jj / 16));
+                    const int c = 32 * m + 8 * (e / 4) + e % 4;
+                    const bool on = c <= last && (c >= first || c < sinks) && !(all_flags & kBadPage << 8 * (c / 16));
                     s[m][e] = on ? s[m][e] : -INFINITY;
                 }
         }
@@ -1223,27 +1310,62 @@ __global__ __launch_bounds__(kThreads, (TileShape<HD, F8, F32>::kPerCu)) void at
         a.split[size_t(tile) * a.G + g] = {row0, tokens * a.GR, 2 * (w * a.G + g) + part,
                                            part < 0 ? 0 : shares.worker_of(tile_hi - 1) - w};
     z += steps;
+    if (whole_tiles && (turn += groups) < tiles) {
+        tile = whole_tile(turn) - 1;
+        z = share_lo = uniform(list.cu[tile + 1]);
+        share_hi = uniform(list.cu[tile + 2]);
+    }
     if (z < share_hi) __syncthreads();   // the stages are free again
     }
 }
 
+template <int HD, bool F8, bool F32>
+__global__ __launch_bounds__(kThreads, (Shape<HD, F8, F32>::kPerCu)) void attend(AttendArgs a) {
+    using S = Shape<HD, F8, F32>;
+    constexpr bool FOUR = S::kTokenStages == 4;
+    __shared__ __align__(1024) uint8_t st0[S::kStage], st1[S::kStage];
+    __shared__ __align__(1024) uint8_t st2[FOUR ? S::kStage : 16], st3[FOUR ? S::kStage : 16];
+    __shared__ __align__(16) float token_scales[kWaves][64];
+    __shared__ __align__(16) TileScratch scratch;
+    __shared__ TileList list;
+    bool one_by_one;
+    const int tiles = build_list(a.list, list, one_by_one);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.tiles = make_int2(tiles, one_by_one);
+    if (tiles == 0) return;
+    const Stages stages{st0, st1, st2, st3};
+    if (one_by_one)
+        attend_token<HD, F8, F32>(a, list, tiles, stages, token_scales);
+    else
+        attend_tile<HD, F8, F32>(a, list, tiles, stages, scratch);
+}
+
 // --------------------------------------------------------------------------------- merge
+struct MergeArgs {         // small: a launch this short waits for its arguments
+    void *out;
+    int64_t out_stride;
+    const Split *split;
+    const int2 *tiles;
+    const float *part_o;
+    const float2 *part_ml;
+    int G, GR;
+};
+
 // Part s of a split tile: the first worker's, then the next ones' first parts (even ones).
 __device__ __forceinline__ size_t part_of(const Split &sp, int G, int s) {
     return s == 0 ? size_t(sp.part) : size_t(sp.part & ~1) + size_t(s) * 2 * G;
 }
 
-// Tiles of one token: grid (tiles * G, GR), a workgroup of N threads per row.  Groups of HD / 4
-// threads take the parts in turn and meet in LDS.
+// Tiles of one token: workgroup (tile * G + g, h) of N threads takes a row.  The parts fall into 4096
+// / HD sums, part s into sum s mod these, each taken by HD / 4 threads; they meet in LDS.  (As many
+// sums whatever N, which goes by T: empty rows of q change no bit of the others.)
 template <int HD, bool F32, int N>
-__global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
-    constexpr int LPR = HD / 4, GROUPS = N / LPR, WAVES = N / kWave;
-    __shared__ float red_m[WAVES], red_d[GROUPS];
-    __shared__ __align__(16) float red[GROUPS][HD];
-    const int t = threadIdx.x, wave = t / kWave, lane = t % kWave, group = t / LPR, at4 = t % LPR;
-    const Split sp = a.split[blockIdx.x];
-    if (int(blockIdx.x) >= a.tiles[0] * a.G || sp.more <= 0) return;
+__device__ __forceinline__ void merge_token(const MergeArgs &a, const Split &sp) {
+    constexpr int LPR = HD / 4, SUMS = 1024 / LPR, WAVES = N / kWave;
+    __shared__ float red_m[WAVES], red_d[SUMS];
+    __shared__ __align__(16) float red[SUMS][HD];
+    const int t = threadIdx.x, wave = t / kWave, lane = t % kWave, at4 = t % LPR;
     const int g = blockIdx.x % a.G, h = blockIdx.y;
+    if (h >= a.GR) return;
     float top = -INFINITY;
     for (int s = t; s <= sp.more; s += N)
         top = fmaxf(top, a.part_ml[part_of(sp, a.G, s) * a.GR + h].x);
@@ -1252,27 +1374,31 @@ __global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < WAVES; ++v) top = fmaxf(top, red_m[v]);
-    float den = 0.f;
-    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int s = group; s <= sp.more; s += GROUPS) {
-        const size_t at = part_of(sp, a.G, s) * a.GR + h;
-        const float2 ml = a.part_ml[at];
-        const float4 o = reinterpret_cast<const float4 *>(a.part_o + at * HD)[at4];
-        const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-        den = fmaf(ml.y, c, den);
-        num.x = fmaf(o.x, c, num.x);
-        num.y = fmaf(o.y, c, num.y);
-        num.z = fmaf(o.z, c, num.z);
-        num.w = fmaf(o.w, c, num.w);
+    const int sums = min(SUMS, sp.more + 1);
+#pragma unroll 1
+    for (int q = t / LPR; q < sums; q += N / LPR) {
+        float den = 0.f;
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4   // (8 take more registers than leave a CU full, which the merge of tiles shares)
+        for (int s = q; s <= sp.more; s += SUMS) {
+            const size_t at = part_of(sp, a.G, s) * a.GR + h;
+            const float2 ml = a.part_ml[at];
+            const float4 o = reinterpret_cast<const float4 *>(a.part_o + at * HD)[at4];
+            const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+            den = fmaf(ml.y, c, den);
+            num.x = fmaf(o.x, c, num.x);
+            num.y = fmaf(o.y, c, num.y);
+            num.z = fmaf(o.z, c, num.z);
+            num.w = fmaf(o.w, c, num.w);
+        }
+        *reinterpret_cast<float4 *>(&red[q][4 * at4]) = num;
+        if (at4 == 0) red_d[q] = den;
     }
-    *reinterpret_cast<float4 *>(&red[group][4 * at4]) = num;
-    if (at4 == 0) red_d[group] = den;
     __syncthreads();
     if (t < HD) {
         float d = 0.f, v = 0.f;
-#pragma unroll
-        for (int q = 0; q < GROUPS; ++q) {
+#pragma unroll 4
+        for (int q = 0; q < sums; ++q) {
             d += red_d[q];
             v += red[q][t];
         }
@@ -1280,13 +1406,13 @@ __global__ __launch_bounds__(N) void merge_tokens(AttendArgs a) {
     }
 }
 
-// Tiles of many rows: grid (tiles * G, y), HD / 4 lanes per row.  Bound by the parts it reads,
-// 64 KB each: 33 MB 11 us behind the launch before; 5 where no tile was split.
+// Tiles of many rows: workgroups (tile * G + g, y) of kThreads at work, HD / 4 lanes per row (more
+// threads on fewer rows' parts: 64 tokens behind 8000 positions 12.9 us instead of 8.6).  Bound by
+// the parts it reads, 64 KB each: 33 MB 10.5 us behind the launch before; 5 where no tile was split.
 template <int HD, bool F32>
-__global__ __launch_bounds__(kThreads) void merge_tiles(AttendArgs a) {
+__device__ __forceinline__ void merge_tile(const MergeArgs &a, const Split &sp) {
     constexpr int LPR = HD / 4, PER = kThreads / LPR;   // rows at a time
-    const Split sp = a.split[blockIdx.x];
-    if (int(blockIdx.x) >= a.tiles[0] * a.G || sp.more <= 0) return;
+    if (threadIdx.x >= kThreads) return;
     const int at4 = threadIdx.x % LPR, g = blockIdx.x % a.G;
     for (int m = blockIdx.y * PER + threadIdx.x / LPR; m < sp.rows; m += gridDim.y * PER) {
         float top = -INFINITY;
@@ -1320,68 +1446,77 @@ __global__ __launch_bounds__(kThreads) void merge_tiles(AttendArgs a) {
     }
 }
 
-// ---------------------------------------------------------------------------------- host
-constexpr int kCus = 256;
+template <int HD, bool F32, int N>
+__global__ __launch_bounds__(N) void merge(MergeArgs a) {
+    const Split sp = a.split[blockIdx.x];
+    const int2 tiles = *a.tiles;
+    // what is needed behind the branch is loaded before it, in one round trip
+    asm volatile("" ::"s"(a.part_o), "s"(a.part_ml), "s"(a.GR), "s"(tiles.x), "s"(tiles.y));
+    if (int(blockIdx.x) >= tiles.x * a.G || sp.more <= 0) return;
+    if (tiles.y)
+        merge_token<HD, F32, N>(a, sp);
+    else
+        merge_tile<HD, F32>(a, sp);
+}
 
-// Which kernel a call takes and what its workspace holds: room for the most workers that a CU
-// may hold, whatever the types.
+// ---------------------------------------------------------------------------------- host
+// What a call's workspace holds, whichever kind of tiles its lengths take: room for the most
+// workers that a CU may hold, whatever the types.
 struct Plan {
-    bool token;
-    int GR, tile_tokens, max_tiles, rows, most_workers;
+    bool tiles;                     // of many rows, perhaps: one row of q has one token
+    bool likely_tokens;             // one by one: no more rows than requests
+    int GR, tile_tokens, max_tiles;
     size_t at_ml, at_o, bytes;
 };
 Plan plan_of(int T, int R, int H, int G, int hd) {
     Plan p;
     p.GR = H / G;
-    // No more rows than requests: single tokens, as a rule; a request that has more of them
-    // is worked on token by token.  31 single tokens, us: 73 by tokens, 76 in tiles; 16 requests of
-    // 2 tokens 28 and 30, 8 of 4 25 and 24; but a chunk among them would be read once a token.
-    p.token = T <= R;
-    p.tile_tokens = p.token ? 1 : kTileRows / p.GR;
-    p.rows = p.token ? p.GR : kTileRows;
-    // the sum of ceil(n / tile_tokens) over min(T, R) requests that have any of T tokens
+    p.tiles = T > 1;
+    p.likely_tokens = T <= R;
+    p.tile_tokens = kTileRows / p.GR;
+    // the sum of ceil(n / tile_tokens) over min(T, R) requests that have any of T tokens; as many
+    // as there are tokens where these are no more than the requests
     p.max_tiles = int(std::min((T + int64_t(p.tile_tokens - 1) * std::min(T, R)) / p.tile_tokens,
                                int64_t(INT_MAX)));
-    p.most_workers = p.token ? kWaves * std::max(1, 2 * kCus / G) : std::max(1, (hd == 128 ? 2 : 3) * kCus / G);
+    const int most = std::max(1, (hd == 128 ? 2 : 3) * kCus / G);   // workgroups that share out a head's units
+    const int token_workers = kWaves * most, workers = p.tiles ? most : 0;
     const auto up = [](size_t v) { return apex::align_up(v, 256); };
-    const size_t parts = 2 * size_t(p.most_workers) * G * p.rows;
+    const size_t rows = 2 * size_t(G) * std::max(size_t(token_workers) * p.GR, size_t(workers) * kTileRows);
     p.at_ml = 256 + up(size_t(std::min(p.max_tiles, kListTiles)) * G * sizeof(Split));
-    p.at_o = p.at_ml + up(parts * sizeof(float2));
-    p.bytes = p.at_o + up(parts * hd * sizeof(float));
+    p.at_o = p.at_ml + up(rows * sizeof(float2));
+    p.bytes = p.at_o + up(rows * hd * sizeof(float));
     return p;
 }
 
 template <int HD, bool F8, bool F32>
 apex_status launch_attention(const Plan &p, hipStream_t st, AttendArgs a) {
-    const int per_cu = p.token ? TokenShape<HD, F8, F32>::kPerCu : TileShape<HD, F8, F32>::kPerCu;
-    a.workers = std::max(1, kCus * per_cu / a.G) * (p.token ? kWaves : 1);
+    using S = Shape<HD, F8, F32>;
+    a.workers = std::max(1, kCus * S::kPerCu / a.G);
+    a.token_workers = a.workers * kWaves;
+    const MergeArgs m{a.out, a.out_stride, a.split, a.tiles, a.part_o, a.part_ml, a.G, a.GR};
     // a launch's units are counted in 32 bits
-    const int unit = p.token ? kTokenUnit : kTileUnit;
-    const int at_once = std::min(kListTiles, INT_MAX / (a.list.room / unit + 2));
+    const int at_once = std::min(kListTiles, INT_MAX / (a.list.room / kTokenUnit + 2));
     for (int f = 0; f < p.max_tiles; f += at_once) {
-        const int tiles = std::min(p.max_tiles - f, at_once);
+        const int tiles = std::min(p.max_tiles - f, at_once), x = tiles * a.G;
         a.list.first_tile = f;
         a.list.most_tiles = tiles;
         // no more workers than there can be shares
-        const int64_t most = int64_t(tiles) * (a.list.room / unit + 1) /
-                                 (p.token ? 1 : kMinShare) + 1;
-        const int workers = int(std::min(int64_t(a.workers), most)), x = tiles * a.G;
-        if (p.token) {
-            hipLaunchKernelGGL((attend_token<HD, F8, F32>), dim3((workers + kWaves - 1) / kWaves * a.G),
-                               dim3(kThreads), 0, st, a);
-            // Few tiles have many parts: 4 requests of up to 131072 positions in 8 groups 4.8 us with 1024
-            // threads, 6.1 with 512; 256 requests' tiles of a few parts each 5.5 with 256, 18.9
-            // with 1024.
-            if (x <= 64)
-                hipLaunchKernelGGL((merge_tokens<HD, F32, 1024>), dim3(x, a.GR), dim3(1024), 0, st, a);
-            else
-                hipLaunchKernelGGL((merge_tokens<HD, F32, 256>), dim3(x, a.GR), dim3(256), 0, st, a);
-        } else {
-            hipLaunchKernelGGL((attend_tile<HD, F8, F32>), dim3(std::max(workers, tiles) * a.G), dim3(kThreads),
-                               0, st, a);
-            hipLaunchKernelGGL((merge_tiles<HD, F32>), dim3(x, std::max(1, std::min(8192 / x, 16))),
-                               dim3(kThreads), 0, st, a);
-        }
+        const auto held = [&](int workers, int64_t units) { return int(std::min(int64_t(workers), tiles * units + 1)); };
+        int groups = (held(a.token_workers, a.list.room / kTokenUnit + 1) + kWaves - 1) / kWaves;
+        if (p.tiles) groups = std::max(groups, held(a.workers, (a.list.room / kTileUnit + 1) / kMinShare + 1));
+        // A workgroup for each tile, so that the GPU hands them out as they end, unless there are
+        // likely to be none (each of them would list the launch's tiles: 1024 single tokens 360 us
+        // instead of 305).
+        if (!p.likely_tokens) groups = std::max(groups, tiles);
+        hipLaunchKernelGGL((attend<HD, F8, F32>), dim3(groups * a.G), dim3(kThreads), 0, st, a);
+        // Few tokens have many parts: 4 requests of up to 131072 positions in 8 groups 4.8 us with 1024
+        // threads, 6.1 with 512; 256 requests' tiles of a few parts each 5.5 with 256, 18.9 with 1024.
+        const int n = p.likely_tokens && x <= 64 ? 1024 : 256, turns = kTileRows / (kThreads / (HD / 4));
+        const dim3 grid(x, std::max(a.GR, p.tiles ? std::min(8192 / x, turns) : 1));
+        if (n == 1024)
+            hipLaunchKernelGGL((merge<HD, F32, 1024>), grid, dim3(1024), 0, st, m);
+        else
+            hipLaunchKernelGGL((merge<HD, F32, 256>), grid, dim3(256), 0, st, m);
         APEX_HIP(hipGetLastError());
     }
     return APEX_OK;
@@ -1459,9 +1594,8 @@ extern "C" apex_status apex_attention_paged(const apex_paged_cache *cache, const
     a.shift = apex::log2_of(page_size);
     a.page_size = page_size;
     a.n_pages = cache->n_pages;
-    a.workers = 1;
     a.scale_log2 = scale * kLog2e;
-    a.tiles = reinterpret_cast<int *>(ws);
+    a.tiles = reinterpret_cast<int2 *>(ws);
     a.split = reinterpret_cast<Split *>(ws + 256);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.at_ml);
     a.part_o = reinterpret_cast<float *>(ws + p.at_o);

@@ -203,6 +203,120 @@ def test_many_tiles_groups_and_parts(torch, R, new, longest, H, G, hd, fmt, dtyp
     print(c.check())
 
 
+def one_by_one(c):
+    """Whether the call's last launch took its tokens one by one (the workspace's second word)."""
+    return bool(c.ws[4:8].view(c.torch.int32)[0])
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("R,new,longest,H,G,hd", MANY, ids=[f"R{c[0]}-{c[2]}-H{c[3]}-G{c[4]}" for c in MANY])
+def test_many_tiles_groups_and_parts_without_padding(torch, R, new, longest, H, G, hd, fmt, dtype):
+    rng = np.random.default_rng(R)
+    n = new(rng, R)
+    lens = [longest if r == 0 else int(x + rng.integers(0, max(longest - x, 1))) for r, x in enumerate(n)]
+    c = Case(torch, lens, n, H, G, hd, 16, fmt, dtype, seed=12)
+    c.check()
+    assert one_by_one(c) == (max(n) == 1)
+
+
+# Requests of few tokens among idle ones: (requests, new tokens of the first `some`, some, longest), H,
+# G, hd, one by one.  The rule's two limits, on either side: tokens as many as requests, contexts
+# read twice; and more tiles than workgroups.
+FEW = [
+    ((40, 2, 20, 300), 8, 2, 128, True), ((39, 2, 20, 300), 8, 2, 128, False),
+    ((40, 3, 10, 300), 8, 2, 128, False), ((300, 3, 100, 90), 32, 16, 128, False),
+    ((300, 3, 100, 90), 32, 16, 64, False), ((1600, 3, 530, 40), 4, 2, 64, False),
+]
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("requests,H,G,hd,kind", FEW, ids=[str(c[0]) + f"-{c[3]}" for c in FEW])
+def test_requests_of_few_tokens_among_idle_ones(torch, requests, H, G, hd, kind, fmt, dtype):
+    R, new, some, longest = requests
+    rng = np.random.default_rng(R)
+    n = np.where(rng.permutation(R) < some, new, 0)
+    lens = [longest if x else 0 for x in n]
+    c = Case(torch, lens, n, H, G, hd, 16, fmt, dtype, seed=24, pad=R - new * some if R > new * some else 0)
+    c.check()
+    assert one_by_one(c) == kind
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 4)])
+def test_rows_without_a_token_change_no_bit(torch, window, sinks, fmt, dtype):
+    """Single tokens and a chunk with and without empty rows behind them (and, not to the bit, among
+    requests that bring nothing)."""
+    for lens, new in (([3000, 90, 1, 400], [1] * 4), ([900], [70])):
+        c = Case(torch, lens, new, 8, 2, 128, 16, fmt, dtype, seed=25)
+        c.check(window, sinks)
+        first = c
+        for pad, idle in ((1, 0), (50, 0), (0, 90), (7, 3)):
+            c = Case(torch, lens + [0] * idle, new + [0] * idle, 8, 2, 128, 16, fmt, dtype, pad=pad, seed=25)
+            assert c.n_pages == first.n_pages and c.cu[len(new)] == len(first.q)
+            c.k, c.v, c.ks, c.vs = first.k, first.v, first.ks, first.vs
+            c.q[:len(first.q)], c.table[:len(lens)] = first.q, first.table
+            c.check(window, sinks)
+            assert one_by_one(c) == (new[0] == 1)
+            assert idle or torch.equal(c.out[:len(first.q)], first.out), (pad, idle)
+
+
+@pytest.mark.parametrize("spread", [0.0, 3.0])
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_padded_single_tokens_have_weights_of_16_bits(torch, fmt, spread):
+    """As test_weights_are_held_to_more_bits_than_the_result, whose bound this is, with empty rows."""
+    for seed in range(4):
+        c = Case(torch, [2, 5, 31], [1] * 3, 8, 2, 128, 16, fmt, "bf16", pad=30, seed=60 + seed)
+        if c.vs is not None:
+            c.vs *= np.exp(c.rng.uniform(-spread, spread, c.vs.shape)).astype(np.float32)
+        c.check()
+        k, v = c.values()
+        want = opaged.attend(c.q, k, v, c.cu, c.lens, c.table, 0, 0, 128 ** -0.5, np.zeros((c.T, 8, 128)))[0][:3]
+        got = c.out.double().cpu().numpy().reshape(c.T, 8, 128)[:3]
+        assert np.linalg.norm(got - want) <= 1.05 * np.linalg.norm(round_bf16(want) - want)
+
+
+def test_a_captured_call_serves_any_lengths(torch):
+    """One graph over 24 rows and 24 requests: single tokens, a chunk, both, none, replayed in turn."""
+    c = Case(torch, [400] * 24, [1] * 24, 8, 2, 128, 16, "fp8", "bf16", seed=26)
+    c.device()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.call(stream=torch.cuda.current_stream().cuda_stream)
+    k, v = c.values()
+    for new in ([1] * 24, [0] * 5 + [24] + [0] * 18, [1] * 8 + [9] + [0] * 8 + [1] * 7, [1] * 4 + [16] + [0] * 19, [0] * 24,
+                [2] * 12 + [0] * 12, [1] * 24):
+        cu = np.concatenate([[0], np.cumsum(new)])
+        lens = c.rng.integers(24, 401, 24)
+        c.dcu.copy_(i32(torch, cu)), c.dseq.copy_(i32(torch, lens))
+        c.out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = c.out.double().cpu().numpy().reshape(24, 8, 128)
+        want, size, peak = opaged.attend(c.q, k, v, cu, lens, c.table, 0, 0, 128 ** -0.5, np.full_like(got, 7.0))
+        compare(got, want, size, peak, 128, "bf16")
+        new = np.array(new)
+        assert one_by_one(c) == ((new * lens).sum() <= 2 * lens[new > 0].sum())
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_as_many_single_tokens_as_there_may_be(torch, pad):
+    """4096 requests of one token each, eight launches over one workspace; a sample against the oracle."""
+    rng = np.random.default_rng(27)
+    n = rng.integers(1, 41, native.MAX_REQUESTS)
+    c = Case(torch, n, [1] * len(n), 16, 2, 64, 16, "bf16", "bf16", pad=pad, seed=27)
+    c.device()
+    c.call()
+    got = c.out.double().cpu().numpy().reshape(c.T, 16, 64)
+    assert one_by_one(c) and (got[len(n):] == 7).all()
+    for r in [0, 1, 511, 512, *rng.integers(0, len(n), 40), len(n) - 1]:
+        want, size, peak = opaged.attend(c.q[r:r + 1], c.k, c.v, [0, 1], n[r:r + 1], c.table[r:r + 1], 0, 0, 0.125,
+                                         np.zeros((1, 16, 64)))
+        compare(got[r:r + 1], want, size, peak, 64, "bf16", norm=False)
+
+
 @pytest.mark.parametrize("fmt,new,pad", [("bf16", 1, 0), ("fp8", 1, 0), ("fp8", 1, 9), ("fp8", 30, 0)])
 @pytest.mark.parametrize("spread", [0.0, 3.0])
 def test_weights_are_held_to_more_bits_than_the_result(torch, fmt, new, pad, spread):

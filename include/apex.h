@@ -412,7 +412,9 @@ typedef enum {
  *   positions        device int32 [T] out, or NULL: -1 behind the last token
  *   free_count_out   device int32 [1] out
  *   status           device int32 [R] out, or NULL: apex_request_status
- * No output may overlap an input or another output (equal pointers are refused).
+ * No output may overlap an input or another output (equal pointers are refused); inputs may.
+ * An invalid request keeps what of its cached positions its row can hold (0 of a negative number) as
+ * its seq_len.
  */
 apex_status apex_paged_plan(const int32_t *cached, const int32_t *n_new, int R, int page_size,
                             int n_pages, int max_blocks, int T, int32_t *free_pages,

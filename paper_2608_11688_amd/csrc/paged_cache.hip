@@ -380,13 +380,14 @@ extern "C" apex_status apex_paged_plan(const int32_t *cached, const int32_t *n_n
     APEX_REQUIRE(free_pages && free_count && cu_new && free_count_out, "%s: NULL pointer", fn);
     APEX_REQUIRE(R == 0 || (cached && n_new && block_table && seq_len), "%s: NULL pointer", fn);
     APEX_REQUIRE(T == 0 || slot_map, "%s: NULL slot_map", fn);
-    const void *all[] = {cached, n_new, free_pages, free_count, block_table, seq_len,
+    // the inputs first: they may be one buffer, an output may be none of the others
+    const void *all[] = {cached, n_new, free_count, free_pages, block_table, seq_len,
                          cu_new, slot_map, positions, free_count_out, status};
-    const int n_all = int(sizeof(all) / sizeof(all[0]));
+    const int n_all = int(sizeof(all) / sizeof(all[0])), n_in = 3;
     for (int i = 0; i < n_all; ++i) {
         APEX_REQUIRE(reinterpret_cast<uintptr_t>(all[i]) % 4 == 0, "%s: misaligned pointer", fn);
-        for (int j = 0; j < i; ++j)
-            APEX_REQUIRE(!all[i] || all[i] != all[j], "%s: two arguments are the same buffer", fn);
+        for (int j = 0; i >= n_in && j < i; ++j)
+            APEX_REQUIRE(!all[i] || all[i] != all[j], "%s: an output is the buffer of another argument", fn);
     }
     const PlanArgs a{cached, n_new, R, page_size, apex::log2_of(page_size), n_pages, max_blocks, T,
                      free_pages, free_count, block_table, seq_len, cu_new, slot_map, positions,

@@ -824,6 +824,25 @@ def test_plan_of_numbers_that_make_no_sense(torch):
         call.check(opaged.plan(cached, n_new, 16, 4, table, 8, free, count))
 
 
+def test_plan_of_inputs_in_one_buffer(torch):
+    """Lengths that are the new tokens as well (each request doubles), and the count of free pages
+    among them."""
+    n = [9, 16, 0, 17, 3]
+    table = np.array([[0, -1, -1], [1, -1, -1], [-1, -1, -1], [2, 3, -1], [4, -1, -1]])
+    free = [5, 6, 7, 8, 9, 10, 11, 12]
+    call = PlanCall(torch, 5, 13, 3, 60)
+    call.table, call.free = i32(torch, table), i32(torch, free + [0] * 5)
+    one = i32(torch, n + [8])
+    native.apex_paged_plan(one, one, 5, 16, 13, 3, 60, call.free, one[5:], call.table, call.seq, call.cu, call.slots,
+                           call.pos, call.count_out, call.status)
+    call.check(opaged.plan(n, n, 16, 13, table, 60, free + [0] * 5, 8))
+    call = PlanCall(torch, 1, 13, 3, 60)                             # all three the same word
+    call.table, call.free, one = i32(torch, [[0, -1, -1]]), i32(torch, list(range(1, 14))), i32(torch, [7])
+    native.apex_paged_plan(one, one, 1, 16, 13, 3, 60, call.free, one, call.table, call.seq, call.cu, call.slots,
+                           call.pos, call.count_out, call.status)
+    call.check(opaged.plan([7], [7], 16, 13, np.array([[0, -1, -1]]), 60, list(range(1, 14)), 7))
+
+
 def test_plan_without_requests_or_rows(torch):
     call = PlanCall(torch, 0, 4, 2, 5)
     free, count = i32(torch, [0, 1, 2, 3]), i32(torch, [3])

@@ -100,6 +100,15 @@ def test_plan_refuses(status, kw):
     refused(status, lambda: plan(**kw))
 
 
+NAMES = ("cached", "n_new", "count", "free", "table", "seq", "cu", "slots", "pos", "count_out", "status")
+
+
+@pytest.mark.parametrize("i,j", [(i, j) for i in range(3, len(NAMES)) for j in range(i)],
+                         ids=lambda x: NAMES[x])
+def test_plan_refuses_an_output_in_place_of_another_argument(i, j):
+    refused(INVAL, lambda: plan(**{NAMES[i]: 64 * A, NAMES[j]: 64 * A}))
+
+
 def test_calls_without_work_do_nothing():
     store(cache(), T=0, k=None, v=None, slots=None)
     attend(cache(), T=0, q=None, out=None, ws=None, n=0)

@@ -462,7 +462,7 @@ apex_status apex_paged_store(const apex_paged_cache *cache, const void *k, const
  *   cu_new, seq_len, block_table [R, max_blocks]   as apex_paged_plan leaves them
  *   T            rows of q and out (at least cu_new[R]), at most APEX_MAX_STEP_TOKENS
  *   H            a multiple of cache->G with H / G <= 16
- *   window, sinks  >= 0;  scale  > 0 and finite (1 / sqrt(hd) as a rule)
+ *   window, sinks  >= 0;  scale  > 0 and below 2.3e38 (1 / sqrt(hd) as a rule)
  *   workspace    device, >= apex_attention_paged_workspace_bytes(T, R, H, G, hd) bytes; must
  *                not be shared by calls that may overlap
  */

@@ -1561,8 +1561,8 @@ extern "C" apex_status apex_attention_paged(const apex_paged_cache *cache, const
         return apex::fail(APEX_E_UNSUPPORTED, "%s: table rows of %d pages of %d positions: 2^31 or more",
                           fn, max_blocks, page_size);
     APEX_REQUIRE(window >= 0 && sinks >= 0, "%s: window=%d and sinks=%d must be >= 0", fn, window, sinks);
-    APEX_REQUIRE(scale > 0.f && scale < INFINITY, "%s: scale=%g must be positive and finite", fn,
-                 double(scale));
+    APEX_REQUIRE(scale > 0.f && scale * kLog2e < INFINITY,   // (what scores are multiplied by)
+                 "%s: scale=%g must be positive and below 2.3e38", fn, double(scale));
     if ((st = apex::check_rows(fn, "q", dtype, q_stride, int64_t(H) * hd)) != APEX_OK) return st;
     if ((st = apex::check_rows(fn, "out", dtype, out_stride, int64_t(H) * hd)) != APEX_OK) return st;
     if (T == 0 || R == 0) return APEX_OK;

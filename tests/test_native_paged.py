@@ -79,6 +79,11 @@ def test_attention_refuses(status, kw):
     refused(status, lambda: attend(cache(), **kw))
 
 
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_scales_whose_powers_of_two_are_infinite(scale):
+    refused(INVAL, lambda: attend(cache(), scale=scale))
+
+
 def plan(**kw):
     names = ("cached", "n_new", "free", "count", "table", "seq", "cu", "slots", "pos", "count_out", "status")
     d = dict(R=3, page=16, n_pages=10, nb=4, T=8, **{n: A * (i + 1) for i, n in enumerate(names)})

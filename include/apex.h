@@ -448,9 +448,9 @@ apex_status apex_paged_store(const apex_paged_cache *cache, const void *k, const
  * nothing, or whose scores are all -infinity, becomes 0.  Whatever keys and values hold at
  * positions a row does not see (NaN included) does not reach it.  An infinite value that it sees
  * makes NaN where its weight is 0 in 32 bits, and may where that is below 2^-76 of the largest.
- * Table entries and pages that no row sees are not read, so
- * pages that left a window may be reused.  Rows before cu_new[0] and from cu_new[R] on are
- * left as they are.
+ * Keys and values of pages that no row sees are not read, so that pages which left a window may be
+ * reused; table entries and E4M3 scales beside those that are seen may be, to no effect.  Rows before
+ * cu_new[0] and from cu_new[R] on are left as they are.
  * Arithmetic: products on the matrix cores, sums, maxima and normalisers in fp32.  dtype
  * APEX_TYPE_BF16: the result is rounded once to bf16, and before it the softmax weights (times the
  * value's scale) for the second product: to 16 bits or more over E4M3 pages and where no request

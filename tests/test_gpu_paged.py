@@ -472,6 +472,27 @@ def test_what_a_row_does_not_see_does_not_reach_it(torch, new, window, sinks, fm
         assert not np.isfinite(got[~clean]).all()
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS, ids=FMT_IDS)
+@pytest.mark.parametrize("new", [1, 70])
+def test_table_entries_that_no_row_sees_have_no_effect(torch, new, fmt, dtype):
+    """Past the last position and under the window: any numbers, page ids of other requests among
+    them."""
+    c = Case(torch, [900, 333 + new], [new, new], 4, 2, 64, 16, fmt, dtype, seed=28)
+    c.check(100, 20)
+    want = c.out.clone()
+    table = c.table.copy()
+    for r in range(2):
+        n, first = int(c.lens[r]), int(c.lens[r]) - new
+        for b in range(c.nb):
+            if b * 16 >= n or (b * 16 >= 20 and b * 16 + 15 <= first - 100):
+                table[r, b] = c.rng.choice([-1, 2 ** 31 - 1, -2 ** 31, c.n_pages, *c.table[1 - r][:9]])
+    assert (table != c.table).sum() > 30
+    c.dtable.copy_(i32(torch, table))
+    c.out.fill_(7.0)
+    c.call(100, 20)
+    assert torch.equal(c.out, want)
+
+
 def test_a_nan_that_is_seen_is_nan(torch):
     c = Case(torch, [50], [1], 2, 1, 64, 16, "bf16", "bf16", seed=5)
     c.v[c.table[0, 1], 0, 3, 7] = np.nan

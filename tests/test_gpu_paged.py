@@ -301,6 +301,22 @@ def test_a_captured_call_serves_any_lengths(torch):
         assert one_by_one(c) == ((new * lens).sum() <= 2 * lens[new > 0].sum())
 
 
+@pytest.mark.parametrize("new", [1, 90])
+def test_as_many_rows_as_there_may_be(torch, new):
+    """All but a few of 2^20 rows empty: the launches behind the first find no tile."""
+    c = Case(torch, [500, 40, 300], [new, 1, new], 2, 1, 64, 16, "bf16", "bf16", seed=29)
+    c.check()
+    want = c.out.clone()
+    live, c.T = c.T, native.MAX_STEP_TOKENS
+    wide = torch.full((c.T, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    wide[:live] = c.dq
+    c.dq, c.out = wide, torch.full_like(wide, 7.0)
+    c.ws = torch.full((native.apex_attention_paged_workspace_bytes(c.T, c.R, 2, 1, 64),), 0xAB, dtype=torch.uint8,
+                      device="cuda")
+    c.call()
+    assert torch.equal(c.out[:live], want) and (c.out[live:] == 7).all()
+
+
 @pytest.mark.parametrize("pad", [0, 3])
 def test_as_many_single_tokens_as_there_may_be(torch, pad):
     """4096 requests of one token each, eight launches over one workspace; a sample against the oracle."""

@@ -876,7 +876,7 @@ __device__ __forceinline__ void attend_token(const AttendArgs &a, TileList &list
 // pieces, 16 bits: the same chunk 1330-1360 us.  One piece, 1090, errs up to 1.8 times as much as the
 // rounding of the result, as alike rows have alike scales; one of fp16, 1140-1160, loses what is 25
 // powers of two below a row's largest product but in its normaliser, and with it outputs that such
-// positions make up.  fp32 in three pieces: 390 TFLOP/s without counting them three times.
+// positions make up.  fp32 in three pieces: 370-380 TFLOP/s without counting them three times.
 constexpr int kTileRows = 128;
 // Units of a share at least: a part is 64 KB.  64 tokens behind 1000 positions, heads of 128: 22.0
 // us with 2 (and with 1), 25.1 with 4, 34.2 with 16; 64 tokens behind 8000: 36.0, with 4 34.0.

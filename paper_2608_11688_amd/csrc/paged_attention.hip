@@ -529,7 +529,7 @@ __device__ __forceinline__ void store_out(void *out, int64_t at, float v) {
 // Bound by the stream of keys and values: 64 tokens under a window of 4096 (1.08 GB) 190 us,
 // 5.65 TB/s, of 5.8 that a kernel that only reads gets.
 constexpr int kMostParts = 512;   // of a launch's tiles, on average: one request of 60000 positions
-                                  // in one group 21 us; in 1024 parts, as many as fit, 24, in 128 28
+                                  // in one group 19.5 us (21 when 1024, as many as fitted, took 24, 128 28)
 constexpr int kTokenShare = 8;    // units: 256 requests of 64 to 256 positions (5 units a share) 50 us with
                                   // all workers, 47 with half; 31 of up to 4096 (12 units) 71.5 and 79.8
 
@@ -575,7 +575,7 @@ __device__ __forceinline__ void attend_token(const AttendArgs &a, TileList &list
     const int w = wg * kWaves + wave;
     const int n = lane & 15, lg = lane >> 4;
     const int all_units = uniform(list.cu[tiles]);
-    // None without a unit; one workgroup a CU where two would have small shares.
+    // None without a unit; half of them where all would have small shares.
     const bool half = S::kTokenStages == 1 && all_units / kTokenShare < a.token_workers;
     const int workers = min(half ? (a.token_workers + 1) / 2 : a.token_workers, min(all_units, kMostParts * tiles));
     if (w >= workers) return;

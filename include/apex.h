@@ -30,9 +30,9 @@
  *    message of the last failing call on the calling thread is apex_last_error().
  *  - Supported sizes: 1 <= E <= 64 experts, 1 <= k <= k_max <= E, d and I multiples
  *    of 8 (16-byte rows of bf16), B >= 0 tokens (B = 0 enqueues nothing).
- *  - apex_prefetch_route, apex_gate_topk, the apex_moe_ffn entry points and the paged-cache
- *    entry points (apex_paged_plan, apex_paged_store, apex_attention_paged) only launch
- *    kernels on the given stream (no allocation, memory set, copy or synchronisation),
+ *  - apex_prefetch_route, apex_gate_topk, the apex_moe_ffn entry points, the paged-cache
+ *    entry points (apex_paged_plan, apex_paged_store, apex_paged_store_rotary,
+ *    apex_attention_paged), apex_rotary and apex_linear_w4 only launch kernels on the given stream (no allocation, memory set, copy or synchronisation),
  *    so a caller may capture them in a HIP graph; apex_moe_ffn_noalloc's first call on
  *    a device looks up that device's scratch array and must come before the capture.
  */
@@ -48,7 +48,7 @@
 extern "C" {
 #endif
 
-#define APEX_ABI_VERSION 5
+#define APEX_ABI_VERSION 6
 #define APEX_MAX_EXPERTS 64
 #define APEX_MAX_PAIRS 1024     /* B * k limit of apex_moe_ffn */
 
@@ -348,6 +348,8 @@ apex_status apex_attention_decode(const float *h, const uint16_t *w_qkv, const u
  * and per layer, behind the projections and rotary positions of the caller,
  *   apex_paged_store      writes the new keys and values into their slots;
  *   apex_attention_paged  attention of the new tokens over their requests' pages.
+ * apex_linear_w4 projects, apex_rotary turns queries and keys by their positions, and
+ * apex_paged_store_rotary does that on the way into the pages.
  * The block is the one of apex_attention_decode (grouped-query attention, query head i uses
  * key/value head i / (H / G)) for requests of any lengths, chunks of several tokens and windows.
  *
@@ -472,6 +474,125 @@ apex_status apex_attention_paged(const apex_paged_cache *cache, const void *q, i
                                  const int32_t *seq_len, const int32_t *block_table, int max_blocks,
                                  int window, int sinks, float scale, void *out, int64_t out_stride,
                                  void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Rotary positions: pair i < dim / 2 of a head's first `dim` values, (a, b), at position p becomes
+ *   amplitude * (a cos(p f_i) - b sin(p f_i),  a sin(p f_i) + b cos(p f_i)),
+ * the values behind them stay as they are.  The pair is
+ *   APEX_ROPE_HALF         values i and i + dim / 2
+ *   APEX_ROPE_INTERLEAVED  values 2 i and 2 i + 1
+ * f_i are radians per position in 64 bits (apex_rotary_frequencies, or a caller's own; negated they
+ * turn back).  Angles are reduced to a fraction of a turn in 64 bits, so that far positions lose
+ * nothing; cosines, sines and products are fp32, the result is rounded once to the rows' type.
+ *   dim        a multiple of 16, at most the head's size
+ *   freq       device double [dim / 2];  amplitude  finite (1 as a rule)
+ * The struct is read during the call only.
+ */
+typedef enum {
+    APEX_ROPE_HALF = 0,
+    APEX_ROPE_INTERLEAVED = 1
+} apex_rope_layout;
+
+typedef struct {
+    int layout;             /* apex_rope_layout */
+    int dim;
+    const double *freq;
+    float amplitude;
+} apex_rotation;
+
+/*
+ * Frequencies f_i = base^(-2 i / dim), i < dim / 2, as `scaling` has them for contexts `factor`
+ * times as long as the `original` one (host only):
+ *   APEX_ROPE_PLAIN   f_i (factor, original, low and high are not looked at)
+ *   APEX_ROPE_LINEAR  f_i / factor: positions interpolated
+ *   APEX_ROPE_BASE    base * factor^(dim / (dim - 2)) in place of base: f_0 stays, the last one is
+ *                     divided by factor
+ *   APEX_ROPE_TURNS   between f_i / factor and f_i, in proportion to where the turns that pair i makes
+ *                     in the original context, n_i = original f_i / (2 pi), stand between low
+ *                     and high:  f_i ((1 - r) / factor + r),  r = (n_i - low) / (high - low) in [0, 1]
+ *   APEX_ROPE_INDEX   the same, r falling with the index: r = 1 - (i - i0) / max(i1 - i0, 0.001) in
+ *                     [0, 1], i0 = max(floor(j(high)), 0), i1 = min(ceil(j(low)), dim - 1), where
+ *                     j(n) = dim ln(original / (2 pi n)) / (2 ln base) is the index that makes n turns
+ *   base > 1;  factor >= 1;  original > 0;  0 < low < high
+ *   freq       host double [dim / 2] out
+ */
+typedef enum {
+    APEX_ROPE_PLAIN = 0,
+    APEX_ROPE_LINEAR = 1,
+    APEX_ROPE_BASE = 2,
+    APEX_ROPE_TURNS = 3,
+    APEX_ROPE_INDEX = 4
+} apex_rope_scaling;
+
+apex_status apex_rotary_frequencies(int dim, double base, int scaling, double factor, double original,
+                                    double low, double high, double *freq);
+
+/*
+ * Rotary positions of T rows of `heads` heads (queries and keys that stand side by side are one row).
+ *   x, out      device, type `dtype` (apex_type): row t's [heads, hd] at x + t * x_stride; strides in
+ *               values, at least heads * hd and multiples of 16 bytes; out may be x (same stride)
+ *   positions   device int32 [T]: a row whose position is negative is left out (its row of out
+ *               stays as it is)
+ *   hd          a multiple of 8, at most 1024
+ */
+apex_status apex_rotary(const apex_rotation *rotation, const void *x, int dtype, int T, int heads, int hd,
+                        int64_t x_stride, const int32_t *positions, void *out, int64_t out_stride,
+                        hipStream_t stream);
+
+/*
+ * apex_paged_store of keys that are turned by their positions on the way, and the queries' turn
+ * beside it: q_out = turned q; turned k and v as they are into their slots.  One pass over a fused
+ * projection's rows.  Turned keys are fp32 until the pool's own rounding (bf16, or E4M3 with the
+ * scale of the turned row), the rest is as in apex_paged_store and apex_rotary.
+ *   q, q_out    device, type `dtype`: row t's [H, hd] at q + t * q_stride; q_out may be q (same
+ *               stride).  H >= 0: with 0, keys and values only, q and q_out may be NULL
+ *   k, v, slot_map   as in apex_paged_store
+ *   positions   device int32 [T]: a token whose position is negative is left out, queries, keys and
+ *               values; one whose slot is outside of the pool has its queries turned, nothing stored
+ */
+apex_status apex_paged_store_rotary(const apex_paged_cache *cache, const apex_rotation *rotation,
+                                    const void *q, const void *k, const void *v, int dtype, int T, int H,
+                                    int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                    const int32_t *slot_map, const int32_t *positions, void *q_out,
+                                    int64_t q_out_stride, hipStream_t stream);
+
+/*
+ * Projection by weights of 4 bits with a scale and a zero point per group:
+ *   y[t, n] = residual[t, n] + bias[n] + sum_k s(n, k / group) (q(n, k) - z(n, k / group)) x[t, k].
+ * Packed weights of [N, K], apex_linear_w4_bytes(N, K, group) = N Kp / 2 + 4 N Kp / group bytes, Kp =
+ * K rounded up to a multiple of 128:
+ *   codes   N rows of Kp / 2 bytes: codes q in 0..15, 64 bytes for every 128 values, in which the
+ *           32-bit word 4 a + j (a, j = 0..3) holds the codes of values 32 j + 8 a + e, e = 0..7,
+ *           at the bits 4 (e / 2) + 16 (e mod 2); 0 behind K
+ *   groups  Kp / group rows of N 32-bit words: bf16 scale s in the upper half, bf16 zero point z in
+ *           the lower (any finite values; 0 for groups behind K)
+ * apex_pack_linear_w4 quantises bf16 weights w [N, K] into that layout (host memory to host memory):
+ * of a group's values and 0, lo and hi are the smallest and the largest; s = bf16((hi - lo) / 15), to
+ * nearest even; z = round(-lo / s) and q = round(v / s) + z, ties to even, each clamped to 0..15.  A
+ * group of zeros, or one so small that s is 0, has s, z and q 0; one with a NaN or an infinity has a
+ * NaN scale.
+ *   K       a multiple of 8, at most 2^20;  N at most 2^24;  group  32, 64 or 128
+ *   x       device, type `x_type` (apex_type): row t's [K] at x + t * x_stride, in values, at least K
+ *           and a multiple of 16 bytes
+ *   bias    device fp32 [N], or NULL
+ *   residual  device, type `y_type`, row t's [N] at residual + t * residual_stride (at least N), or
+ *           NULL; may be y (same stride)
+ *   y       device, type `y_type` out: row t's [N] at y + t * y_stride (at least N)
+ *   T       rows, at most APEX_MAX_STEP_TOKENS
+ *   workspace  device, >= apex_linear_w4_workspace_bytes(T, N, K, group, x_type) bytes (may be NULL where
+ *           that is 0); must not be shared by calls that may overlap
+ * Arithmetic: products on the matrix cores, of the weights and of x as they are (fp32 values go
+ * through in three pieces), sums in fp32, one rounding to y_type; no atomics, deterministic.  A row of
+ * x with a NaN or an infinity has NaN in all of its row of y; the other rows do not see it.  |x| is
+ * to be below 2^115 and what of it stands below 2^-126 may count as 0.
+ */
+size_t apex_linear_w4_bytes(int N, int K, int group);
+apex_status apex_pack_linear_w4(const uint16_t *w, int N, int K, int group, void *out);
+size_t apex_linear_w4_workspace_bytes(int T, int N, int K, int group, int x_type);
+apex_status apex_linear_w4(const void *w, int N, int K, int group, const void *x, int x_type, int T,
+                           int64_t x_stride, const float *bias, const void *residual,
+                           int64_t residual_stride, void *y, int y_type, int64_t y_stride,
+                           void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Cache plan of one layer for one decode step (pure host function, no HIP calls).

@@ -21,6 +21,8 @@ Memory-Efficient Edge MoE Inference) and cites it by section, equation or algori
 Operators of serving that the paper does not define are written from their definitions:
 
 * ``paged``      paged key/value cache: plan of pages and slots, store, attention over pages
+* ``rotary``     rotary positions and their frequencies
+* ``linear_w4``  projection by weights of 4 bits with a scale and a zero point per group
 
 Pins: every function is checked in ``tests/test_oracle_*.py`` against brute force,
 closed forms, library routines on special cases and invariants the paper states.

@@ -2,7 +2,7 @@
 
 * ``libapex.so``       every entry point of include/apex.h: HIP kernels for gfx950 plus
                        the host code around them (hipcc).
-* ``libapex_plan.so``  the host-only part (cache plan, expert packing, errors), built
+* ``libapex_plan.so``  the host-only part (cache plan, packing of weights, rotary frequencies, errors), built
                        with g++ so that it loads and runs on machines without a GPU.
 
 Usage: ``python -m paper_2608_11688_amd.build`` (or ``__graft_entry__.build()``).
@@ -23,10 +23,12 @@ LIB = os.path.join(PKG, "libapex.so")
 PLAN_LIB = os.path.join(PKG, "libapex_plan.so")
 
 HIP_SOURCES = ["errors.cpp", "residency.cpp", "pack_fp8.cpp", "pack_mxfp4.cpp", "pack_fp32.cpp",
-               "decode.cpp", "route_gate.hip", "moe_ffn.cpp", "ffn_b1.hip", "ffn_b1_e4m3.hip",
+               "pack_linear.cpp", "rotary_frequencies.cpp", "decode.cpp", "route_gate.hip", "moe_ffn.cpp", "ffn_b1.hip", "ffn_b1_e4m3.hip",
                "ffn_b1_mxfp4.hip", "ffn_b1_fp32.hip", "ffn_gemm.hip", "ffn_noalloc.hip",
-               "attention.hip", "paged_cache.hip", "paged_attention.hip", "prefetch.hip", "util.hip"]
-HOST_SOURCES = ["errors.cpp", "residency.cpp", "pack_fp8.cpp", "pack_mxfp4.cpp", "pack_fp32.cpp"]
+               "attention.hip", "paged_cache.hip", "paged_attention.hip",
+               "rotary.hip", "linear_w4.hip", "prefetch.hip", "util.hip"]
+HOST_SOURCES = ["errors.cpp", "residency.cpp", "pack_fp8.cpp", "pack_mxfp4.cpp", "pack_fp32.cpp",
+                "pack_linear.cpp", "rotary_frequencies.cpp"]
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
                # keep the compiler from forming packed fp32 instructions

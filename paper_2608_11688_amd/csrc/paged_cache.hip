@@ -9,10 +9,13 @@
 #include "common.h"
 #include "ffn_device.h"
 #include "paged_internal.h"
+#include "paged_store.h"
 
 namespace {
 
 using apex::ffn::kWave;
+using apex::paged::e4m3_row;
+using apex::paged::pack_bf16;
 
 // ---------------------------------------------------------------------------------- plan
 constexpr int kPlanBlocks = 64;   // workgroups at most
@@ -257,46 +260,6 @@ __device__ __forceinline__ void load8(const void *row, int at, float (&x)[8], ui
     }
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    return uint32_t(__builtin_bit_cast(uint16_t, static_cast<__bf16>(lo))) |
-           uint32_t(__builtin_bit_cast(uint16_t, static_cast<__bf16>(hi))) << 16;
-}
-
-// The maximum over the N lanes (8 or 16, aligned) that share a row.
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp(uint32_t v) {
-    return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xf, 0xf, false));
-}
-template <int N>
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
-    v = max(v, dpp<0xb1>(v));                   // quad_perm 1,0,3,2
-    v = max(v, dpp<0x4e>(v));                   // quad_perm 2,3,0,1
-    v = max(v, dpp<0x141>(v));                  // row_half_mirror
-    if (N == 16) v = max(v, dpp<0x140>(v));     // row_mirror
-    return v;
-}
-
-// x / s for the conversion to E4M3, near enough to the quotient that the conversion rounds as the
-// exact quotient would: x * (1 / s) is off by a few units in the last place, which matters only
-// next to a tie (halfway between two codes: of 20 lower bits only the highest set, or an odd
-// multiple of 2^-10 below 2^-6).  There the sign of x - tie * s, exact in one fused
-// multiply-add, tells the side; a tie stays one.
-__device__ __forceinline__ float code_ratio(float x, float s, float inv) {
-    const float q = x * inv;
-    const float a = fabsf(q);
-    float tie;
-    if (a >= 0.015625f) {
-        const uint32_t u = __float_as_uint(q);
-        tie = __uint_as_float((u & 0xfff00000u) | 0x80000u);
-    } else {
-        tie = copysignf((floorf(a * 512.f) + 0.5f) * (1.f / 512.f), q);
-    }
-    if (fabsf(q - tie) > a * 0x1p-20f) return q;
-    const float d = copysignf(1.f, q) * fmaf(-tie, s, x);   // > 0: beyond the tie
-    const int up = d > 0.f ? 1 : d < 0.f ? -1 : 0;
-    return __uint_as_float(__float_as_uint(tie) + up);
-}
-
 // HD / 8 lanes per row of one token and head, 8 values each; keys and values in turn.
 // Bound by memory, each value read and written once: 8192 fp32 rows of 8 heads of 128 into E4M3
 // pools (84 MB moved, a fifth of it written) 16.2-17.2 us, 4.9-5.2 TB/s, where a large copy gets 4.9.
@@ -323,30 +286,11 @@ __global__ __launch_bounds__(kStoreThreads) void paged_store(StoreArgs a) {
                              pack_bf16(x[6], x[7]));
         *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.pages[kv]) + row * HD + at) = raw;
     } else {
-        // magnitudes compare as integers, infinity and NaN above every number
-        uint32_t peak = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) peak = max(peak, __float_as_uint(x[e]) & 0x7fffffffu);
-        peak = lanes_max<LPR>(peak);
-        const bool bad = peak >= 0x7f800000u;
-        const float s = __uint_as_float(peak) / 448.f;
-        uint32_t code[2] = {0u, 0u};
-        if (!bad && s > 0.f) {
-            // tiny rows: both sides of the quotient scaled alike, away from subnormal numbers
-            const float up = s < 0x1p-100f ? 0x1p64f : 1.f, su = s * up, inv = 1.f / su;
-            float q[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                q[e] = fminf(fmaxf(code_ratio(x[e] * up, su, inv), -448.f), 448.f);
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                int c = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * w], q[4 * w + 1], 0, false);
-                code[w] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * w + 2], q[4 * w + 3], c, true));
-            }
-        }
+        uint32_t code[2];
+        const float s = e4m3_row<LPR>(x, code);
         *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.pages[kv]) + row * HD + at) =
             make_uint2(code[0], code[1]);
-        if (at == 0) a.scales[kv][row] = bad ? NAN : s;
+        if (at == 0) a.scales[kv][row] = s;
     }
 }
 

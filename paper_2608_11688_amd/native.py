@@ -26,8 +26,10 @@ MODE_EXACT, MODE_STALL_FREE = 0, 1
 WEIGHTS_BF16, WEIGHTS_FP8_E4M3, WEIGHTS_MXFP4, WEIGHTS_FP32 = 0, 1, 2, 3
 KV_BF16, KV_FP8_E4M3 = 0, 1
 TYPE_FP32, TYPE_BF16 = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_TURNS, ROPE_INDEX = 0, 1, 2, 3, 4
 REQ_SERVED, REQ_ENDED, REQ_WAITS, REQ_INVALID = 0, 1, 2, 3
-ABI_VERSION = 5
+ABI_VERSION = 6
 MAX_EXPERTS = 64
 MAX_PAIRS = 1024
 NOALLOC_WORKSPACE_BYTES = 64 << 20
@@ -81,6 +83,11 @@ class PagedCache(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("format", "G", "hd", "page_size", "n_pages")] + [
         (n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scales", "v_scales")]
 
+
+class Rotation(C.Structure):
+    _fields_ = [("layout", C.c_int), ("dim", C.c_int), ("freq", C.c_void_p), ("amplitude", C.c_float)]
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "apex_abi_version": (C.c_int, []),
@@ -111,6 +118,13 @@ SIGNATURES = {
     "apex_attention_paged_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
     "apex_attention_paged": (I32, [P, P, I32, I32, I32, I32, I64, P, P, P, I32, I32, I32, F32, P,
                                    I64, P, SZ, P]),
+    "apex_rotary_frequencies": (I32, [I32, F64, I32, F64, F64, F64, F64, P]),
+    "apex_rotary": (I32, [P, P, I32, I32, I32, I32, I64, P, P, I64, P]),
+    "apex_paged_store_rotary": (I32, [P, P, P, P, P, I32, I32, I32, I64, I64, I64, P, P, P, I64, P]),
+    "apex_linear_w4_bytes": (SZ, [I32, I32, I32]),
+    "apex_pack_linear_w4": (I32, [P, I32, I32, I32, P]),
+    "apex_linear_w4_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
+    "apex_linear_w4": (I32, [P, I32, I32, I32, P, I32, I32, I64, P, P, I64, P, I32, I64, P, SZ, P]),
     "apex_plan_residency": (I32, [I32, I32, P, P, I32, I32, I64, P, P, P, P, P]),
     "apex_expert_prefetch": (I32, [P, P, I32, I32, SZ, P, P, I32, I32, I64, P, P, P, P, P, P, P,
                                    P, P, P]),
@@ -136,7 +150,8 @@ SIGNATURES = {
 HOST_ONLY = ("apex_abi_version", "apex_last_error", "apex_expert_bytes", "apex_pack_expert",
              "apex_expert_bytes_fp8", "apex_pack_expert_fp8", "apex_expert_bytes_mxfp4",
              "apex_pack_expert_mxfp4", "apex_expert_bytes_fp32", "apex_pack_expert_fp32",
-             "apex_plan_residency")
+             "apex_plan_residency", "apex_rotary_frequencies", "apex_linear_w4_bytes",
+             "apex_pack_linear_w4")
 
 
 def header_functions(path=HEADER):
@@ -374,6 +389,58 @@ def apex_attention_paged(cache, q, dtype, T, R, H, q_stride, cu_new, seq_len, bl
     _call("apex_attention_paged", _ref(cache), ptr(q), _code(TYPES, dtype), T, R, H, q_stride,
           ptr(cu_new), ptr(seq_len), ptr(block_table), max_blocks, window, sinks, scale, ptr(out),
           out_stride, ptr(workspace), workspace_bytes, stream)
+
+
+ROPE_LAYOUTS = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"plain": ROPE_PLAIN, "linear": ROPE_LINEAR, "base": ROPE_BASE, "turns": ROPE_TURNS,
+                 "index": ROPE_INDEX}
+
+
+def rotary(layout, dim, freq, amplitude=1.0):
+    """The apex_rotation of rotary positions.  layout: an APEX_ROPE_* code or "half", "interleaved".
+    Holds the address of the frequencies (device, float64) only: the caller keeps them alive."""
+    return Rotation(_code(ROPE_LAYOUTS, layout), dim, ptr(freq), float(amplitude))
+
+
+def apex_rotary_frequencies(dim, base, scaling, factor, original, low, high, freq, L=None):
+    """freq: host float64 [dim / 2] out.  scaling: an APEX_ROPE_* code or "plain", "linear", "base",
+    "turns", "index"."""
+    _call("apex_rotary_frequencies", dim, base, _code(ROPE_SCALINGS, scaling), factor, original, low, high,
+          ptr(freq), L=L)
+
+
+def apex_rotary(rotation, x, dtype, T, heads, hd, x_stride, positions, out, out_stride, stream=None):
+    """dtype: an APEX_TYPE_* code or "fp32", "bf16"."""
+    _call("apex_rotary", _ref(rotation), ptr(x), _code(TYPES, dtype), T, heads, hd, x_stride, ptr(positions),
+          ptr(out), out_stride, stream)
+
+
+def apex_paged_store_rotary(cache, rotation, q, k, v, dtype, T, H, q_stride, k_stride, v_stride, slot_map,
+                            positions, q_out, q_out_stride, stream=None):
+    """dtype: an APEX_TYPE_* code or "fp32", "bf16"."""
+    _call("apex_paged_store_rotary", _ref(cache), _ref(rotation), ptr(q), ptr(k), ptr(v), _code(TYPES, dtype),
+          T, H, q_stride, k_stride, v_stride, ptr(slot_map), ptr(positions), ptr(q_out), q_out_stride, stream)
+
+
+def apex_linear_w4_bytes(N, K, group, L=None):
+    return (L or lib()).apex_linear_w4_bytes(N, K, group)
+
+
+def apex_pack_linear_w4(w, N, K, group, out, L=None):
+    _call("apex_pack_linear_w4", ptr(w), N, K, group, ptr(out), L=L)
+
+
+def apex_linear_w4_workspace_bytes(T, N, K, group, x_type):
+    """x_type: an APEX_TYPE_* code or "fp32", "bf16"."""
+    return lib().apex_linear_w4_workspace_bytes(T, N, K, group, _code(TYPES, x_type))
+
+
+def apex_linear_w4(w, N, K, group, x, x_type, T, x_stride, bias, residual, residual_stride, y, y_type,
+                   y_stride, workspace, workspace_bytes, stream=None):
+    """x_type, y_type: APEX_TYPE_* codes or "fp32", "bf16"."""
+    _call("apex_linear_w4", ptr(w), N, K, group, ptr(x), _code(TYPES, x_type), T, x_stride, ptr(bias),
+          ptr(residual), residual_stride, ptr(y), _code(TYPES, y_type), y_stride, ptr(workspace),
+          workspace_bytes, stream)
 
 
 def apex_plan_residency(E, Cslots, pf_idx, pf_count, B, k_max, step, expert_of_slot, last_used,

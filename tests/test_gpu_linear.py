@@ -1,0 +1,278 @@
+"""Projection by 4-bit weights against the float64 oracle.
+
+Tolerances.  Per output, with size = sum |s| (32 + q + |z|) |x| (plus |bias| and |residual|): every product is exact
+(5 bits times 8), and a group's two sums of products and the sum over groups are at most P * group + K / 32 + 40 additions
+(P = 3 pieces of fp32 values, else 1), each off by at most 2^-24 of a partial sum that `size` bounds.  A bf16 result adds
+half a step, 2^-8 of it, an fp32 one 2^-24.  That bound is for each output.  Over all outputs the 2-norm of the error is
+much smaller, as roundings are independent and partial sums of the values of mixed signs here grow with the root of their
+number: sums of n terms of rms 24 |x| round with an rms of 2^-24 * 0.4 * 24 |x| sqrt(n) each, sqrt(n / 2) of them like the
+last, which is 1e-6 of the result's sqrt(n) * 4.6 |x| for n = 128, 1.5e-6 with the sum of x as well and at most 2.6e-6 with
+the additions of three pieces: fp32 at most 3e-6, where a lost third piece would leave 7e-6.  bf16 rounds once, with an
+rms of at most 2^-8 / sqrt(3) * 0.72 = 1.63e-3: 2e-3.
+"""
+import numpy as np
+import pytest
+
+from oracle import linear_w4
+from paper_2608_11688_amd import native
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available()
+    native.lib()
+    return t
+
+
+class Case:
+    def __init__(self, torch, T, N, K, group, x="bf16", y="bf16", bias=False, residual=False, seed=0, extra=0):
+        self.torch, self.T, self.N, self.K, self.group, self.x_type, self.y_type = torch, T, N, K, group, x, y
+        rng = np.random.default_rng(seed)
+        groups = linear_w4.padded(K) // group
+        self.q = rng.integers(0, 16, (N, K))
+        self.s = linear_w4.bf16(((rng.random((N, groups)) + 0.5) * 0.05).astype(np.float32))
+        self.z = linear_w4.bf16(rng.integers(5, 11, (N, groups)).astype(np.float32))
+        self.x = self.rounded(rng.standard_normal((T, K)), x)
+        self.b = rng.standard_normal(N).astype(np.float32) if bias else None
+        self.r = self.rounded(rng.standard_normal((T, N)), y) if residual else None
+        self.extra = extra
+
+    @staticmethod
+    def rounded(v, kind):
+        v = v.astype(np.float32)
+        return linear_w4.bf16(v) if kind == "bf16" else v.astype(np.float64)
+
+    def type(self, kind):
+        return self.torch.bfloat16 if kind == "bf16" else self.torch.float32
+
+    def rows(self, v, kind, fill):
+        """On the GPU, with `extra` values of `fill` behind every row."""
+        wide = self.torch.full((v.shape[0], v.shape[1] + self.extra), fill, dtype=self.type(kind), device="cuda")
+        wide[:, :v.shape[1]] = self.torch.from_numpy(np.ascontiguousarray(v)).cuda().to(self.type(kind))
+        return wide
+
+    def device(self):
+        torch = self.torch
+        self.dw = torch.from_numpy(linear_w4.pack(self.q, self.s, self.z)).cuda()
+        assert self.dw.numel() == native.apex_linear_w4_bytes(self.N, self.K, self.group)
+        self.dx = self.rows(self.x, self.x_type, float("nan"))     # what stands between rows is not read
+        self.db = None if self.b is None else torch.from_numpy(self.b).cuda()
+        self.dr = None if self.r is None else self.rows(self.r, self.y_type, 5.0)
+        self.dy = torch.full((self.T, self.N + self.extra), 7.0, dtype=self.type(self.y_type), device="cuda")
+        n = native.apex_linear_w4_workspace_bytes(self.T, self.N, self.K, self.group, self.x_type)
+        self.ws = torch.full((n + 64,), 0xAB, dtype=torch.uint8, device="cuda")
+        return self
+
+    def call(self, stream=None, y=None):
+        y = self.dy if y is None else y
+        native.apex_linear_w4(self.dw, self.N, self.K, self.group, self.dx, self.x_type, self.T, self.dx.stride(0),
+                              self.db, self.dr, self.dr.stride(0) if self.dr is not None else 0, y, self.y_type,
+                              y.stride(0), self.ws, self.ws.numel() - 64, stream)
+
+    def check(self, norm=True):
+        self.device()
+        self.call()
+        self.torch.cuda.synchronize()
+        assert (self.dy[:, self.N:] == 7).all() and (self.ws[-64:] == 0xAB).all()
+        return self.compare(self.dy, norm)
+
+    def compare(self, y, norm=True):
+        got = y[:, :self.N].double().cpu().numpy()
+        with np.errstate(invalid="ignore", over="ignore"):
+            want, size = linear_w4.apply(self.x, self.q, self.s, self.z, self.group, self.b, self.r)
+        return compare(got, want, size, self.group, self.K, self.x_type, self.y_type, norm)
+
+
+def compare(got, want, size, group, K, x_type, y_type, norm=True):
+    bad = ~np.isfinite(want)
+    assert np.array_equal(np.isnan(got), bad)
+    step = 2.0 ** -8 if y_type == "bf16" else 2.0 ** -24
+    adds = (3 if x_type == "fp32" else 1) * group + K / 32 + 40
+    err = np.abs(got - want)
+    bound = size * adds * 2.0 ** -24 + np.abs(want) * step
+    assert (err[~bad] <= bound[~bad]).all(), (err[~bad] - bound[~bad]).max()
+    rel = np.linalg.norm(err[~bad]) / max(np.linalg.norm(want[~bad]), 1e-30)
+    if norm:
+        assert rel <= (2e-3 if y_type == "bf16" else 3e-6), rel
+    return rel
+
+
+TYPES = [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "bf16"), ("fp32", "fp32")]
+TYPE_IDS = ["-".join(t) for t in TYPES]
+
+# T, N, K, group, bias, residual, extra values in a row
+CASES = [
+    (1, 16, 128, 128, False, False, 0), (1, 1, 8, 32, True, True, 0), (1, 17, 40, 32, False, True, 8),
+    (1, 100, 1000, 64, True, False, 16), (1, 2048, 1024, 64, False, False, 0), (1, 33, 4104, 128, True, True, 0),
+    (2, 37, 96, 32, False, False, 0), (3, 50, 264, 128, True, True, 8), (4, 130, 520, 64, False, True, 0),
+    (5, 64, 2048, 32, False, False, 0), (7, 1031, 1416, 32, True, False, 0), (8, 48, 256, 64, False, False, 8),
+    (9, 31, 136, 128, False, True, 0), (15, 65, 384, 64, True, True, 0), (16, 16, 640, 32, False, False, 0),
+    (17, 95, 512, 128, False, True, 8), (31, 129, 360, 64, True, False, 0), (32, 512, 1024, 64, False, True, 0),
+    (33, 63, 128, 32, True, True, 8), (48, 100, 776, 128, False, False, 0), (63, 257, 256, 32, False, False, 0),
+    (64, 64, 1152, 64, True, True, 0), (65, 127, 400, 128, False, False, 8), (100, 300, 512, 64, True, True, 0),
+    (127, 129, 264, 32, False, True, 0), (128, 128, 256, 128, False, False, 0), (129, 255, 640, 64, True, False, 8),
+    (200, 77, 1000, 32, False, False, 0), (256, 256, 384, 128, False, True, 0), (300, 511, 136, 64, True, True, 0),
+    (513, 260, 904, 128, True, True, 8),
+]
+
+
+@pytest.mark.parametrize("x,y", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("T,N,K,group,bias,residual,extra", CASES, ids=[str(c) for c in CASES])
+def test_projection(torch, T, N, K, group, bias, residual, extra, x, y):
+    print(Case(torch, T, N, K, group, x, y, bias, residual, seed=T + N, extra=extra).check(norm=T * N >= 1000))
+
+
+@pytest.mark.parametrize("T", [1, 5, 40, 150])
+@pytest.mark.parametrize("x", ["bf16", "fp32"])
+def test_residual_in_place_and_repeated(torch, T, x):
+    c = Case(torch, T, 200, 520, 32, x, "fp32", True, True, seed=T).device()
+    keep = c.dr.clone()
+    c.call()
+    first = c.dy.clone()
+    c.call(y=c.dr)
+    assert torch.equal(c.dr, first)               # the residual's own rows as the output
+    c.dr.copy_(keep)
+    c.ws.fill_(0xFF)
+    c.call()
+    assert torch.equal(c.dy, first)
+    c.compare(first)
+
+
+@pytest.mark.parametrize("T", [1, 3, 20, 70, 300])
+@pytest.mark.parametrize("x", ["bf16", "fp32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_not_finite(torch, T, x, value):
+    c = Case(torch, T, 70, 264, 64, x, "fp32", seed=T)
+    c.x[T // 2, 77] = value
+    c.device()
+    c.call()
+    got = c.dy.double().cpu().numpy()
+    assert np.isnan(got[T // 2]).all()
+    c.x[T // 2] = 0
+    c.device()
+    c.call()
+    rest = np.arange(T) != T // 2
+    assert np.array_equal(got[rest], c.dy.double().cpu().numpy()[rest])
+    c.compare(c.dy, norm=False)
+
+
+@pytest.mark.parametrize("T", [1, 20, 130])
+def test_scales_of_any_kind(torch, T):
+    c = Case(torch, T, 80, 300 // 8 * 8, 32, "bf16", "fp32", seed=9)
+    c.s[3], c.z[3] = 0.0, 0.0                     # a row of zeros
+    c.s[4, 1] = 0.0
+    c.s[5] *= -1.0
+    c.s[6] = linear_w4.bf16(np.float32(1e-30))
+    c.s[7] = linear_w4.bf16(np.float32(1e30))
+    c.z[8] = linear_w4.bf16(np.float32(-3.625))   # zero points outside of the codes and between them
+    c.z[9] = linear_w4.bf16(np.float32(200.0))
+    c.s[10, 2] = np.nan
+    c.check(norm=False)
+    assert (c.dy[:, 3] == 0).all()
+
+
+@pytest.mark.parametrize("x", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 2, 20, 200])
+def test_values_of_any_size(torch, T, x):
+    c = Case(torch, T, 60, 400, 128, x, "fp32", seed=11)
+    c.x = c.rounded(c.x * 2.0 ** np.random.default_rng(1).integers(-90, 100, c.x.shape), x)
+    c.check(norm=False)
+    c.x[:] = 0
+    c.check(norm=False)
+    assert (c.dy == 0).all()
+
+
+@pytest.mark.parametrize("x", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N", [(1, 3), (2, 40), (70, 20)])
+def test_longest_rows(torch, T, N, x):
+    print(Case(torch, T, N, 1 << 20, 128, x, "fp32", seed=5).check(norm=False))
+
+
+def test_weights_past_32_bit_offsets(torch):
+    N, K, group = 8300, 1 << 20, 128
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n = native.apex_linear_w4_bytes(N, K, group)
+    w = torch.empty(n, dtype=torch.uint8, device="cuda")
+    codes = w[:N * K // 2]
+    for part in codes.split(1 << 30):
+        part.copy_(torch.randint(0, 256, part.shape, dtype=torch.uint8, generator=gen, device="cuda"))
+    words = w[N * K // 2:].view(torch.bfloat16).view(K // group, N, 2)
+    words[..., 0] = 8.0
+    words[..., 1] = 0.01
+    x = torch.randn(2, K, generator=gen, device="cuda").bfloat16()
+    y = torch.zeros(2, N, device="cuda")
+    native.apex_linear_w4(w, N, K, group, x, "bf16", 2, K, None, None, 0, y, "fp32", N, None, 0)
+    rows = [0, 1, 4095, 8191, 8192, N - 1]
+    pick = torch.cat([codes.view(N, -1)[rows].reshape(-1), words[:, rows].contiguous().view(torch.uint8).reshape(-1)])
+    q, s, z = linear_w4.unpack(pick.cpu().numpy(), len(rows), K, group)
+    want, size = linear_w4.apply(x.double().cpu().numpy(), q, s, z, group)
+    compare(y[:, rows].double().cpu().numpy(), want, size, group, K, "bf16", "fp32", norm=False)
+
+
+@pytest.mark.parametrize("x,y", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("T", [1, 6, 33, 140])
+def test_captured_and_replayed(torch, T, x, y):
+    c = Case(torch, T, 150, 392, 64, x, y, True, True, seed=T).device()
+    c.call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            c.call(stream=side.cuda_stream)
+    for i in range(4):
+        c.x = c.rounded(np.random.default_rng(i).standard_normal(c.x.shape), x)
+        c.dx.copy_(c.rows(c.x, x, float("nan")))
+        c.dy.fill_(7.0)
+        c.ws.fill_(i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = c.dy.clone()
+        c.compare(replayed, norm=False)
+        c.call()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, c.dy)
+
+
+def test_two_streams_at_once(torch):
+    a, b = (Case(torch, T, 1000, 2048, 64, "fp32", "fp32", seed=T).device() for T in (1, 90))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.call(streams[0].cuda_stream)
+        b.call(streams[1].cuda_stream)
+    torch.cuda.synchronize()
+    a.compare(a.dy)
+    b.compare(b.dy)
+
+
+def test_a_chunk_agrees_with_its_rows(torch):
+    """Rows alone and in a chunk: other orders of the same sums."""
+    c = Case(torch, 130, 100, 640, 64, "fp32", "fp32", seed=2).device()
+    c.call()
+    c.compare(c.dy)
+    whole = c.dy.clone()
+    for t in (0, 64, 129):
+        one = Case(torch, 1, 100, 640, 64, "fp32", "fp32", seed=2)
+        one.x = c.x[t:t + 1]
+        one.device()
+        one.call()
+        one.compare(one.dy, norm=False)
+        assert torch.allclose(one.dy[0], whole[t], rtol=1e-4, atol=1e-4)
+
+
+def test_packed_by_the_library(torch):
+    rng = np.random.default_rng(8)
+    w = linear_w4.bf16((rng.standard_normal((90, 200)) * 0.05).astype(np.float32))
+    c = Case(torch, 3, 90, 200, 64, "fp32", "fp32", seed=8)
+    c.q, c.s, c.z = linear_w4.quantise(w, 64)
+    c.device()
+    out = np.zeros(native.apex_linear_w4_bytes(90, 200, 64), np.uint8)
+    native.apex_pack_linear_w4((w.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16), 90, 200, 64, out)
+    c.dw = torch.from_numpy(out).cuda()
+    c.call()
+    c.compare(c.dy, norm=False)

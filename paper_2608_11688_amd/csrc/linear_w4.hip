@@ -81,9 +81,10 @@ __device__ __forceinline__ void put(const LinearArgs &a, int64_t t, int n, float
 
 // 8 fp32 values as three rows of bf16 pieces whose sum they are: the upper 8 bits of the value, of
 // what is left, and of what is left then.
-__device__ __forceinline__ void cut(uint4 u, uint4 v, uint4 (&p)[3]) {
-    float f[8] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w),
-                  __uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+__device__ __forceinline__ void cut(const float (&v)[8], uint4 (&p)[3]) {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = v[e];
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
         uint32_t top[8];
@@ -191,7 +192,8 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
             *reinterpret_cast<uint4 *>(to + t * x_pitch) = v[0];
         } else {
             uint4 p[3];
-            cut(v[0], v[1], p);
+            cut({__uint_as_float(v[0].x), __uint_as_float(v[0].y), __uint_as_float(v[0].z), __uint_as_float(v[0].w),
+                 __uint_as_float(v[1].x), __uint_as_float(v[1].y), __uint_as_float(v[1].z), __uint_as_float(v[1].w)}, p);
 #pragma unroll
             for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + (3 * t + j) * x_pitch) = p[j];
         }
@@ -381,20 +383,218 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     }
 }
 
-// Rows of fp32 values as three rows of bf16 pieces whose sum they are, zeros behind K.
-__global__ __launch_bounds__(256) void split_x(const float *x, int64_t stride, int T, int K, int Kp, uint16_t *out) {
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    const int lanes = Kp / 8;
-    const int64_t t = i / lanes;
-    const int k = int(i - t * lanes) * 8;
-    if (t >= T) return;
-    uint4 p[3] = {};
-    if (k < K) {
-        const uint4 *from = reinterpret_cast<const uint4 *>(x + t * stride + k);
-        cut(from[0], from[1], p);
-    }
+// Many rows.  A workgroup of 4 wavefronts takes 32 TT tokens by 32 R rows of the weights, each wavefront
+// half of both, a block of 128 codes of one piece of x at a step.  x goes from memory to LDS
+// directly (two stages, chunks placed as in linear_some), codes to registers, a step ahead; one
+// barrier a step.  The sums of (16 + q) x are per group; the other half, (16 + z) sum x over groups, is
+// a small product of its own, on the matrix cores in fp32, of sums of x that a launch before has
+// made: 4 groups at a time, lane quarter q standing for group 4 m + q.
+#define APEX_LDS __attribute__((address_space(3)))
+constexpr int kManyThreads = 256;
+
+__device__ __forceinline__ void barrier_after_loads() {       // every load of this wavefront has landed
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+struct ManyArgs {
+    LinearArgs a;
+    const float *totals;            // sums of x over groups, [T, blocks * 128 / GROUP]
+    float *parts;                   // sums of a share of K, [splits][T][N]; NULL: one share, y is written
+    int m_tiles, n_tiles, splits, share;      // blocks of a share, a multiple of 4
+};
+
+template <int GROUP, int TT, int R>
+__global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void linear_many(ManyArgs m) {
+    constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, BM = 32 * TT, BN = 32 * R, LOADS = BM / 16;
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[BM * 256], stage1[BM * 256];
+    const LinearArgs &a = m.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    // an eighth of the tiles to each XCD, tokens first
+    const int all = m.m_tiles * m.n_tiles * m.splits, id = (blockIdx.x & 7) * ((all + 7) / 8) + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= (all + 7) / 8 || id >= all) return;
+    const int split = id / (m.m_tiles * m.n_tiles), tile = id - split * (m.m_tiles * m.n_tiles);
+    const int n_tile = tile / m.m_tiles, t0 = (tile - n_tile * m.m_tiles) * BM, n0 = n_tile * BN;
+    const int tw = t0 + (wave & 1) * 16 * TT, nw = n0 + (wave >> 1) * 16 * R;
+    const int first = split * m.share, last = min(first + m.share, a.blocks);
+
+    // row 4 i + quarter of this wavefront's part of the tile, its chunk for place `col`
+    int from[LOADS];
+    const int mine = wave * (BM / 4), rows = min(BM, a.T - t0);
 #pragma unroll
-    for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(out + (int64_t(j) * T + t) * Kp + k) = p[j];
+    for (int i = 0; i < LOADS; ++i) {
+        const int row = mine + 4 * i + quarter;
+        from[i] = min(row, rows - 1) * int(a.x_stride) * 2 + 16 * (col ^ (row & 15));
+    }
+    const int x_bytes = (rows - 1) * int(a.x_stride) * 2 + a.x_cols * 2;
+    const auto load_x = [&](uint8_t *stage, int b, int p) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.x) + p * a.x_piece + t0 * a.x_stride, 0,
+                                                            x_bytes, 0x00027000);
+        const bool tail = (b + 1) * kBlock > a.x_cols;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            int at = from[i] + b * 256;
+            if (tail && b * kBlock + 8 * (col ^ ((mine + 4 * i + quarter) & 15)) >= a.x_cols) at = 0x7ffffff0;   // zeros
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (APEX_LDS void *)(stage + (mine + 4 * i) * 256), 16, at, 0, 0, 0);
+        }
+    };
+    Block<GROUP, R> next;
+    float sum_x[TT];
+    const auto load_w = [&](int b) {
+        next.load(a, nw, b, b < last && nw < a.N, lane);
+    };
+    const int groups = a.blocks * PER;
+    const auto load_totals = [&](int b) {              // of the 4 groups that block b is among
+        const int g = b * PER / 4 * 4 + quarter;
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) {
+            const float *p = m.totals + int64_t(min(tw + 16 * tt + col, a.T - 1)) * groups + min(g, groups - 1);
+            sum_x[tt] = *p;
+        }
+    };
+    floatx4 sum[R][TT] = {};
+    uint32_t kept[R];                                  // words of 4 groups, one a lane quarter
+#pragma unroll
+    for (int r = 0; r < R; ++r) kept[r] = 0;
+
+    const auto step = [&](const uint8_t *stage, uint8_t *other, int b, int p) {
+        barrier_after_loads();
+        const Block<GROUP, R> now = next;
+        const bool ends = p == a.pieces - 1;           // of the block
+        if (!ends)
+            load_x(other, b, p + 1);
+        else if (b + 1 < last)
+            load_x(other, b + 1, 0);
+        if (ends) load_w(b + 1);
+        if (ends) {
+            load_totals(b);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (quarter / PER == b % (4 / PER)) kept[r] = now.word[r];
+        }
+        const uint8_t *at = stage + (wave & 1) * (16 * TT) * 256 + col * 256;
+#pragma unroll
+        for (int g = 0; g < PER; ++g) {
+            bf16x8 x[STEPS][TT];
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+                    x[j][tt] = *reinterpret_cast<const bf16x8 *>(at + tt * 4096 + 16 * ((4 * (g * STEPS + j) + quarter) ^ col));
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                uint32_t words[PER];
+                now.words_of(r, words);
+                const float s = __uint_as_float(words[g] & 0xffff0000u);
+                floatx4 prod[TT] = {};
+#pragma unroll
+                for (int j = 0; j < STEPS; ++j) {
+                    const bf16x8 q = widen(word_of(now.code[r], g * STEPS + j));
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt) prod[tt] = mfma(x[j][tt], q, prod[tt]);
+                }
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[r][tt][i] = fmaf(s, prod[tt][i], sum[r][tt][i]);
+            }
+        }
+        if (ends && (b % (4 / PER) == 4 / PER - 1 || b == last - 1)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const Scale w(kept[r]);
+                const float c = -(w.s * w.z);
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt) sum[r][tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(sum_x[tt], c, sum[r][tt], 0, 0, 0);
+                kept[r] = 0;
+            }
+        }
+    };
+    load_x(stage0, first, 0);
+    next.load(a, nw, first, nw < a.N, lane);
+    int b = first, p = 0;
+    const auto forward = [&] {
+        if (++p == a.pieces) p = 0, ++b;
+    };
+    while (b < last) {
+        step(stage0, stage1, b, p);
+        forward();
+        if (b >= last) break;
+        step(stage1, stage0, b, p);
+        forward();
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                // no load into LDS outlives the workgroup
+
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int n = nw + 16 * r + col;
+        if (n >= a.N) continue;
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t t = tw + 16 * tt + 4 * quarter + i;
+                if (t >= a.T) continue;
+                if (m.parts)
+                    m.parts[(split * int64_t(a.T) + t) * a.N + n] = sum[r][tt][i];
+                else
+                    put(a, t, n, sum[r][tt][i]);
+            }
+    }
+}
+
+// The shares of K of every value of y, in order.
+__global__ __launch_bounds__(256) void join(LinearArgs a, const float *parts, int splits) {
+    const int64_t all = int64_t(a.T) * a.N;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+        float v = parts[i];
+        for (int s = 1; s < splits; ++s) v += parts[s * all + i];
+        const int64_t t = i / a.N;
+        put(a, t, int(i - t * a.N), v);
+    }
+}
+
+// Sums of x over groups of GROUP values, [T, groups], and, of fp32 values (PIECES), their bf16 pieces, three
+// rows of Kp with zeros behind K.  A lane takes 8 values, GROUP / 8 lanes a group.
+template <int GROUP, bool PIECES>
+__global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
+                                              uint16_t *out) {
+    const int lanes = Kp / 8;
+    const int64_t all = int64_t(T) * lanes;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+        const int64_t t = i / lanes;
+        const int k = int(i - t * lanes) * 8;
+        float v[8] = {};
+        if (k < K) {
+            if constexpr (PIECES) {
+                const float *from = static_cast<const float *>(x) + t * stride + k;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = from[e];
+            } else {
+                const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + t * stride + k);
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[2 * e] = __uint_as_float(u[e] << 16);
+                    v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                }
+            }
+        }
+        if constexpr (PIECES) {
+            uint4 p[3];
+            cut(v, p);
+#pragma unroll
+            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(out + (int64_t(j) * T + t) * Kp + k) = p[j];
+        }
+        float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        // 4, 8 or 16 lanes of a group, aligned, all of which are here: Kp is a multiple of 128
+        s += __shfl_xor(s, 1);
+        s += __shfl_xor(s, 2);
+        if constexpr (GROUP >= 64) s += __shfl_xor(s, 4);
+        if constexpr (GROUP >= 128) s += __shfl_xor(s, 8);
+        if (totals && k % GROUP == 0) totals[t * (Kp / GROUP) + k / GROUP] = s;
+    }
 }
 
 bool sizes_ok(int N, int K, int group) { return apex_linear_w4_bytes(N, K, group) != 0; }
@@ -446,13 +646,49 @@ void launch(const LinearArgs &a, bool stage, Rows rows, hipStream_t st) {
 
 bool is_type(int t) { return t == APEX_TYPE_FP32 || t == APEX_TYPE_BF16; }
 
+// How a call is worked on.
+struct Plan {
+    enum { kStaged, kSome, kMany } kind;
+    Rows rows;                       // kStaged
+    int m_tiles, n_tiles, splits, share;     // kMany
+    size_t pieces, totals, parts;    // bytes of the workspace, in this order
+    size_t bytes() const { return pieces + totals + parts; }
+};
+
+constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int kManyTokens = 128, kManyRows = 128;
+
+Plan plan_of(int T, int N, int K, int group, int pieces) {
+    Plan p{};
+    const int Kp = padded(K), blocks = Kp / kBlock;
+    if (stages(T, K, pieces, &p.rows)) {
+        p.kind = Plan::kStaged;
+        return p;
+    }
+    if (pieces == 3) p.pieces = up256(size_t(3) * T * Kp * 2);
+    if (T <= (pieces == 3 ? 16 : 32)) {
+        p.kind = Plan::kSome;
+        return p;
+    }
+    p.kind = Plan::kMany;
+    p.totals = up256(size_t(T) * (Kp / group) * 4);
+    p.m_tiles = (T + kManyTokens - 1) / kManyTokens;
+    p.n_tiles = (N + kManyRows - 1) / kManyRows;
+    // shares of K until two workgroups a CU have work, of 4 blocks or more
+    const int64_t tiles = int64_t(p.m_tiles) * p.n_tiles;
+    const int fours = (blocks + 3) / 4, want = int(std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), fours));
+    p.share = (fours + want - 1) / want * 4;
+    p.splits = (blocks + p.share - 1) / p.share;
+    p.parts = p.splits > 1 ? up256(size_t(p.splits) * T * N * 4) : 0;
+    return p;
+}
+
 }  // namespace
 
 extern "C" size_t apex_linear_w4_workspace_bytes(int T, int N, int K, int group, int x_type) {
-    if (T < 1 || T > APEX_MAX_STEP_TOKENS || !sizes_ok(N, K, group) || x_type != APEX_TYPE_FP32) return 0;
-    Rows rows;
-    if (stages(T, K, 3, &rows)) return 0;
-    return size_t(3) * T * padded(K) * 2;
+    if (T < 1 || T > APEX_MAX_STEP_TOKENS || !sizes_ok(N, K, group) || !is_type(x_type)) return 0;
+    return plan_of(T, N, K, group, x_type == APEX_TYPE_FP32 ? 3 : 1).bytes();
 }
 
 extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, const void *x, int x_type, int T,
@@ -471,37 +707,58 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
     APEX_REQUIRE(y_stride >= N && (!residual || residual_stride >= N), "%s: rows of %d values overlap", fn, N);
     if (T > APEX_MAX_STEP_TOKENS)
         return apex::fail(APEX_E_UNSUPPORTED, "%s: T=%d exceeds %d", fn, T, APEX_MAX_STEP_TOKENS);
+    if (x_stride > (1 << 23))      // offsets in a tile of 128 rows are 32-bit numbers of bytes
+        return apex::fail(APEX_E_UNSUPPORTED, "%s: x_stride=%lld exceeds 2^23", fn, static_cast<long long>(x_stride));
     if (T == 0) return APEX_OK;
     APEX_REQUIRE(w && x && y, "%s: NULL pointer", fn);
     APEX_REQUIRE(apex::aligned16(w) && apex::aligned16(x) && apex::aligned16(y) && apex::aligned16(bias) &&
                      apex::aligned16(residual) && apex::aligned16(workspace),
                  "%s: pointers must be 16-byte aligned", fn);
     APEX_REQUIRE(residual != y || residual_stride == y_stride, "%s: y is the residual with another stride", fn);
-    const size_t need = apex_linear_w4_workspace_bytes(T, N, K, group, x_type);
+    const int Kp = padded(K), pieces = x_type == APEX_TYPE_FP32 ? 3 : 1;
+    const Plan plan = plan_of(T, N, K, group, pieces);
+    const size_t need = plan.bytes();
     APEX_REQUIRE(need == 0 || workspace, "%s: NULL workspace", fn);
     if (workspace_bytes < need)
         return apex::fail(APEX_E_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
-    const int Kp = padded(K), pieces = x_type == APEX_TYPE_FP32 ? 3 : 1;
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
                  static_cast<const uint16_t *>(x), x_stride, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
                  Kp / kBlock, pieces, y_type == APEX_TYPE_FP32};
-    Rows rows;
-    const bool stage = stages(T, K, pieces, &rows);
-    if (!stage && pieces > 1) {
-        uint16_t *out = static_cast<uint16_t *>(workspace);
+    char *ws = static_cast<char *>(workspace);
+    float *totals = reinterpret_cast<float *>(ws + plan.pieces);
+    if (plan.kind != Plan::kStaged && (pieces > 1 || plan.kind == Plan::kMany)) {
+        uint16_t *out = reinterpret_cast<uint16_t *>(ws);
         const int64_t items = int64_t(T) * (Kp / 8);
-        hipLaunchKernelGGL(split_x, dim3(unsigned((items + 255) / 256)), dim3(256), 0, stream,
-                           static_cast<const float *>(x), x_stride, T, K, Kp, out);
+        const dim3 grid(unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)));
+        const auto f = pieces > 1 ? (group == 32 ? survey<32, true> : group == 64 ? survey<64, true> : survey<128, true>)
+                                  : (group == 32 ? survey<32, false> : group == 64 ? survey<64, false> : survey<128, false>);
+        hipLaunchKernelGGL(f, grid, dim3(256), 0, stream, x, x_stride, T, K, Kp, plan.totals ? totals : nullptr, out);
         APEX_HIP(hipGetLastError());
-        a.x = out;
-        a.x_stride = Kp;
-        a.x_piece = int64_t(T) * Kp;
-        a.x_cols = Kp;
+        if (pieces > 1) {
+            a.x = out;
+            a.x_stride = Kp;
+            a.x_piece = int64_t(T) * Kp;
+            a.x_cols = Kp;
+        }
     }
-    group == 32   ? launch<32>(a, stage, rows, stream)
-    : group == 64 ? launch<64>(a, stage, rows, stream)
-                  : launch<128>(a, stage, rows, stream);
+    if (plan.kind == Plan::kMany) {
+        float *parts = plan.splits > 1 ? reinterpret_cast<float *>(ws + plan.pieces + plan.totals) : nullptr;
+        const ManyArgs m{a, totals, parts, plan.m_tiles, plan.n_tiles, plan.splits, plan.share};
+        const int64_t all = int64_t(plan.m_tiles) * plan.n_tiles * plan.splits;
+        const auto f = group == 32 ? linear_many<32, 4, 4> : group == 64 ? linear_many<64, 4, 4> : linear_many<128, 4, 4>;
+        hipLaunchKernelGGL(f, dim3(unsigned((all + 7) / 8 * 8)), dim3(kManyThreads), 0, stream, m);
+        if (parts) {
+            APEX_HIP(hipGetLastError());
+            hipLaunchKernelGGL(join, dim3(unsigned(std::min<int64_t>((int64_t(T) * N + 255) / 256, 4096))), dim3(256), 0,
+                               stream, a, parts, plan.splits);
+        }
+    } else {
+        const bool stage = plan.kind == Plan::kStaged;
+        group == 32   ? launch<32>(a, stage, plan.rows, stream)
+        : group == 64 ? launch<64>(a, stage, plan.rows, stream)
+                      : launch<128>(a, stage, plan.rows, stream);
+    }
     APEX_HIP(hipGetLastError());
     return APEX_OK;
 }

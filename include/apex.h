@@ -572,8 +572,8 @@ apex_status apex_paged_store_rotary(const apex_paged_cache *cache, const apex_ro
  * group of zeros, or one so small that s is 0, has s, z and q 0; one with a NaN or an infinity has a
  * NaN scale.
  *   K       a multiple of 8, at most 2^20;  N at most 2^24;  group  32, 64 or 128
- *   x       device, type `x_type` (apex_type): row t's [K] at x + t * x_stride, in values, at least K,
- *           a multiple of 16 bytes and at most 2^23
+ *   x       device, type `x_type` (apex_type): row t's [K] at x + t * x_stride, in values, at least K
+ *           and a multiple of 16 bytes
  *   bias    device fp32 [N], or NULL
  *   residual  device, type `y_type`, row t's [N] at residual + t * residual_stride (at least N), or
  *           NULL; may be y (same stride)

@@ -24,7 +24,7 @@ struct LinearArgs {
     const uint8_t *codes;
     const uint32_t *words;
     const uint16_t *x;              // bf16, or the pieces of fp32
-    int64_t x_stride, x_piece;      // in values
+    int64_t x_stride, x_block, x_piece;      // in values: of rows, of 128 values along K, of pieces
     int x_cols;                     // values of a row of x that there are (a multiple of 8)
     const float *bias;
     const void *residual;
@@ -33,15 +33,18 @@ struct LinearArgs {
     int N, T, blocks;               // blocks of kBlock codes in a row
     int pieces;                     // of x: 1 (bf16) or 3 (fp32; in memory where !STAGE)
     bool y32;
+    bool fours;                     // rows of y and of the residual begin at multiples of 4 values, and so does N
 };
 
 // Codes 2 i and 2 i + 1 of a word as bf16 pairs 16 + q.
 __device__ __forceinline__ bf16x8 widen(uint32_t w) {
+    uint32_t base = 0x41804180u;
+    asm("" : "+v"(base));       // in a vector register: an instruction takes one scalar operand, the mask
     uint4 b;
-    b.x = ((w << 3) & 0x00780078u) | 0x41804180u;
-    b.y = ((w >> 1) & 0x00780078u) | 0x41804180u;
-    b.z = ((w >> 5) & 0x00780078u) | 0x41804180u;
-    b.w = ((w >> 9) & 0x00780078u) | 0x41804180u;
+    b.x = ((w << 3) & 0x00780078u) | base;
+    b.y = ((w >> 1) & 0x00780078u) | base;
+    b.z = ((w >> 5) & 0x00780078u) | base;
+    b.w = ((w >> 9) & 0x00780078u) | base;
     return __builtin_bit_cast(bf16x8, b);
 }
 
@@ -79,6 +82,52 @@ __device__ __forceinline__ void put(const LinearArgs &a, int64_t t, int n, float
     store_y(a.y32, a.y, t * a.y_stride + n, y);
 }
 
+// A lane's values of row n of the weights and 4 tokens from t on.  Where rows of y begin at multiples of 4 values, 4
+// lanes (n a multiple of 4 in the first) first trade places, so that each has 4 values of one token, side by side.
+template <int CTRL>
+__device__ __forceinline__ float quad(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, floatx4 v) {
+    if (!a.fours) {
+        if (n >= a.N) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t + i < a.T) put(a, t + i, n, v[i]);
+        return;
+    }
+    // lane l of the four, value i -> lane i, value l: by halves (l ^ 2 and i ^ 2), then by ones
+    const int l = threadIdx.x & 3;
+    const float p0 = quad<0x4e>(l & 2 ? v[0] : v[2]), p1 = quad<0x4e>(l & 2 ? v[1] : v[3]);
+    if (l & 2) v[0] = p0, v[1] = p1;
+    else v[2] = p0, v[3] = p1;
+    const float q0 = quad<0xb1>(l & 1 ? v[0] : v[1]), q1 = quad<0xb1>(l & 1 ? v[2] : v[3]);
+    if (l & 1) v[0] = q0, v[2] = q1;
+    else v[1] = q0, v[3] = q1;
+    t += l;
+    n -= l;
+    if (t >= a.T || n >= a.N) return;                  // N is a multiple of 4
+    if (a.bias) {
+        const float4 b = *reinterpret_cast<const float4 *>(a.bias + n);
+        v[0] += b.x, v[1] += b.y, v[2] += b.z, v[3] += b.w;
+    }
+    if (a.y32) {
+        if (a.residual) v += *reinterpret_cast<const floatx4 *>(static_cast<const float *>(a.residual) + t * a.residual_stride + n);
+        *reinterpret_cast<floatx4 *>(static_cast<float *>(a.y) + t * a.y_stride + n) = v;
+    } else {
+        if (a.residual) {
+            const uint2 r = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.residual) + t * a.residual_stride + n);
+            v[0] += __uint_as_float(r.x << 16), v[1] += __uint_as_float(r.x & 0xffff0000u);
+            v[2] += __uint_as_float(r.y << 16), v[3] += __uint_as_float(r.y & 0xffff0000u);
+        }
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = static_cast<__bf16>(v[i]);
+        *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.y) + t * a.y_stride + n) = y;
+    }
+}
+
 // 8 fp32 values as three rows of bf16 pieces whose sum they are: the upper 8 bits of the value, of
 // what is left, and of what is left then.
 __device__ __forceinline__ void cut(const float (&v)[8], uint4 (&p)[3]) {
@@ -114,9 +163,24 @@ struct Walk {
 constexpr int kWaves = 8;
 constexpr int kPad = 64;            // bytes behind a staged row: rows begin 16 banks apart
 
+// The words of a row's PER groups in a block, of which lane quarter q has loaded that of group q mod PER.
+template <int PER>
+__device__ __forceinline__ void words_of(uint32_t word, uint32_t (&w)[PER]) {
+    if constexpr (PER == 1) {
+        w[0] = word;
+    } else if constexpr (PER == 2) {
+        const auto v = __builtin_amdgcn_permlane16_swap(word, word, false, false);
+        w[0] = v[0], w[1] = v[1];
+    } else {
+        const auto h = __builtin_amdgcn_permlane32_swap(word, word, false, false);
+        const auto lo = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+        w[0] = lo[0], w[1] = lo[1], w[2] = hi[0], w[3] = hi[1];
+    }
+}
+
 // The codes and the group words of a block of 16 R rows, D blocks ahead of their use.  Descriptors end
-// with the tile's rows, and are empty for blocks that are not there: such loads move nothing.  A quarter of
-// the wavefront loads the words of one group (of less than 128 codes) and gets the others' from it.
+// with the tile's rows, and are empty for blocks that are not there: such loads move nothing. 
 template <int GROUP, int R>
 struct Block {
     static constexpr int PER = kBlock / GROUP;
@@ -136,19 +200,6 @@ struct Block {
             code[r] = __builtin_bit_cast(
                 uint4, __builtin_amdgcn_raw_buffer_load_b128(codes, (16 * r + col) * pitch + 16 * quarter, 0, 0));
             word[r] = __builtin_amdgcn_raw_buffer_load_b32(words, (quarter % PER * a.N + 16 * r + col) * 4, 0, 0);
-        }
-    }
-    __device__ __forceinline__ void words_of(int r, uint32_t (&w)[PER]) const {
-        if constexpr (PER == 1) {
-            w[0] = word[r];
-        } else if constexpr (PER == 2) {
-            const auto v = __builtin_amdgcn_permlane16_swap(word[r], word[r], false, false);
-            w[0] = v[0], w[1] = v[1];
-        } else {
-            const auto h = __builtin_amdgcn_permlane32_swap(word[r], word[r], false, false);
-            const auto lo = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
-            const auto hi = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
-            w[0] = lo[0], w[1] = lo[1], w[2] = hi[0], w[3] = hi[1];
         }
     }
 };
@@ -238,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
             for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const uint4 *>(staged + b * 256 + 64 * j);
             uint32_t words[R][PER];
 #pragma unroll
-            for (int r = 0; r < R; ++r) next.words_of(r, words[r]);
+            for (int r = 0; r < R; ++r) words_of<PER>(next.word[r], words[r]);
 #pragma unroll
             for (int g = 0; g < PER; ++g) {
                 floatx4 prod[R] = {}, total = {};
@@ -313,7 +364,8 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int t = min(t0 + 4 * (i % (4 * TT)) + quarter, a.T - 1);
-            uint4 v = *reinterpret_cast<const uint4 *>(a.x + i / (4 * TT) * a.x_piece + t * a.x_stride + (there ? k : 0));
+            uint4 v = *reinterpret_cast<const uint4 *>(a.x + i / (4 * TT) * a.x_piece + t * a.x_stride +
+                                                       (there ? b * a.x_block + 8 * col : 0));
             if (!there) v = make_uint4(0u, 0u, 0u, 0u);
             x[i] = v;
         }
@@ -333,7 +385,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
         next.load(a, n0, b + kWaves, b + kWaves < a.blocks, lane);
         uint32_t words[R][PER];
 #pragma unroll
-        for (int r = 0; r < R; ++r) now.words_of(r, words[r]);
+        for (int r = 0; r < R; ++r) words_of<PER>(now.word[r], words[r]);
 #pragma unroll
         for (int g = 0; g < PER; ++g) {
             floatx4 prod[R][TT] = {}, total[TT] = {};
@@ -383,180 +435,267 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     }
 }
 
-// Many rows.  A workgroup of 4 wavefronts takes 32 TT tokens by 32 R rows of the weights, each wavefront
-// half of both, a block of 128 codes of one piece of x at a step.  x goes from memory to LDS
-// directly (two stages, chunks placed as in linear_some), codes to registers, a step ahead; one
-// barrier a step.  The sums of (16 + q) x are per group; the other half, (16 + z) sum x over groups, is
-// a small product of its own, on the matrix cores in fp32, of sums of x that a launch before has
-// made: 4 groups at a time, lane quarter q standing for group 4 m + q.
+// Many rows.  A workgroup of 8 wavefronts takes a tile of 16 TT tokens by 256 rows of the weights, each
+// wavefront all of the tokens by 32 rows, so that no code is widened twice; a step is a block of 128 codes
+// and one piece of x.  x and codes go from memory to LDS directly (chunks of x placed as in
+// linear_some) into three stages, from there to registers a quarter of a step ahead.  The one barrier
+// of a step stands before its last quarter, when all of the stage has been read: the next step's first
+// values are read behind it, and the stage takes the loads of the step after the next two.
+// The sums of (16 + q) x are scaled group by group; the other half, (16 + z) sum x over groups, is a small
+// product of its own at the end, on the matrix cores in fp32, of sums of x that a launch before has made.
+//
+// There is a workgroup a CU.  The last tiles, fewer than that, are cut along K into shares, whose sums go
+// to memory in the order of the lanes and are joined by another launch.
 #define APEX_LDS __attribute__((address_space(3)))
-constexpr int kManyThreads = 256;
-
-__device__ __forceinline__ void barrier_after_loads() {       // every load of this wavefront has landed
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
+constexpr int kManyThreads = 512, kManyRows = 256, kManySlots = 256;
+constexpr int kManyR = 2;                       // tiles of 16 rows of a wavefront
 
 struct ManyArgs {
     LinearArgs a;
-    const float *totals;            // sums of x over groups, [T, blocks * 128 / GROUP]
-    float *parts;                   // sums of a share of K, [splits][T][N]; NULL: one share, y is written
-    int m_tiles, n_tiles, splits, share;      // blocks of a share, a multiple of 4
+    const float *totals;            // sums of x over groups, 4 at a time: [groups / 4][T][4]
+    float *parts;                   // of the tiles that are cut: [tile][split][tile's values]
+    int m_tiles, tiles, whole;      // the first `whole` tiles are not cut
+    int splits, share;              // blocks of a share, a multiple of 4
 };
 
-template <int GROUP, int TT, int R>
+// Keeps the additions where they stand: put off, as they may be for all of a loop's body, they leave the products of
+// every group in registers.
+__device__ __forceinline__ void settle(floatx4 &v) { asm volatile("" : "+v"(v)); }
+
+constexpr int vmcnt_only(int n) { return 0x0f70 | (n & 15) | (n >> 4 << 14); }   // the s_waitcnt operand
+
+// What lane values of the tile stand for: token and row of value i of (r, tt) of a wavefront.
+template <int TT>
+struct Place {
+    int t, n;                       // of i = 0; i counts tokens
+    __device__ __forceinline__ Place(int tile, int m_tiles, int wave, int lane, int r, int tt) {
+        const int n_tile = tile / m_tiles;
+        t = (tile - n_tile * m_tiles) * (16 * TT) + 16 * tt + 4 * (lane >> 4);
+        n = n_tile * kManyRows + wave * (16 * kManyR) + 16 * r + (lane & 15);
+    }
+};
+
+// Of a wavefront of linear_many: the zero points' half of the groups of blocks first .. last - 1 (within the loop, on
+// every fourth block or so, it costs the compiler a second set of registers for the sums), then the results.
+template <int GROUP, int TT>
+__device__ __forceinline__ void finish(const ManyArgs &m, floatx4 (&sum)[kManyR][TT], int lane, int wave, int tile, int rest,
+                                       bool cut_up, int first, int last) {
+    constexpr int PER = kBlock / GROUP, R = kManyR;
+    const LinearArgs &a = m.a;
+    const int col = lane & 15, quarter = lane >> 4;
+    const int n_tile = tile / m.m_tiles, t0 = (tile - n_tile * m.m_tiles) * (16 * TT);
+    const int nw = n_tile * kManyRows + wave * (16 * R);
+    const int g_last = last * PER;
+    constexpr int AHEAD = 4;                           // fours of groups whose values are on their way at once
+    for (int g0 = first * PER; g0 < g_last; g0 += 4 * AHEAD) {
+        float sum_x[AHEAD][TT];
+        uint32_t word[AHEAD][R];
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f) {              // lane quarter q: group g0 + 4 f + q
+            const int g = g0 + 4 * f + quarter;
+            const bool there = g < g_last;
+            const float *from = m.totals + (there ? int64_t(g >> 2) * a.T * 4 + quarter : 0);
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt) sum_x[f][tt] = from[min(t0 + 16 * tt + col, a.T - 1) * 4];
+#pragma unroll
+            for (int r = 0; r < R; ++r) word[f][r] = there ? a.words[int64_t(g) * a.N + min(nw + 16 * r + col, a.N - 1)] : 0u;
+        }
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f) {
+            if (g0 + 4 * f >= g_last) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const Scale of(word[f][r]);
+                const float c = -(of.s * of.z);
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt) sum[r][tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(sum_x[f][tt], c, sum[r][tt], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) {
+            if (cut_up) {
+                floatx4 *to = reinterpret_cast<floatx4 *>(m.parts) + int64_t(rest) * (16 * TT * kManyRows / 4);
+                to[((wave * R + r) * TT + tt) * 64 + lane] = sum[r][tt];
+                continue;
+            }
+            const Place<TT> at(tile, m.m_tiles, wave, lane, r, tt);
+            put_four(a, at.t, at.n, sum[r][tt]);
+        }
+}
+
+template <int GROUP, int TT>
 __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void linear_many(ManyArgs m) {
-    constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, BM = 32 * TT, BN = 32 * R, LOADS = BM / 16;
-    __shared__ __attribute__((aligned(1024))) uint8_t stage0[BM * 256], stage1[BM * 256];
+    constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, BM = 16 * TT, R = kManyR;
+    constexpr int XLOADS = BM / 32, WLOADS = 2;        // of a wavefront a step: 4 rows of x, 16 rows of codes each
+    __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * 256], x1[BM * 256], x2[BM * 256];
+    __shared__ __attribute__((aligned(1024))) uint8_t w0[kManyRows * 64], w1[kManyRows * 64], w2[kManyRows * 64];
     const LinearArgs &a = m.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
-    // an eighth of the tiles to each XCD, tokens first
-    const int all = m.m_tiles * m.n_tiles * m.splits, id = (blockIdx.x & 7) * ((all + 7) / 8) + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= (all + 7) / 8 || id >= all) return;
-    const int split = id / (m.m_tiles * m.n_tiles), tile = id - split * (m.m_tiles * m.n_tiles);
-    const int n_tile = tile / m.m_tiles, t0 = (tile - n_tile * m.m_tiles) * BM, n0 = n_tile * BN;
-    const int tw = t0 + (wave & 1) * 16 * TT, nw = n0 + (wave >> 1) * 16 * R;
-    const int first = split * m.share, last = min(first + m.share, a.blocks);
+    // units, a tile or a share of one, in the order of the launch's rounds; of a round an eighth to each XCD
+    const int units = m.whole + (m.tiles - m.whole) * m.splits;
+    const int round = blockIdx.x / kManySlots, in_round = min(units - round * kManySlots, kManySlots);
+    const int slot = blockIdx.x % kManySlots, per = (in_round + 7) / 8;
+    if ((slot >> 3) >= per || (slot & 7) * per + (slot >> 3) >= in_round) return;
+    const int unit = round * kManySlots + (slot & 7) * per + (slot >> 3);
+    const bool cut_up = unit >= m.whole && m.splits > 1;
+    const int rest = cut_up ? unit - m.whole : 0, split = cut_up ? rest % m.splits : 0;
+    const int tile = cut_up ? m.whole + rest / m.splits : unit;
+    const int n_tile = tile / m.m_tiles, t0 = (tile - n_tile * m.m_tiles) * BM, n0 = n_tile * kManyRows;
+    const int nw = n0 + wave * (16 * R);
+    const int first = split * m.share, last = cut_up ? min(first + m.share, a.blocks) : a.blocks;
 
-    // row 4 i + quarter of this wavefront's part of the tile, its chunk for place `col`
-    int from[LOADS];
-    const int mine = wave * (BM / 4), rows = min(BM, a.T - t0);
+    // x: rows 4 i + quarter of this wavefront's part of the tile, the chunk for place `col`; past T nothing
+    const int mine = wave * (BM / 8), x_bytes = min(BM, a.T - t0) * 256;
+    int from[4];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int row = mine + 4 * i + quarter;
-        from[i] = min(row, rows - 1) * int(a.x_stride) * 2 + 16 * (col ^ (row & 15));
-    }
-    const int x_bytes = (rows - 1) * int(a.x_stride) * 2 + a.x_cols * 2;
-    const auto load_x = [&](uint8_t *stage, int b, int p) {
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.x) + p * a.x_piece + t0 * a.x_stride, 0,
-                                                            x_bytes, 0x00027000);
-        const bool tail = (b + 1) * kBlock > a.x_cols;
+    for (int i = 0; i < 4; ++i) from[i] = (mine + quarter) * 256 + 16 * (col ^ ((mine + 4 * i + quarter) & 15));
+    const int pitch = a.blocks * 64, w_rows = min(kManyRows, a.N - n0);
+    const int from_w = (wave * 32 + (lane >> 2)) * pitch + 16 * (lane & 3);
+    int b_ahead = first, p_ahead = 0;                  // the step whose loads go out
+    // the loads of a step, as many whatever the step: past the last one they move nothing
+    const auto load = [&](uint8_t *x, uint8_t *w) {
+        const int b = b_ahead, p = p_ahead;
+        const bool there = b < last;
+        const auto codes = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t *>(a.codes) + (there ? int64_t(n0) * pitch + b * 64 : 0), 0,
+            there ? (w_rows - 1) * pitch + 64 : 0, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            int at = from[i] + b * 256;
-            if (tail && b * kBlock + 8 * (col ^ ((mine + 4 * i + quarter) & 15)) >= a.x_cols) at = 0x7ffffff0;   // zeros
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (APEX_LDS void *)(stage + (mine + 4 * i) * 256), 16, at, 0, 0, 0);
-        }
-    };
-    Block<GROUP, R> next;
-    float sum_x[TT];
-    const auto load_w = [&](int b) {
-        next.load(a, nw, b, b < last && nw < a.N, lane);
-    };
-    const int groups = a.blocks * PER;
-    const auto load_totals = [&](int b) {              // of the 4 groups that block b is among
-        const int g = b * PER / 4 * 4 + quarter;
+        for (int i = 0; i < WLOADS; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, (APEX_LDS void *)(w + (wave * 32 + 16 * i) * 64), 16,
+                                                     from_w + 16 * i * pitch, 0, 0, 0);
+        const auto xs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint16_t *>(a.x) + (there ? p * a.x_piece + b * a.x_block + t0 * a.x_stride : 0), 0,
+            there ? x_bytes : 0, 0x00027000);
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt) {
-            const float *p = m.totals + int64_t(min(tw + 16 * tt + col, a.T - 1)) * groups + min(g, groups - 1);
-            sum_x[tt] = *p;
-        }
+        for (int i = 0; i < XLOADS; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, (APEX_LDS void *)(x + (mine + 4 * i) * 256), 16, from[i & 3] + i * 1024, 0,
+                                                     0, 0);
+        if (++p_ahead == a.pieces) p_ahead = 0, ++b_ahead;
     };
+    const int n_valid = a.N - nw;                      // rows of this wavefront's that there are, or more
+    const auto load_words = [&](uint32_t (&w)[R], int b) {
+        const bool there = b < last && n_valid > 0;
+        const auto words = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint32_t *>(a.words) + (there ? int64_t(b) * PER * a.N + nw : 0), 0,
+            there ? ((PER - 1) * a.N + min(n_valid, 16 * R)) * 4 : 0, 0x00027000);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            w[r] = __builtin_amdgcn_raw_buffer_load_b32(words, (quarter % PER * a.N + 16 * r + col) * 4, 0, 0);
+    };
+    constexpr int HT = TT / 2;
+    bf16x8 v[2][HT];                                   // of half h of the tokens in v[h]
+    uint4 code_next[R];
+    const auto read_x = [&](const uint8_t *x, int j, int h) {
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+            v[h][i] = *reinterpret_cast<const bf16x8 *>(x + col * 256 + (h * HT + i) * 4096 + 16 * ((4 * j + quarter) ^ col));
+    };
+    const auto read_codes = [&](const uint8_t *w) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            code_next[r] = *reinterpret_cast<const uint4 *>(w + (wave * 32 + 16 * r + col) * 64 + 16 * quarter);
+    };
+
     floatx4 sum[R][TT] = {};
-    uint32_t kept[R];                                  // words of 4 groups, one a lane quarter
+    uint32_t word_next[R];
+    int b = first, p = 0;
+    // one step; its stage, the next step's
+    const auto step = [&](uint8_t *x, uint8_t *w, const uint8_t *x_next, const uint8_t *w_next) {
+        uint4 code[R];
+        uint32_t word[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) kept[r] = 0;
-
-    const auto step = [&](const uint8_t *stage, uint8_t *other, int b, int p) {
-        barrier_after_loads();
-        const Block<GROUP, R> now = next;
-        const bool ends = p == a.pieces - 1;           // of the block
-        if (!ends)
-            load_x(other, b, p + 1);
-        else if (b + 1 < last)
-            load_x(other, b + 1, 0);
-        if (ends) load_w(b + 1);
-        if (ends) {
-            load_totals(b);
+        for (int r = 0; r < R; ++r) code[r] = code_next[r], word[r] = word_next[r];
+        floatx4 prod[R][TT];
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (quarter / PER == b % (4 / PER)) kept[r] = now.word[r];
-        }
-        const uint8_t *at = stage + (wave & 1) * (16 * TT) * 256 + col * 256;
+        for (int j = 0; j < 4; ++j) {
+            bf16x8 q[R];
 #pragma unroll
-        for (int g = 0; g < PER; ++g) {
-            bf16x8 x[STEPS][TT];
+            for (int r = 0; r < R; ++r) q[r] = widen(word_of(code[r], j));
 #pragma unroll
-            for (int j = 0; j < STEPS; ++j)
-#pragma unroll
-                for (int tt = 0; tt < TT; ++tt)
-                    x[j][tt] = *reinterpret_cast<const bf16x8 *>(at + tt * 4096 + 16 * ((4 * (g * STEPS + j) + quarter) ^ col));
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                uint32_t words[PER];
-                now.words_of(r, words);
-                const float s = __uint_as_float(words[g] & 0xffff0000u);
-                floatx4 prod[TT] = {};
-#pragma unroll
-                for (int j = 0; j < STEPS; ++j) {
-                    const bf16x8 q = widen(word_of(now.code[r], g * STEPS + j));
-#pragma unroll
-                    for (int tt = 0; tt < TT; ++tt) prod[tt] = mfma(x[j][tt], q, prod[tt]);
+            for (int h = 0; h < 2; ++h) {
+                if (h == 0) {
+                    read_x(x, j, 1);
+                } else if (j < 3) {
+                    read_x(x, j + 1, 0);
+                } else {
+                    // the next step's loads have landed; those of the one behind it, the last that went
+                    // out, may be on their way
+                    __builtin_amdgcn_s_waitcnt(vmcnt_only(XLOADS + WLOADS));
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    load_words(word_next, p == a.pieces - 1 ? b + 1 : b);
+                    load(x, w);
+                    read_codes(w_next);
+                    read_x(x_next, 0, 0);
                 }
 #pragma unroll
-                for (int tt = 0; tt < TT; ++tt)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[r][tt][i] = fmaf(s, prod[tt][i], sum[r][tt][i]);
+                    for (int i = 0; i < HT; ++i)
+                        prod[r][h * HT + i] = mfma(v[h][i], q[r], j % STEPS == 0 ? floatx4{} : prod[r][h * HT + i]);
+            }
+            if ((j + 1) % STEPS == 0) {                // a group ends
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    uint32_t words[PER];
+                    words_of<PER>(word[r], words);
+                    const float s = __uint_as_float(words[j / STEPS] & 0xffff0000u);
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[r][tt][i] = fmaf(s, prod[r][tt][i], sum[r][tt][i]);
+                        settle(sum[r][tt]);
+                    }
+                }
             }
         }
-        if (ends && (b % (4 / PER) == 4 / PER - 1 || b == last - 1)) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const Scale w(kept[r]);
-                const float c = -(w.s * w.z);
-#pragma unroll
-                for (int tt = 0; tt < TT; ++tt) sum[r][tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(sum_x[tt], c, sum[r][tt], 0, 0, 0);
-                kept[r] = 0;
-            }
-        }
-    };
-    load_x(stage0, first, 0);
-    next.load(a, nw, first, nw < a.N, lane);
-    int b = first, p = 0;
-    const auto forward = [&] {
         if (++p == a.pieces) p = 0, ++b;
     };
-    while (b < last) {
-        step(stage0, stage1, b, p);
-        forward();
-        if (b >= last) break;
-        step(stage1, stage0, b, p);
-        forward();
+    load_words(word_next, first);
+    load(x0, w0);
+    load(x1, w1);
+    load(x2, w2);
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * (XLOADS + WLOADS)));
+    asm volatile("s_barrier" ::: "memory");
+    read_codes(w0);
+    read_x(x0, 0, 0);
+    int left = (last - first) * a.pieces;
+    for (; left >= 3; left -= 3) {
+        step(x0, w0, x1, w1);
+        step(x1, w1, x2, w2);
+        step(x2, w2, x0, w0);
     }
+    if (left >= 1) step(x0, w0, x1, w1);
+    if (left >= 2) step(x1, w1, x2, w2);
     __builtin_amdgcn_s_waitcnt(0x0f70);                // no load into LDS outlives the workgroup
 
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int n = nw + 16 * r + col;
-        if (n >= a.N) continue;
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = tw + 16 * tt + 4 * quarter + i;
-                if (t >= a.T) continue;
-                if (m.parts)
-                    m.parts[(split * int64_t(a.T) + t) * a.N + n] = sum[r][tt][i];
-                else
-                    put(a, t, n, sum[r][tt][i]);
-            }
-    }
+    // what follows starts from a lane number of its own, so that none of its addresses is made, and kept in registers,
+    // before the loop
+    int lane_after = lane;
+    asm volatile("" : "+v"(lane_after));
+    finish<GROUP, TT>(m, sum, lane_after, wave, tile, rest, cut_up, first, last);
 }
 
-// The shares of K of every value of y, in order.
-__global__ __launch_bounds__(256) void join(LinearArgs a, const float *parts, int splits) {
-    const int64_t all = int64_t(a.T) * a.N;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
-        float v = parts[i];
-        for (int s = 1; s < splits; ++s) v += parts[s * all + i];
-        const int64_t t = i / a.N;
-        put(a, t, int(i - t * a.N), v);
-    }
+// The shares of the tiles that were cut, in order.
+template <int TT>
+__global__ __launch_bounds__(256) void join(ManyArgs m) {
+    constexpr int values = 16 * TT * kManyRows / 4, R = kManyR;       // of 4 tokens
+    const int rest = blockIdx.x / (values / 256), e = blockIdx.x % (values / 256) * 256 + threadIdx.x;
+    const floatx4 *from = reinterpret_cast<const floatx4 *>(m.parts) + int64_t(rest) * m.splits * values + e;
+    floatx4 v = from[0];
+    for (int s = 1; s < m.splits; ++s) v += from[int64_t(s) * values];
+    const int lane = e & 63, tt = (e >> 6) % TT, r = (e >> 6) / TT % R, wave = (e >> 6) / TT / R;
+    const Place<TT> at(m.whole + rest, m.m_tiles, wave, lane, r, tt);
+    put_four(m.a, at.t, at.n, v);
 }
 
-// Sums of x over groups of GROUP values, [T, groups], and, of fp32 values (PIECES), their bf16 pieces, three
-// rows of Kp with zeros behind K.  A lane takes 8 values, GROUP / 8 lanes a group.
+// Sums of x over groups of GROUP values, [groups / 4][T][4] (or NULL), and x as bf16 (PIECES: fp32 values as three pieces)
+// in the order in which it is read: [piece][block of 128 values][T][128], zeros behind K.  Rows of x as they are,
+// often a power of two of bytes apart, have the same block of all rows in one channel of the L2: a chunk of 2048 rows
+// through 6144 x 4096 took 146 us instead of #MANY#.  A lane takes 8 values, GROUP / 8 lanes a group.
 template <int GROUP, bool PIECES>
 __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
                                               uint16_t *out) {
@@ -565,35 +704,37 @@ __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
         const int64_t t = i / lanes;
         const int k = int(i - t * lanes) * 8;
+        uint16_t *to = out + (int64_t(k / kBlock) * T + t) * kBlock + k % kBlock;
         float v[8] = {};
-        if (k < K) {
-            if constexpr (PIECES) {
-                const float *from = static_cast<const float *>(x) + t * stride + k;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = from[e];
-            } else {
-                const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + t * stride + k);
-                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[2 * e] = __uint_as_float(u[e] << 16);
-                    v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-                }
-            }
-        }
         if constexpr (PIECES) {
+            if (k < K) {
+                const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(x) + t * stride + k);
+                const float4 f = from[0], g = from[1];
+                v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w, v[4] = g.x, v[5] = g.y, v[6] = g.z, v[7] = g.w;
+            }
             uint4 p[3];
             cut(v, p);
 #pragma unroll
-            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(out + (int64_t(j) * T + t) * Kp + k) = p[j];
+            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + j * int64_t(T) * Kp) = p[j];
+        } else {
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if (k < K) w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + t * stride + k);
+            *reinterpret_cast<uint4 *>(to) = w;
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __uint_as_float(u[e] << 16);
+                v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            }
         }
+        if (!totals) continue;
         float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         // 4, 8 or 16 lanes of a group, aligned, all of which are here: Kp is a multiple of 128
         s += __shfl_xor(s, 1);
         s += __shfl_xor(s, 2);
         if constexpr (GROUP >= 64) s += __shfl_xor(s, 4);
         if constexpr (GROUP >= 128) s += __shfl_xor(s, 8);
-        if (totals && k % GROUP == 0) totals[t * (Kp / GROUP) + k / GROUP] = s;
+        if (k % GROUP == 0) totals[(int64_t(k / GROUP / 4) * T + t) * 4 + k / GROUP % 4] = s;
     }
 }
 
@@ -624,6 +765,20 @@ void launch_some(const LinearArgs &a, hipStream_t st) {
                        dim3(64 * kWaves), 0, st, a);
 }
 
+template <int GROUP, int TT>
+void launch_many(const ManyArgs &m, hipStream_t st) {
+    const int units = m.whole + (m.tiles - m.whole) * m.splits;
+    const int rounds = (units + kManySlots - 1) / kManySlots;
+    hipLaunchKernelGGL((linear_many<GROUP, TT>), dim3(rounds * kManySlots), dim3(kManyThreads), 0, st, m);
+    if (m.splits > 1)
+        hipLaunchKernelGGL(join<TT>, dim3((m.tiles - m.whole) * (16 * TT * kManyRows / 1024)), dim3(256), 0, st, m);
+}
+
+template <int GROUP>
+void launch_many(const ManyArgs &m, int tt, hipStream_t st) {
+    tt == 4 ? launch_many<GROUP, 4>(m, st) : launch_many<GROUP, 8>(m, st);
+}
+
 // Rows of the weights a workgroup takes: 16 while that leaves it a CU of its own, else 32.
 bool narrow(int N) { return N <= 16 * 256; }
 
@@ -650,14 +805,12 @@ bool is_type(int t) { return t == APEX_TYPE_FP32 || t == APEX_TYPE_BF16; }
 struct Plan {
     enum { kStaged, kSome, kMany } kind;
     Rows rows;                       // kStaged
-    int m_tiles, n_tiles, splits, share;     // kMany
+    int tt, m_tiles, tiles, whole, splits, share;     // kMany
     size_t pieces, totals, parts;    // bytes of the workspace, in this order
     size_t bytes() const { return pieces + totals + parts; }
 };
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-
-constexpr int kManyTokens = 128, kManyRows = 128;
 
 Plan plan_of(int T, int N, int K, int group, int pieces) {
     Plan p{};
@@ -666,21 +819,23 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
         p.kind = Plan::kStaged;
         return p;
     }
-    if (pieces == 3) p.pieces = up256(size_t(3) * T * Kp * 2);
-    if (T <= (pieces == 3 ? 16 : 32)) {
-        p.kind = Plan::kSome;
-        return p;
+    p.kind = T <= (pieces == 3 ? 16 : 32) ? Plan::kSome : Plan::kMany;
+    if (pieces == 3 || p.kind == Plan::kMany) p.pieces = up256(size_t(pieces) * T * Kp * 2);
+    if (p.kind == Plan::kSome) return p;
+    p.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
+    p.tt = T <= 64 ? 4 : 8;
+    p.m_tiles = (T + 16 * p.tt - 1) / (16 * p.tt);
+    p.tiles = p.m_tiles * ((N + kManyRows - 1) / kManyRows);
+    p.whole = p.tiles / kManySlots * kManySlots;
+    const int rest = p.tiles - p.whole, fours = (blocks + 3) / 4;
+    p.splits = 1;
+    p.share = fours * 4;
+    if (rest > 0) {
+        const int want = std::min(kManySlots / rest, fours);
+        p.share = (fours + want - 1) / want * 4;
+        p.splits = (blocks + p.share - 1) / p.share;
+        if (p.splits > 1) p.parts = size_t(rest) * p.splits * (16 * p.tt * kManyRows * 4);
     }
-    p.kind = Plan::kMany;
-    p.totals = up256(size_t(T) * (Kp / group) * 4);
-    p.m_tiles = (T + kManyTokens - 1) / kManyTokens;
-    p.n_tiles = (N + kManyRows - 1) / kManyRows;
-    // shares of K until two workgroups a CU have work, of 4 blocks or more
-    const int64_t tiles = int64_t(p.m_tiles) * p.n_tiles;
-    const int fours = (blocks + 3) / 4, want = int(std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), fours));
-    p.share = (fours + want - 1) / want * 4;
-    p.splits = (blocks + p.share - 1) / p.share;
-    p.parts = p.splits > 1 ? up256(size_t(p.splits) * T * N * 4) : 0;
     return p;
 }
 
@@ -707,8 +862,6 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
     APEX_REQUIRE(y_stride >= N && (!residual || residual_stride >= N), "%s: rows of %d values overlap", fn, N);
     if (T > APEX_MAX_STEP_TOKENS)
         return apex::fail(APEX_E_UNSUPPORTED, "%s: T=%d exceeds %d", fn, T, APEX_MAX_STEP_TOKENS);
-    if (x_stride > (1 << 23))      // offsets in a tile of 128 rows are 32-bit numbers of bytes
-        return apex::fail(APEX_E_UNSUPPORTED, "%s: x_stride=%lld exceeds 2^23", fn, static_cast<long long>(x_stride));
     if (T == 0) return APEX_OK;
     APEX_REQUIRE(w && x && y, "%s: NULL pointer", fn);
     APEX_REQUIRE(apex::aligned16(w) && apex::aligned16(x) && apex::aligned16(y) && apex::aligned16(bias) &&
@@ -723,11 +876,12 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         return apex::fail(APEX_E_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
-                 static_cast<const uint16_t *>(x), x_stride, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
-                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32};
+                 static_cast<const uint16_t *>(x), x_stride, kBlock, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
+                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32,
+                 N % 4 == 0 && y_stride % 4 == 0 && (!residual || residual_stride % 4 == 0)};
     char *ws = static_cast<char *>(workspace);
     float *totals = reinterpret_cast<float *>(ws + plan.pieces);
-    if (plan.kind != Plan::kStaged && (pieces > 1 || plan.kind == Plan::kMany)) {
+    if (plan.pieces) {
         uint16_t *out = reinterpret_cast<uint16_t *>(ws);
         const int64_t items = int64_t(T) * (Kp / 8);
         const dim3 grid(unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)));
@@ -735,24 +889,17 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
                                   : (group == 32 ? survey<32, false> : group == 64 ? survey<64, false> : survey<128, false>);
         hipLaunchKernelGGL(f, grid, dim3(256), 0, stream, x, x_stride, T, K, Kp, plan.totals ? totals : nullptr, out);
         APEX_HIP(hipGetLastError());
-        if (pieces > 1) {
-            a.x = out;
-            a.x_stride = Kp;
-            a.x_piece = int64_t(T) * Kp;
-            a.x_cols = Kp;
-        }
+        a.x = out;
+        a.x_stride = kBlock;
+        a.x_block = int64_t(T) * kBlock;
+        a.x_piece = int64_t(T) * Kp;
+        a.x_cols = Kp;
     }
     if (plan.kind == Plan::kMany) {
-        float *parts = plan.splits > 1 ? reinterpret_cast<float *>(ws + plan.pieces + plan.totals) : nullptr;
-        const ManyArgs m{a, totals, parts, plan.m_tiles, plan.n_tiles, plan.splits, plan.share};
-        const int64_t all = int64_t(plan.m_tiles) * plan.n_tiles * plan.splits;
-        const auto f = group == 32 ? linear_many<32, 4, 4> : group == 64 ? linear_many<64, 4, 4> : linear_many<128, 4, 4>;
-        hipLaunchKernelGGL(f, dim3(unsigned((all + 7) / 8 * 8)), dim3(kManyThreads), 0, stream, m);
-        if (parts) {
-            APEX_HIP(hipGetLastError());
-            hipLaunchKernelGGL(join, dim3(unsigned(std::min<int64_t>((int64_t(T) * N + 255) / 256, 4096))), dim3(256), 0,
-                               stream, a, parts, plan.splits);
-        }
+        const ManyArgs m{a, totals, reinterpret_cast<float *>(ws + plan.pieces + plan.totals), plan.m_tiles, plan.tiles,
+                         plan.whole, plan.splits, plan.share};
+        group == 32 ? launch_many<32>(m, plan.tt, stream) : group == 64 ? launch_many<64>(m, plan.tt, stream)
+                                                                        : launch_many<128>(m, plan.tt, stream);
     } else {
         const bool stage = plan.kind == Plan::kStaged;
         group == 32   ? launch<32>(a, stage, plan.rows, stream)

@@ -169,7 +169,7 @@ def project(**kw):
 @pytest.mark.parametrize("status,kw", [
     (INVAL, dict(T=-1)), (UNSUPPORTED, dict(T=native.MAX_STEP_TOKENS + 1)), (INVAL, dict(N=0)), (INVAL, dict(K=252)),
     (INVAL, dict(K=0)), (INVAL, dict(group=48)), (INVAL, dict(xt=2)), (INVAL, dict(yt=-1)), (INVAL, dict(xs=248)),
-    (INVAL, dict(xs=260)), (UNSUPPORTED, dict(xs=(1 << 23) + 8)), (INVAL, dict(xt="fp32", xs=258)), (INVAL, dict(ys=95)), (INVAL, dict(rs=95)),
+    (INVAL, dict(xs=260)), (INVAL, dict(xt="fp32", xs=258)), (INVAL, dict(ys=95)), (INVAL, dict(rs=95)),
     (INVAL, dict(w=None)), (INVAL, dict(x=None)), (INVAL, dict(y=None)), (INVAL, dict(w=A + 8)), (INVAL, dict(x=A + 8)),
     (INVAL, dict(y=A + 8)), (INVAL, dict(bias=A + 4)), (INVAL, dict(r=A + 2)), (INVAL, dict(ws=A + 8)),
     (INVAL, dict(r=2 * A, rs=200)), (INVAL, dict(N=(1 << 24) + 1, ys=1 << 25, rs=1 << 25)),
@@ -190,3 +190,4 @@ def test_linear_workspace():
     assert f(0, 96, 256, 64, "fp32") == 0 and f(4, 96, 250, 64, "fp32") == 0 and f(-1, 96, 256, 64, "bf16") == 0
     for T in (1, 100, 5000):
         assert f(T, 96, 256, 64, "fp32") <= (T + 256) * 256 * 2 * 4 + (1 << 20)
+        assert f(T, 96, 256, 64, "bf16") <= (T + 256) * 256 * 2 * 2 + (1 << 20)

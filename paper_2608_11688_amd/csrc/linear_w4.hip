@@ -555,36 +555,37 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     for (int i = 0; i < 4; ++i) from[i] = (mine + quarter) * 256 + 16 * (col ^ ((mine + 4 * i + quarter) & 15));
     const int pitch = a.blocks * 64, w_rows = min(kManyRows, a.N - n0);
     const int from_w = (wave * 32 + (lane >> 2)) * pitch + 16 * (lane & 3);
-    int b_ahead = first, p_ahead = 0;                  // the step whose loads go out
-    // the loads of a step, as many whatever the step: past the last one they move nothing
+    // the step whose loads go out: how many are left, the next one's piece, x, codes
+    int ahead = (last - first) * a.pieces, p_ahead = 0;
+    const uint16_t *x_ahead = a.x + first * a.x_block + t0 * a.x_stride;
+    const uint8_t *w_ahead = a.codes + int64_t(n0) * pitch + first * 64;
+    // as many loads whatever the step: past the last one they move nothing
     const auto load = [&](uint8_t *x, uint8_t *w) {
-        const int b = b_ahead, p = p_ahead;
-        const bool there = b < last;
-        const auto codes = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint8_t *>(a.codes) + (there ? int64_t(n0) * pitch + b * 64 : 0), 0,
-            there ? (w_rows - 1) * pitch + 64 : 0, 0x00027000);
+        const auto codes = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(w_ahead), 0,
+                                                             ahead > 0 ? (w_rows - 1) * pitch + 64 : 0, 0x00027000);
+        const auto xs = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(x_ahead), 0, ahead > 0 ? x_bytes : 0,
+                                                          0x00027000);
 #pragma unroll
         for (int i = 0; i < WLOADS; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, (APEX_LDS void *)(w + (wave * 32 + 16 * i) * 64), 16,
                                                      from_w + 16 * i * pitch, 0, 0, 0);
-        const auto xs = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint16_t *>(a.x) + (there ? p * a.x_piece + b * a.x_block + t0 * a.x_stride : 0), 0,
-            there ? x_bytes : 0, 0x00027000);
 #pragma unroll
         for (int i = 0; i < XLOADS; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, (APEX_LDS void *)(x + (mine + 4 * i) * 256), 16, from[i & 3] + i * 1024, 0,
                                                      0, 0);
-        if (++p_ahead == a.pieces) p_ahead = 0, ++b_ahead;
+        --ahead;
+        x_ahead += a.x_piece;                          // pieces of a block, and blocks, one behind the other
+        if (++p_ahead == a.pieces) p_ahead = 0, w_ahead += 64;
     };
-    const int n_valid = a.N - nw;                      // rows of this wavefront's that there are, or more
-    const auto load_words = [&](uint32_t (&w)[R], int b) {
-        const bool there = b < last && n_valid > 0;
-        const auto words = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint32_t *>(a.words) + (there ? int64_t(b) * PER * a.N + nw : 0), 0,
-            there ? ((PER - 1) * a.N + min(n_valid, 16 * R)) * 4 : 0, 0x00027000);
+    const int word_bytes = ((PER - 1) * a.N + min(a.N - nw, 16 * R)) * 4;      // of a block's words, this wavefront's rows
+    const uint32_t *words_at = a.words + int64_t(first) * PER * a.N + nw;
+    int words_left = nw < a.N ? last - first : 0;
+    const auto load_words = [&](uint32_t (&to)[R]) {
+        const auto words = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t *>(words_at), 0, words_left > 0 ? word_bytes : 0,
+                                                             0x00027000);
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            w[r] = __builtin_amdgcn_raw_buffer_load_b32(words, (quarter % PER * a.N + 16 * r + col) * 4, 0, 0);
+            to[r] = __builtin_amdgcn_raw_buffer_load_b32(words, (quarter % PER * a.N + 16 * r + col) * 4, 0, 0);
     };
     constexpr int HT = TT / 2;
     bf16x8 v[2][HT];                                   // of half h of the tokens in v[h]
@@ -600,23 +601,35 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
             code_next[r] = *reinterpret_cast<const uint4 *>(w + (wave * 32 + 16 * r + col) * 64 + 16 * quarter);
     };
 
-    floatx4 sum[R][TT] = {};
+    floatx4 sum[R][TT] = {}, prod[R][TT] = {};
     uint32_t word_next[R];
-    int b = first, p = 0;
-    // one step; its stage, the next step's
+    bf16x8 q_next[R];
+    float s_before[R] = {};                            // of the group before, whose second half is still to be added
+    int p = 0;
+    const auto add = [&](int h, int r, float s) {
+#pragma unroll
+        for (int i = h * HT; i < (h + 1) * HT; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[r][i][e] = fmaf(s, prod[r][i][e], sum[r][i][e]);
+            settle(sum[r][i]);
+        }
+    };
+    // One step; its stage, the next step's.  Eight phases: a quarter of the block's codes by half of the tokens.  What the
+    // vector unit does in a phase is for other values than its matrix instructions': the codes of the next
+    // quarter are widened, and a group's sums scaled, half a quarter later.
     const auto step = [&](uint8_t *x, uint8_t *w, const uint8_t *x_next, const uint8_t *w_next) {
         uint4 code[R];
         uint32_t word[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) code[r] = code_next[r], word[r] = word_next[r];
-        floatx4 prod[R][TT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             bf16x8 q[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) q[r] = widen(word_of(code[r], j));
+            for (int r = 0; r < R; ++r) q[r] = q_next[r];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                __builtin_amdgcn_sched_barrier(0);
                 if (h == 0) {
                     read_x(x, j, 1);
                 } else if (j < 3) {
@@ -626,35 +639,37 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
                     // out, may be on their way
                     __builtin_amdgcn_s_waitcnt(vmcnt_only(XLOADS + WLOADS));
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                    load_words(word_next, p == a.pieces - 1 ? b + 1 : b);
-                    load(x, w);
                     read_codes(w_next);
                     read_x(x_next, 0, 0);
+                    if (++p == a.pieces) p = 0, words_at += PER * a.N, --words_left;
+                    load_words(word_next);
+                    load(x, w);
                 }
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
                     for (int i = 0; i < HT; ++i)
                         prod[r][h * HT + i] = mfma(v[h][i], q[r], j % STEPS == 0 ? floatx4{} : prod[r][h * HT + i]);
-            }
-            if ((j + 1) % STEPS == 0) {                // a group ends
+                if (h == 0 && j % STEPS == 0) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    uint32_t words[PER];
-                    words_of<PER>(word[r], words);
-                    const float s = __uint_as_float(words[j / STEPS] & 0xffff0000u);
+                    for (int r = 0; r < R; ++r) add(1, r, s_before[r]);
+                }
+                if (h == 1) {
 #pragma unroll
-                    for (int tt = 0; tt < TT; ++tt) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[r][tt][i] = fmaf(s, prod[r][tt][i], sum[r][tt][i]);
-                        settle(sum[r][tt]);
+                    for (int r = 0; r < R; ++r) {
+                        q_next[r] = widen(j < 3 ? word_of(code[r], j + 1) : code_next[r].x);
+                        if ((j + 1) % STEPS == 0) {    // a group ends
+                            uint32_t words[PER];
+                            words_of<PER>(word[r], words);
+                            s_before[r] = __uint_as_float(words[j / STEPS] & 0xffff0000u);
+                            add(0, r, s_before[r]);
+                        }
                     }
                 }
             }
         }
-        if (++p == a.pieces) p = 0, ++b;
     };
-    load_words(word_next, first);
+    load_words(word_next);
     load(x0, w0);
     load(x1, w1);
     load(x2, w2);
@@ -662,6 +677,8 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     asm volatile("s_barrier" ::: "memory");
     read_codes(w0);
     read_x(x0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r) q_next[r] = widen(code_next[r].x);
     int left = (last - first) * a.pieces;
     for (; left >= 3; left -= 3) {
         step(x0, w0, x1, w1);
@@ -670,6 +687,8 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
     if (left >= 1) step(x0, w0, x1, w1);
     if (left >= 2) step(x1, w1, x2, w2);
+#pragma unroll
+    for (int r = 0; r < R; ++r) add(1, r, s_before[r]);
     __builtin_amdgcn_s_waitcnt(0x0f70);                // no load into LDS outlives the workgroup
 
     // what follows starts from a lane number of its own, so that none of its addresses is made, and kept in registers,
@@ -693,7 +712,7 @@ __global__ __launch_bounds__(256) void join(ManyArgs m) {
 }
 
 // Sums of x over groups of GROUP values, [groups / 4][T][4] (or NULL), and x as bf16 (PIECES: fp32 values as three pieces)
-// in the order in which it is read: [piece][block of 128 values][T][128], zeros behind K.  Rows of x as they are,
+// in the order in which it is read: [block of 128 values][piece][T][128], zeros behind K.  Rows of x as they are,
 // often a power of two of bytes apart, have the same block of all rows in one channel of the L2: a chunk of 2048 rows
 // through 6144 x 4096 took 146 us instead of #MANY#.  A lane takes 8 values, GROUP / 8 lanes a group.
 template <int GROUP, bool PIECES>
@@ -704,7 +723,7 @@ __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
         const int64_t t = i / lanes;
         const int k = int(i - t * lanes) * 8;
-        uint16_t *to = out + (int64_t(k / kBlock) * T + t) * kBlock + k % kBlock;
+        uint16_t *to = out + (int64_t(k / kBlock) * (PIECES ? 3 : 1) * T + t) * kBlock + k % kBlock;
         float v[8] = {};
         if constexpr (PIECES) {
             if (k < K) {
@@ -715,7 +734,7 @@ __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int
             uint4 p[3];
             cut(v, p);
 #pragma unroll
-            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + j * int64_t(T) * Kp) = p[j];
+            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + j * int64_t(T) * kBlock) = p[j];
         } else {
             uint4 w = make_uint4(0u, 0u, 0u, 0u);
             if (k < K) w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + t * stride + k);
@@ -819,7 +838,13 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
         p.kind = Plan::kStaged;
         return p;
     }
-    p.kind = T <= (pieces == 3 ? 16 : 32) ? Plan::kSome : Plan::kMany;
+    // linear_some reads the weights once for every tile of tokens, linear_many is three launches.  us, some and many:
+    // bf16 rows through 4096 x 4096 (17 million codes), 32: 7.9 and 18.8, 128: 19.8 and 29.2, 192: 26.4 and 28.8; through
+    // 16384 x 4096, 32: 16 and 22, 48: 28.6 and 23.2; through 512 x 2048, 192: 5.9 and 20; fp32 rows through 4096 x 4096,
+    // 32: 18.5 and 26.2, 48: 26.0 and 27.2, 64: 33.0 and 28.2; through 4096 x 14336, 16: 26.7 and 36.0, 24: 47.1 and 36.5.
+    const int tokens = pieces == 3 ? 16 : 32;          // of a tile of linear_some
+    const int64_t reads = int64_t((T + tokens - 1) / tokens) * N * K;
+    p.kind = T <= tokens || reads <= (pieces == 3 ? 50000000 : 110000000) ? Plan::kSome : Plan::kMany;
     if (pieces == 3 || p.kind == Plan::kMany) p.pieces = up256(size_t(pieces) * T * Kp * 2);
     if (p.kind == Plan::kSome) return p;
     p.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
@@ -891,8 +916,8 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         APEX_HIP(hipGetLastError());
         a.x = out;
         a.x_stride = kBlock;
-        a.x_block = int64_t(T) * kBlock;
-        a.x_piece = int64_t(T) * Kp;
+        a.x_piece = int64_t(T) * kBlock;
+        a.x_block = pieces * a.x_piece;
         a.x_cols = Kp;
     }
     if (plan.kind == Plan::kMany) {

@@ -125,6 +125,112 @@ def test_projection(torch, T, N, K, group, bias, residual, extra, x, y):
     print(Case(torch, T, N, K, group, x, y, bias, residual, seed=T + N, extra=extra).check(norm=T * N >= 1000))
 
 
+class Large:
+    """Sizes of the product in tiles, its reference in float64 on the GPU."""
+
+    def __init__(self, torch, T, N, K, group, x, y, bias=False, residual=False, extra=0, seed=0):
+        self.torch, self.T, self.N, self.K, self.group, self.x_type, self.y_type = torch, T, N, K, group, x, y
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        types = {"bf16": torch.bfloat16, "fp32": torch.float32}
+        n = native.apex_linear_w4_bytes(N, K, group)
+        Kp = linear_w4.padded(K)
+        self.w = torch.randint(0, 256, (n,), dtype=torch.uint8, generator=gen, device="cuda")
+        words = self.w[N * Kp // 2:].view(torch.bfloat16).view(Kp // group, N, 2)
+        words[..., 0] = torch.randint(5, 11, words.shape[:2], generator=gen, device="cuda").bfloat16()
+        words[..., 1] = (torch.rand(words.shape[:2], generator=gen, device="cuda") * 0.05 + 0.02).bfloat16()
+        self.x = torch.full((T, K + extra), float("nan"), dtype=types[x], device="cuda")
+        self.x[:, :K] = torch.randn(T, K, generator=gen, device="cuda")
+        self.b = torch.randn(N, generator=gen, device="cuda") if bias else None
+        self.r = torch.randn(T, N + extra, generator=gen, device="cuda").to(types[y]) if residual else None
+        self.y = torch.full((T, N + extra), 7.0, dtype=types[y], device="cuda")
+        need = native.apex_linear_w4_workspace_bytes(T, N, K, group, x)
+        assert need > 2 * T * Kp                       # x in the order of the tiles, and more
+        self.ws = torch.full((need + 64,), 0xAB, dtype=torch.uint8, device="cuda")
+
+    def call(self, stream=None):
+        native.apex_linear_w4(self.w, self.N, self.K, self.group, self.x, self.x_type, self.T, self.x.stride(0), self.b, self.r,
+                              self.r.stride(0) if self.r is not None else 0, self.y, self.y_type, self.y.stride(0), self.ws,
+                              self.ws.numel() - 64, stream)
+
+    def reference(self):
+        torch, N, K, Kp = self.torch, self.N, self.K, linear_w4.padded(self.K)
+        code = self.w[:N * Kp // 2].view(torch.int32).view(N, Kp // 128, 4, 4)      # [row, block, a, j]
+        q = torch.stack([code >> (4 * (e // 2) + 16 * (e % 2)) & 15 for e in range(8)], -1)
+        q = q.transpose(2, 3).reshape(N, Kp)[:, :K].double()
+        words = self.w[N * Kp // 2:].view(torch.bfloat16).view(Kp // self.group, N, 2).double()
+        z, s = (words[..., i].t().repeat_interleave(self.group, 1)[:, :K] for i in (0, 1))
+        x = self.x[:, :K].double()
+        want = x @ (s * (q - z)).t().contiguous()
+        size = x.abs() @ (s.abs() * (32 + q + z.abs())).t().contiguous()
+        for extra in (self.b, self.r[:, :N] if self.r is not None else None):
+            if extra is not None:
+                want, size = want + extra.double(), size + extra.double().abs()
+        return want.cpu().numpy(), size.cpu().numpy()
+
+    def check(self):
+        self.call()
+        self.torch.cuda.synchronize()
+        assert (self.y[:, self.N:] == 7).all() and (self.ws[-64:] == 0xAB).all()
+        want, size = self.reference()
+        return compare(self.y[:, :self.N].double().cpu().numpy(), want, size, self.group, self.K, self.x_type, self.y_type)
+
+
+# T, N, K, group, types of x and y, bias, residual, extra values in a row
+LARGE = [
+    (33, 7000, 8136, 128, "bf16", "bf16", False, False, 0), (64, 14337, 4096, 32, "bf16", "fp32", True, True, 8),
+    (63, 9000, 6912, 64, "bf16", "bf16", True, False, 16), (65, 4999, 7688, 32, "bf16", "bf16", False, True, 0),
+    (17, 5000, 5400, 64, "fp32", "fp32", False, True, 0), (48, 3333, 6016, 128, "fp32", "bf16", True, False, 8),
+    (100, 2052, 3840, 32, "fp32", "fp32", True, True, 0), (129, 3001, 7936, 128, "bf16", "fp32", False, False, 0),
+    (300, 2816, 4104, 64, "bf16", "bf16", True, True, 8), (513, 5121, 1416, 128, "bf16", "bf16", False, True, 0),
+    (2050, 4100, 520, 32, "bf16", "fp32", False, False, 0),       # more tiles than a round, shares behind it
+    (2048, 4096, 512, 128, "bf16", "bf16", False, False, 0),      # a round of whole tiles and nothing behind it
+    (1700, 4001, 392, 64, "fp32", "bf16", True, True, 0),
+    (800, 255, 20000, 64, "bf16", "fp32", False, False, 0), (3000, 60, 24000, 128, "bf16", "bf16", False, True, 0),
+    (70000, 250, 232, 64, "bf16", "bf16", False, False, 0),       # many tiles of few steps
+]
+
+
+@pytest.mark.parametrize("case", LARGE, ids=[str(c) for c in LARGE])
+def test_products_in_tiles(torch, case):
+    print(Large(torch, *case, seed=case[0]).check())
+
+
+@pytest.mark.parametrize("case", [LARGE[1], LARGE[6], LARGE[8], LARGE[10]], ids=str)
+def test_products_in_tiles_captured_and_replayed(torch, case):
+    c = Large(torch, *case, seed=1)
+    c.call()
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            c.call(side.cuda_stream)
+    for i in range(3):
+        c.x[:, :c.K] = torch.randn(c.T, c.K, device="cuda")
+        c.ws[:-64].fill_(i)
+        c.y.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = c.y.clone()
+        c.y.fill_(7.0)
+        c.call()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, c.y)
+    c.check()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_not_finite_in_tiles(torch, value):
+    c = Large(torch, 300, 2816, 4104, 64, "bf16", "fp32")
+    c.call()
+    clean = c.y.clone()
+    c.x[137, 4000], c.x[299, 0] = value, value
+    c.call()
+    bad = torch.zeros(300, dtype=torch.bool, device="cuda")
+    bad[[137, 299]] = True
+    assert c.y[bad].isnan().all() and torch.equal(c.y[~bad], clean[~bad])
+
+
 @pytest.mark.parametrize("T", [1, 5, 40, 150])
 @pytest.mark.parametrize("x", ["bf16", "fp32"])
 def test_residual_in_place_and_repeated(torch, T, x):

@@ -207,20 +207,18 @@ struct Block {
 // How the rows of x stand in the 16 rows of a matrix instruction, whose lane holds rows 4 q + i, i =
 // 0..3, of the result (q = lane / 16):
 enum Rows {
-    kFew,       // up to 4 rows of bf16, row q at i = 0: one result a lane
-    kPieces,    // up to 4 rows of fp32, the pieces of row q at i = 0..2: one result a lane, their sum
-    kMore       // up to 16 rows of bf16
+    kFew,       // up to 4 rows of bf16, row q at i = 0
+    kPieces     // up to 4 rows of fp32, the pieces of row q at i = 0..2, added at the end
 };
 constexpr int staged_rows(int rows, int T) { return rows == kPieces ? 3 * T : T; }
 
-// Few rows: all of x goes to LDS first, at most stage_bytes() of it.  The wavefronts join their sums in LDS
+// Up to 4 rows: all of x goes to LDS first, at most stage_bytes() of it.  The wavefronts join their sums in LDS
 // in a fixed order.
 template <int GROUP, int R, int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
     extern __shared__ uint4 lds[];
     constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32;
-    constexpr int NI = ROWS == kFew ? 1 : ROWS == kPieces ? 3 : 4;    // results of a lane,
-    constexpr int NO = ROWS == kMore ? 4 : 1;                         // and after adding the pieces
+    constexpr int NI = ROWS == kFew ? 1 : 3;           // results of a lane
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
@@ -273,8 +271,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
         }
     __syncthreads();
     // rows of the instruction that stand for none repeat one
-    const int row = ROWS == kMore ? min(col, a.T - 1)
-                                  : ROWS == kFew ? min(col >> 2, a.T - 1) : 3 * min(col >> 2, a.T - 1) + min(col & 3, 2);
+    const int row = ROWS == kFew ? min(col >> 2, a.T - 1) : 3 * min(col >> 2, a.T - 1) + min(col & 3, 2);
     const char *staged = reinterpret_cast<const char *>(lds) + row * x_pitch + 16 * quarter;
     float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(lds) + staged_rows(ROWS, a.T) * x_pitch);
 
@@ -310,23 +307,20 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
         }
         load();
         if (now.step == steps - 1) {               // the tile is done: join, then bias and residual
-            float *mine = part + flip * (kWaves * R * NO * 64);
+            float *mine = part + flip * (kWaves * R * 64);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int i = 0; i < NO; ++i) {
-                    float v = sum[r][i];
-                    if constexpr (ROWS == kPieces) v = sum[r][2] + sum[r][1] + v;
-                    mine[((wave * R + r) * NO + i) * 64 + lane] = v;
-                }
+            for (int r = 0; r < R; ++r) {
+                float v = sum[r][0];
+                if constexpr (ROWS == kPieces) v = sum[r][2] + sum[r][1] + v;
+                mine[(wave * R + r) * 64 + lane] = v;
+            }
             __syncthreads();
-            for (int e = threadIdx.x; e < R * NO * 64; e += 64 * kWaves) {
+            const int e = threadIdx.x;
+            if (e < R * 64) {
                 float v = mine[e];
 #pragma unroll
-                for (int w = 1; w < kWaves; ++w) v += mine[w * (R * NO * 64) + e];
-                const int at = e & 63, i = (e >> 6) % NO, r = (e >> 6) / NO;
-                const int64_t t = ROWS == kMore ? 4 * (at >> 4) + i : at >> 4;
-                const int n = now.tile * 16 * R + 16 * r + (at & 15);
+                for (int w = 1; w < kWaves; ++w) v += mine[w * (R * 64) + e];
+                const int t = (e & 63) >> 4, n = now.tile * 16 * R + 16 * (e >> 6) + (e & 15);
                 if (t < a.T && n < a.N) put(a, t, n, v);
             }
             flip ^= 1;                              // the next tile's sums: other wavefronts may still read these
@@ -761,18 +755,20 @@ bool sizes_ok(int N, int K, int group) { return apex_linear_w4_bytes(N, K, group
 
 int padded(int K) { return (K + kBlock - 1) / kBlock * kBlock; }
 
-// Staged rows at most: with two buffers of sums, of four times the size for kMore, 64 KiB.
-constexpr int stage_bytes(Rows rows) { return (rows == kMore ? 31 : 48) << 10; }
+// Staged rows at most.  fp32 rows that are not staged take a launch more, for their pieces: one row of 14336 (86 KiB)
+// through 4096 rows 11.2 us, 24.8 not staged.  bf16 rows of more than this are as fast in linear_some, whose
+// workgroups have LDS for company: 4 rows of 14336 (115 KiB) 13.0 us and 11.4; 4 of 4096 through 32768 14.7 and 18.1.
+constexpr int stage_bytes(Rows rows) { return (rows == kPieces ? 136 : 48) << 10; }
 
 // Whether all of x goes to LDS, and in which rows.
 bool stages(int T, int K, int pieces, Rows *rows) {
-    *rows = pieces == 3 ? kPieces : T <= 4 ? kFew : kMore;
-    return T <= (pieces == 3 ? 4 : 16) && int64_t(staged_rows(*rows, T)) * (padded(K) * 2 + kPad) <= stage_bytes(*rows);
+    *rows = pieces == 3 ? kPieces : kFew;
+    return T <= 4 && int64_t(staged_rows(*rows, T)) * (padded(K) * 2 + kPad) <= stage_bytes(*rows);
 }
 
 template <int GROUP, int R, int ROWS>
 void launch_few(const LinearArgs &a, hipStream_t st) {
-    const size_t lds = staged_rows(ROWS, a.T) * (a.blocks * 256 + kPad) + 2 * 4 * (kWaves * R * 64 * (ROWS == kMore ? 4 : 1));
+    const size_t lds = staged_rows(ROWS, a.T) * (a.blocks * 256 + kPad) + 2 * 4 * (kWaves * R * 64);
     const int tiles = (a.N + 16 * R - 1) / (16 * R);
     hipLaunchKernelGGL((linear_few<GROUP, R, ROWS>), dim3(std::min((tiles + 7) / 8 * 8, 768)), dim3(64 * kWaves), lds, st, a);
 }
@@ -804,9 +800,7 @@ bool narrow(int N) { return N <= 16 * 256; }
 template <int GROUP, int R>
 void launch(const LinearArgs &a, bool stage, Rows rows, hipStream_t st) {
     if (stage)
-        rows == kFew      ? launch_few<GROUP, R, kFew>(a, st)
-        : rows == kPieces ? launch_few<GROUP, R, kPieces>(a, st)
-                          : launch_few<GROUP, R, kMore>(a, st);
+        rows == kFew ? launch_few<GROUP, R, kFew>(a, st) : launch_few<GROUP, R, kPieces>(a, st);
     else if (a.pieces == 3)
         launch_some<GROUP, R, 1, 3>(a, st);
     else

@@ -119,23 +119,31 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
     const int l = threadIdx.x % lanes, first = threadIdx.x / lanes;
     if (first >= rows) return;
     const Places at = places<INTER>(l, a.turn.dim);
-    for (int tok = 0; tok < TOK; ++tok) {
-        const int64_t t = t0 + tok;
-        if (t >= a.turn.T || a.turn.positions[t] < 0) continue;
-        for (int h = blockIdx.y * rows + first; h < a.heads; h += rows * gridDim.y) {
-            char *src = static_cast<char *>(a.x) + (t * a.x_stride + int64_t(h) * a.hd) * size;
-            char *dst = static_cast<char *>(a.out) + (t * a.out_stride + int64_t(h) * a.hd) * size;
-            auto u = four<F32>(src, at.first), v = four<F32>(src, at.second);
+    bool live[TOK];
+#pragma unroll
+    for (int tok = 0; tok < TOK; ++tok) live[tok] = t0 + tok < a.turn.T && a.turn.positions[t0 + tok] >= 0;
+    for (int h = blockIdx.y * rows + first; h < a.heads; h += rows * gridDim.y) {
+        typename Four<F32>::Raw u[TOK], v[TOK];        // of all tokens before the first result goes out
+#pragma unroll
+        for (int tok = 0; tok < TOK; ++tok) {
+            if (!live[tok]) continue;
+            char *src = static_cast<char *>(a.x) + ((t0 + tok) * a.x_stride + int64_t(h) * a.hd) * size;
+            u[tok] = four<F32>(src, at.first), v[tok] = four<F32>(src, at.second);
+        }
+#pragma unroll
+        for (int tok = 0; tok < TOK; ++tok) {
+            if (!live[tok]) continue;
             if (at.turned) {
                 float x[8];
-                widen(u, x);
-                widen(v, x + 4);
+                widen(u[tok], x);
+                widen(v[tok], x + 4);
                 turn<INTER>(x, table + tok * (a.turn.dim / 2) + 4 * l);
-                u = narrow<F32>(x);
-                v = narrow<F32>(x + 4);
+                u[tok] = narrow<F32>(x);
+                v[tok] = narrow<F32>(x + 4);
             }
-            four<F32>(dst, at.first) = u;
-            four<F32>(dst, at.second) = v;
+            char *dst = static_cast<char *>(a.out) + ((t0 + tok) * a.out_stride + int64_t(h) * a.hd) * size;
+            four<F32>(dst, at.first) = u[tok];
+            four<F32>(dst, at.second) = v[tok];
         }
     }
 }
@@ -159,35 +167,46 @@ __global__ __launch_bounds__(kThreads) void store_rotary(StoreArgs a) {
     fill_table<TOK>(a.turn, t0, table);
     const int l = threadIdx.x % lanes, first = threadIdx.x / lanes;
     const Places at = places<INTER>(l, a.turn.dim);
+    int slot[TOK];                                     // -1: not stored, -2: left out
+#pragma unroll
     for (int tok = 0; tok < TOK; ++tok) {
         const int64_t t = t0 + tok;
-        if (t >= a.turn.T || a.turn.positions[t] < 0) continue;
-        const int slot = a.slot_map[t];
-        const bool stored = slot >= 0 && slot < a.n_slots;
-        for (int h = blockIdx.y * rows + first; h < a.H + 2 * a.G; h += rows * gridDim.y) {
-            const bool is_q = h < a.H, is_v = h >= a.H + a.G;
-            if (!is_q && !stored) continue;      // a head's lanes take the same way
-            const int g = is_q ? h : is_v ? h - a.H - a.G : h - a.H;
-            void *base = is_q ? a.q : is_v ? a.v : a.k;
-            const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
-            char *src = static_cast<char *>(base) + (t * stride + int64_t(g) * HD) * size;
-            auto u = four<F32>(src, at.first), v = four<F32>(src, at.second);
-            const bool turned = at.turned && !is_v;
+        slot[tok] = -2;
+        if (t < a.turn.T && a.turn.positions[t] >= 0) {
+            const int s = a.slot_map[t];
+            slot[tok] = s >= 0 && s < a.n_slots ? s : -1;
+        }
+    }
+    for (int h = blockIdx.y * rows + first; h < a.H + 2 * a.G; h += rows * gridDim.y) {
+        const bool is_q = h < a.H, is_v = h >= a.H + a.G;
+        const int g = is_q ? h : is_v ? h - a.H - a.G : h - a.H;
+        const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
+        char *from = static_cast<char *>(is_q ? a.q : is_v ? a.v : a.k) + (t0 * stride + int64_t(g) * HD) * size;
+        const auto left_out = [&](int tok) { return slot[tok] < (is_q ? -1 : 0); };     // a head's lanes take the same way
+        typename Four<F32>::Raw u[TOK], v[TOK];        // of all tokens before the first result goes out
+#pragma unroll
+        for (int tok = 0; tok < TOK; ++tok) {
+            if (left_out(tok)) continue;
+            u[tok] = four<F32>(from + tok * stride * size, at.first), v[tok] = four<F32>(from + tok * stride * size, at.second);
+        }
+#pragma unroll
+        for (int tok = 0; tok < TOK; ++tok) {
+            if (left_out(tok)) continue;
             float x[8];
-            widen(u, x);
-            widen(v, x + 4);
-            if (turned) {
+            widen(u[tok], x);
+            widen(v[tok], x + 4);
+            if (at.turned && !is_v) {
                 turn<INTER>(x, table + tok * (a.turn.dim / 2) + 4 * l);
-                u = narrow<F32>(x);
-                v = narrow<F32>(x + 4);
+                u[tok] = narrow<F32>(x);
+                v[tok] = narrow<F32>(x + 4);
             }
             if (is_q) {
-                char *dst = static_cast<char *>(a.q_out) + (t * a.q_out_stride + int64_t(g) * HD) * size;
-                four<F32>(dst, at.first) = u;
-                four<F32>(dst, at.second) = v;
+                char *dst = static_cast<char *>(a.q_out) + ((t0 + tok) * a.q_out_stride + int64_t(g) * HD) * size;
+                four<F32>(dst, at.first) = u[tok];
+                four<F32>(dst, at.second) = v[tok];
                 continue;
             }
-            const size_t row = (size_t(slot >> a.shift) * a.G + g) * a.page_size + (slot & (a.page_size - 1));
+            const size_t row = (size_t(slot[tok] >> a.shift) * a.G + g) * a.page_size + (slot[tok] & (a.page_size - 1));
             char *dst = static_cast<char *>(is_v ? a.v_pages : a.k_pages) + row * HD * (F8 ? 1 : 2);
             if constexpr (F8) {
                 uint32_t code[2];
@@ -199,8 +218,8 @@ __global__ __launch_bounds__(kThreads) void store_rotary(StoreArgs a) {
                 four<false>(dst, at.first) = narrow<false>(x);
                 four<false>(dst, at.second) = narrow<false>(x + 4);
             } else {
-                four<false>(dst, at.first) = u;
-                four<false>(dst, at.second) = v;
+                four<false>(dst, at.first) = u[tok];
+                four<false>(dst, at.second) = v[tok];
             }
         }
     }

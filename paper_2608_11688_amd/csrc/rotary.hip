@@ -1,8 +1,8 @@
 // Rotary positions (apex_rotary) and the store of turned keys, with their values, into the paged cache
 // (apex_paged_store_rotary).
 //
-// A workgroup takes a few tokens.  Its threads first fill a table in LDS with the cosines and sines of
-// those tokens' angles, one angle each: the angle as turns, position * f / (2 pi) in 64 bits, less its
+// A workgroup takes a token.  Its threads first fill a table in LDS with the cosines and sines of
+// the token's angles, one angle each: the angle as turns, position * f / (2 pi) in 64 bits, less its
 // nearest whole number, is exact to 2^-50 of a turn for any position, and only that fraction goes to
 // 32 bits.  Then lane l of a head's hd / 8 holds 8 values: four pairs of the table where l < dim / 8,
 // else 8 values that stay as they are.  Every head of a token uses the same table, so an angle
@@ -34,17 +34,10 @@ struct Turn {
     int dim, T;
 };
 
-// cos and sin (times the amplitude) of tokens t0 .. t0 + TOK - 1, dim / 2 of each; tokens without a
-// position have no entries.
-template <int TOK>
-__device__ __forceinline__ void fill_table(const Turn &a, int64_t t0, float2 *table) {
-    const int pairs = a.dim / 2;
-    for (int i = threadIdx.x; i < TOK * pairs; i += kThreads) {
-        const int tok = i / pairs;
-        const int64_t t = t0 + tok;
-        const int p = t < a.T ? a.positions[t] : -1;
-        if (p < 0) continue;
-        const double turns = p * a.freq[i - tok * pairs] * 0.15915494309189533577;   // 1 / (2 pi)
+// cos and sin (times the amplitude) of the angles of position p, dim / 2 of them.
+__device__ __forceinline__ void fill_table(const Turn &a, int p, float2 *table) {
+    for (int i = threadIdx.x; i < a.dim / 2; i += kThreads) {
+        const double turns = p * a.freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
         const float part = float(turns - rint(turns));
         float s, c;
         sincospif(2.f * part, &s, &c);
@@ -53,16 +46,16 @@ __device__ __forceinline__ void fill_table(const Turn &a, int64_t t0, float2 *ta
     __syncthreads();
 }
 
-// The two places in a head where lane l's 8 values stand, four each.
+// The two places in a head where lane l's 8 values stand, four each: of the turned part and of the rest both halves
+// are in the order of the lanes, so that neighbours' 16 (or 8) bytes are side by side.
 struct Places {
     int first, second;
     bool turned;
 };
-template <bool INTER>
-__device__ __forceinline__ Places places(int l, int dim) {
+__device__ __forceinline__ Places places(int l, int dim, int hd) {
     const bool turned = l < dim / 8;
-    if (turned && !INTER) return {4 * l, dim / 2 + 4 * l, true};
-    return {8 * l, 8 * l + 4, turned};
+    const int base = turned ? 0 : dim, half = (turned ? dim : hd - dim) / 2, at = base + 4 * (turned ? l : l - dim / 8);
+    return {at, at + half, turned};
 }
 
 // Four values as they stand in memory.
@@ -90,16 +83,39 @@ __device__ __forceinline__ typename Four<F32>::Raw narrow(const float *x) {
         return make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
 }
 
-// Four pairs of x: x[i] with x[4 + i], or neighbours.
+// Lane l's four pairs: x[i] with x[4 + i], or neighbours.
 template <bool INTER>
-__device__ __forceinline__ void turn(float (&x)[8], const float2 *cs) {
+__device__ __forceinline__ void turn(float (&x)[8], const float2 *table, int l, int dim) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        const float2 cs = table[INTER ? (i < 2 ? 2 * l + i : dim / 4 + 2 * l + i - 2) : 4 * l + i];
         float &a = x[INTER ? 2 * i : i], &b = x[INTER ? 2 * i + 1 : 4 + i];
-        const float u = a, v = b, c = cs[i].x, s = cs[i].y;
-        a = fmaf(u, c, -(v * s));
-        b = fmaf(u, s, v * c);
+        const float u = a, v = b;
+        a = fmaf(u, cs.x, -(v * cs.y));
+        b = fmaf(u, cs.y, v * cs.x);
     }
+}
+
+// Rows are read once: their lines need not stay.  Results need not either where they are many (`stream`).
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float4 load(const float4 &p) {
+    return __builtin_bit_cast(float4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(&p)));
+}
+__device__ __forceinline__ uint2 load(const uint2 &p) {
+    return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(&p)));
+}
+__device__ __forceinline__ void store(float4 &p, float4 v, bool stream) {
+    if (stream)
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(&p));
+    else
+        p = v;
+}
+__device__ __forceinline__ void store(uint2 &p, uint2 v, bool stream) {
+    if (stream)
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x2, v), reinterpret_cast<u32x2 *>(&p));
+    else
+        p = v;
 }
 
 struct RotaryArgs {
@@ -107,44 +123,35 @@ struct RotaryArgs {
     void *x, *out;       // x is read only
     int64_t x_stride, out_stride;
     int heads, hd;
+    bool stream;
 };
 
-template <bool F32, bool INTER, int TOK>
+template <bool F32, bool INTER>
 __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
-    __shared__ float2 table[TOK * (kMaxHd / 2)];
+    __shared__ float2 table[kMaxHd / 2];
     constexpr int size = F32 ? 4 : 2;
-    const int64_t t0 = int64_t(blockIdx.x) * TOK;
-    fill_table<TOK>(a.turn, t0, table);
+    const int64_t t = blockIdx.x;
+    const int p = a.turn.positions[t];
+    if (p < 0) return;
+    fill_table(a.turn, p, table);
     const int lanes = a.hd / 8, rows = kThreads / lanes;      // of a head; heads at a time
     const int l = threadIdx.x % lanes, first = threadIdx.x / lanes;
     if (first >= rows) return;
-    const Places at = places<INTER>(l, a.turn.dim);
-    bool live[TOK];
-#pragma unroll
-    for (int tok = 0; tok < TOK; ++tok) live[tok] = t0 + tok < a.turn.T && a.turn.positions[t0 + tok] >= 0;
+    const Places at = places(l, a.turn.dim, a.hd);
     for (int h = blockIdx.y * rows + first; h < a.heads; h += rows * gridDim.y) {
-        typename Four<F32>::Raw u[TOK], v[TOK];        // of all tokens before the first result goes out
-#pragma unroll
-        for (int tok = 0; tok < TOK; ++tok) {
-            if (!live[tok]) continue;
-            char *src = static_cast<char *>(a.x) + ((t0 + tok) * a.x_stride + int64_t(h) * a.hd) * size;
-            u[tok] = four<F32>(src, at.first), v[tok] = four<F32>(src, at.second);
+        char *src = static_cast<char *>(a.x) + (t * a.x_stride + int64_t(h) * a.hd) * size;
+        char *dst = static_cast<char *>(a.out) + (t * a.out_stride + int64_t(h) * a.hd) * size;
+        auto u = load(four<F32>(src, at.first)), v = load(four<F32>(src, at.second));
+        if (at.turned) {
+            float x[8];
+            widen(u, x);
+            widen(v, x + 4);
+            turn<INTER>(x, table, l, a.turn.dim);
+            u = narrow<F32>(x);
+            v = narrow<F32>(x + 4);
         }
-#pragma unroll
-        for (int tok = 0; tok < TOK; ++tok) {
-            if (!live[tok]) continue;
-            if (at.turned) {
-                float x[8];
-                widen(u[tok], x);
-                widen(v[tok], x + 4);
-                turn<INTER>(x, table + tok * (a.turn.dim / 2) + 4 * l);
-                u[tok] = narrow<F32>(x);
-                v[tok] = narrow<F32>(x + 4);
-            }
-            char *dst = static_cast<char *>(a.out) + ((t0 + tok) * a.out_stride + int64_t(h) * a.hd) * size;
-            four<F32>(dst, at.first) = u[tok];
-            four<F32>(dst, at.second) = v[tok];
-        }
+        store(four<F32>(dst, at.first), u, a.stream);
+        store(four<F32>(dst, at.second), v, a.stream);
     }
 }
 
@@ -157,70 +164,55 @@ struct StoreArgs {
     void *k_pages, *v_pages;
     float *k_scales, *v_scales;
     int H, G, page_size, shift, n_slots;
+    bool stream;
 };
 
-template <int HD, bool F32, bool F8, bool INTER, int TOK>
+template <int HD, bool F32, bool F8, bool INTER>
 __global__ __launch_bounds__(kThreads) void store_rotary(StoreArgs a) {
-    __shared__ float2 table[TOK * (HD / 2)];
+    __shared__ float2 table[HD / 2];
     constexpr int size = F32 ? 4 : 2, lanes = HD / 8, rows = kThreads / lanes;
-    const int64_t t0 = int64_t(blockIdx.x) * TOK;
-    fill_table<TOK>(a.turn, t0, table);
+    const int64_t t = blockIdx.x;
+    const int p = a.turn.positions[t], slot = a.slot_map[t];
+    if (p < 0) return;
+    fill_table(a.turn, p, table);
+    const bool stored = slot >= 0 && slot < a.n_slots;
     const int l = threadIdx.x % lanes, first = threadIdx.x / lanes;
-    const Places at = places<INTER>(l, a.turn.dim);
-    int slot[TOK];                                     // -1: not stored, -2: left out
-#pragma unroll
-    for (int tok = 0; tok < TOK; ++tok) {
-        const int64_t t = t0 + tok;
-        slot[tok] = -2;
-        if (t < a.turn.T && a.turn.positions[t] >= 0) {
-            const int s = a.slot_map[t];
-            slot[tok] = s >= 0 && s < a.n_slots ? s : -1;
-        }
-    }
+    const Places at = places(l, a.turn.dim, HD);
     for (int h = blockIdx.y * rows + first; h < a.H + 2 * a.G; h += rows * gridDim.y) {
         const bool is_q = h < a.H, is_v = h >= a.H + a.G;
+        if (!is_q && !stored) continue;          // a head's lanes take the same way
         const int g = is_q ? h : is_v ? h - a.H - a.G : h - a.H;
         const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
-        char *from = static_cast<char *>(is_q ? a.q : is_v ? a.v : a.k) + (t0 * stride + int64_t(g) * HD) * size;
-        const auto left_out = [&](int tok) { return slot[tok] < (is_q ? -1 : 0); };     // a head's lanes take the same way
-        typename Four<F32>::Raw u[TOK], v[TOK];        // of all tokens before the first result goes out
-#pragma unroll
-        for (int tok = 0; tok < TOK; ++tok) {
-            if (left_out(tok)) continue;
-            u[tok] = four<F32>(from + tok * stride * size, at.first), v[tok] = four<F32>(from + tok * stride * size, at.second);
+        char *src = static_cast<char *>(is_q ? a.q : is_v ? a.v : a.k) + (t * stride + int64_t(g) * HD) * size;
+        auto u = load(four<F32>(src, at.first)), v = load(four<F32>(src, at.second));
+        float x[8];
+        widen(u, x);
+        widen(v, x + 4);
+        if (at.turned && !is_v) {
+            turn<INTER>(x, table, l, a.turn.dim);
+            u = narrow<F32>(x);
+            v = narrow<F32>(x + 4);
         }
-#pragma unroll
-        for (int tok = 0; tok < TOK; ++tok) {
-            if (left_out(tok)) continue;
-            float x[8];
-            widen(u[tok], x);
-            widen(v[tok], x + 4);
-            if (at.turned && !is_v) {
-                turn<INTER>(x, table + tok * (a.turn.dim / 2) + 4 * l);
-                u[tok] = narrow<F32>(x);
-                v[tok] = narrow<F32>(x + 4);
-            }
-            if (is_q) {
-                char *dst = static_cast<char *>(a.q_out) + ((t0 + tok) * a.q_out_stride + int64_t(g) * HD) * size;
-                four<F32>(dst, at.first) = u[tok];
-                four<F32>(dst, at.second) = v[tok];
-                continue;
-            }
-            const size_t row = (size_t(slot[tok] >> a.shift) * a.G + g) * a.page_size + (slot[tok] & (a.page_size - 1));
-            char *dst = static_cast<char *>(is_v ? a.v_pages : a.k_pages) + row * HD * (F8 ? 1 : 2);
-            if constexpr (F8) {
-                uint32_t code[2];
-                const float s = e4m3_row<lanes>(x, code);
-                *reinterpret_cast<uint32_t *>(dst + at.first) = code[0];
-                *reinterpret_cast<uint32_t *>(dst + at.second) = code[1];
-                if (l == 0) (is_v ? a.v_scales : a.k_scales)[row] = s;
-            } else if constexpr (F32) {
-                four<false>(dst, at.first) = narrow<false>(x);
-                four<false>(dst, at.second) = narrow<false>(x + 4);
-            } else {
-                four<false>(dst, at.first) = u[tok];
-                four<false>(dst, at.second) = v[tok];
-            }
+        if (is_q) {
+            char *dst = static_cast<char *>(a.q_out) + (t * a.q_out_stride + int64_t(g) * HD) * size;
+            store(four<F32>(dst, at.first), u, a.stream);
+            store(four<F32>(dst, at.second), v, a.stream);
+            continue;
+        }
+        const size_t row = (size_t(slot >> a.shift) * a.G + g) * a.page_size + (slot & (a.page_size - 1));
+        char *dst = static_cast<char *>(is_v ? a.v_pages : a.k_pages) + row * HD * (F8 ? 1 : 2);
+        if constexpr (F8) {
+            uint32_t code[2];
+            const float s = e4m3_row<lanes>(x, code);
+            *reinterpret_cast<uint32_t *>(dst + at.first) = code[0];
+            *reinterpret_cast<uint32_t *>(dst + at.second) = code[1];
+            if (l == 0) (is_v ? a.v_scales : a.k_scales)[row] = s;
+        } else if constexpr (F32) {
+            four<false>(dst, at.first) = narrow<false>(x);
+            four<false>(dst, at.second) = narrow<false>(x + 4);
+        } else {
+            four<false>(dst, at.first) = u;
+            four<false>(dst, at.second) = v;
         }
     }
 }
@@ -236,35 +228,23 @@ apex_status check_rotation(const char *fn, const apex_rotation *r, int hd, bool 
     return APEX_OK;
 }
 
-// Tokens of a workgroup, and workgroups along a token's heads.
-constexpr int kTokens = 4;
-
-dim3 grid_of(int T, int tok, int heads, int rows) {
-    const int64_t groups = (int64_t(T) + tok - 1) / tok;
-    // few tokens: their heads over more workgroups
-    const int64_t along = std::min<int64_t>((heads + rows - 1) / rows, std::max<int64_t>(1, 512 / groups));
-    return dim3(unsigned(groups), unsigned(along));
+// A workgroup a token; of few tokens the heads over several.
+dim3 grid_of(int T, int heads, int rows) {
+    return dim3(unsigned(T), unsigned(std::min((heads + rows - 1) / rows, std::max(1, 512 / T))));
 }
+
+// Results of more than this are written past the caches, which the next kernel finds full of something else.
+constexpr int64_t kStreamBytes = int64_t(32) << 20;
 
 template <bool F32, bool INTER>
 void launch_rotary(const RotaryArgs &a, hipStream_t st) {
-    const int rows = kThreads / (a.hd / 8);
-    if (a.turn.T <= 1024)
-        hipLaunchKernelGGL((rotary<F32, INTER, 1>), grid_of(a.turn.T, 1, a.heads, rows), dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL((rotary<F32, INTER, kTokens>), grid_of(a.turn.T, kTokens, a.heads, rows), dim3(kThreads), 0,
-                           st, a);
+    hipLaunchKernelGGL((rotary<F32, INTER>), grid_of(a.turn.T, a.heads, kThreads / (a.hd / 8)), dim3(kThreads), 0, st, a);
 }
 
 template <int HD, bool F32, bool F8, bool INTER>
 void launch_store(const StoreArgs &a, hipStream_t st) {
-    const int rows = kThreads / (HD / 8), heads = a.H + 2 * a.G;
-    if (a.turn.T <= 1024)
-        hipLaunchKernelGGL((store_rotary<HD, F32, F8, INTER, 1>), grid_of(a.turn.T, 1, heads, rows), dim3(kThreads), 0,
-                           st, a);
-    else
-        hipLaunchKernelGGL((store_rotary<HD, F32, F8, INTER, kTokens>), grid_of(a.turn.T, kTokens, heads, rows),
-                           dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((store_rotary<HD, F32, F8, INTER>), grid_of(a.turn.T, a.H + 2 * a.G, kThreads / (HD / 8)),
+                       dim3(kThreads), 0, st, a);
 }
 
 template <int HD>
@@ -308,7 +288,7 @@ extern "C" apex_status apex_rotary(const apex_rotation *rotation, const void *x,
     APEX_REQUIRE(x != out || x_stride == out_stride, "%s: out is x with another stride", fn);
     const RotaryArgs a{{rotation->freq, positions, rotation->amplitude, rotation->dim, T}, const_cast<void *>(x),
                        out, x_stride,
-                       out_stride, heads, hd};
+                       out_stride, heads, hd, int64_t(T) * heads * hd * (dtype == APEX_TYPE_FP32 ? 4 : 2) > kStreamBytes};
     const bool inter = rotation->layout == APEX_ROPE_INTERLEAVED;
     if (dtype == APEX_TYPE_FP32)
         inter ? launch_rotary<true, true>(a, stream) : launch_rotary<true, false>(a, stream);
@@ -348,7 +328,8 @@ extern "C" apex_status apex_paged_store_rotary(const apex_paged_cache *cache, co
                       const_cast<void *>(k), const_cast<void *>(v), q_out,
                       q_stride, k_stride, v_stride, q_out_stride, slot_map, cache->k_pages, cache->v_pages,
                       cache->k_scales, cache->v_scales, H, G, cache->page_size, apex::log2_of(cache->page_size),
-                      cache->n_pages * cache->page_size};
+                      cache->n_pages * cache->page_size,
+                      int64_t(T) * H * hd * (dtype == APEX_TYPE_FP32 ? 4 : 2) > kStreamBytes};
     const bool f32 = dtype == APEX_TYPE_FP32, f8 = cache->format == APEX_KV_FP8_E4M3;
     const bool inter = rotation->layout == APEX_ROPE_INTERLEAVED;
     if (hd == 64)

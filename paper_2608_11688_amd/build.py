@@ -23,7 +23,8 @@ LIB = os.path.join(PKG, "libapex.so")
 PLAN_LIB = os.path.join(PKG, "libapex_plan.so")
 
 HIP_SOURCES = ["errors.cpp", "residency.cpp", "pack_fp8.cpp", "pack_mxfp4.cpp", "pack_fp32.cpp",
-               "pack_linear.cpp", "rotary_frequencies.cpp", "decode.cpp", "route_gate.hip", "moe_ffn.cpp", "ffn_b1.hip", "ffn_b1_e4m3.hip",
+               "pack_linear.cpp", "rotary_frequencies.cpp", "decode.cpp",
+               "route_gate.hip", "moe_ffn.cpp", "ffn_b1.hip", "ffn_b1_e4m3.hip",
                "ffn_b1_mxfp4.hip", "ffn_b1_fp32.hip", "ffn_gemm.hip", "ffn_noalloc.hip",
                "attention.hip", "paged_cache.hip", "paged_attention.hip",
                "rotary.hip", "linear_w4.hip", "prefetch.hip", "util.hip"]

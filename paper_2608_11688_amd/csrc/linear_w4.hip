@@ -24,8 +24,8 @@ struct LinearArgs {
     const uint8_t *codes;
     const uint32_t *words;
     const uint16_t *x;              // bf16, or the pieces of fp32
-    int64_t x_stride, x_block, x_piece;      // in values: of rows, of 128 values along K, of pieces
-    int x_cols;                     // values of a row of x that there are (a multiple of 8)
+    int64_t x_stride, x_block, x_piece;      // in values: of rows; for linear_many also of 128 values along K, of pieces
+    int x_cols;                     // values of a row of x that there are (a multiple of 8), but for linear_many
     const float *bias;
     const void *residual;
     void *y;
@@ -33,7 +33,6 @@ struct LinearArgs {
     int N, T, blocks;               // blocks of kBlock codes in a row
     int pieces;                     // of x: 1 (bf16) or 3 (fp32; in memory where !STAGE)
     bool y32;
-    bool fours;                     // rows of y and of the residual begin at multiples of 4 values, and so does N
 };
 
 // Codes 2 i and 2 i + 1 of a word as bf16 pairs 16 + q.
@@ -82,20 +81,13 @@ __device__ __forceinline__ void put(const LinearArgs &a, int64_t t, int n, float
     store_y(a.y32, a.y, t * a.y_stride + n, y);
 }
 
-// A lane's values of row n of the weights and 4 tokens from t on.  Where rows of y begin at multiples of 4 values, 4
-// lanes (n a multiple of 4 in the first) first trade places, so that each has 4 values of one token, side by side.
+// A lane's values of row n of the weights and 4 tokens from t on.  4 lanes (n a multiple of 4 in the first) first trade
+// places, so that each has 4 values of one token, side by side; rows may begin at any value.
 template <int CTRL>
 __device__ __forceinline__ float quad(float v) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
 }
 __device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, floatx4 v) {
-    if (!a.fours) {
-        if (n >= a.N) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (t + i < a.T) put(a, t + i, n, v[i]);
-        return;
-    }
     // lane l of the four, value i -> lane i, value l: by halves (l ^ 2 and i ^ 2), then by ones
     const int l = threadIdx.x & 3;
     const float p0 = quad<0x4e>(l & 2 ? v[0] : v[2]), p1 = quad<0x4e>(l & 2 ? v[1] : v[3]);
@@ -106,17 +98,29 @@ __device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, 
     else v[1] = q0, v[3] = q1;
     t += l;
     n -= l;
-    if (t >= a.T || n >= a.N) return;                  // N is a multiple of 4
+    if (t >= a.T || n >= a.N) return;
+    if (n + 4 > a.N) {                                 // the last values of a row
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (n + i < a.N) put(a, t, n + i, v[i]);
+        return;
+    }
     if (a.bias) {
         const float4 b = *reinterpret_cast<const float4 *>(a.bias + n);
         v[0] += b.x, v[1] += b.y, v[2] += b.z, v[3] += b.w;
     }
+    const int64_t to = t * a.y_stride + n, from = t * a.residual_stride + n;
     if (a.y32) {
-        if (a.residual) v += *reinterpret_cast<const floatx4 *>(static_cast<const float *>(a.residual) + t * a.residual_stride + n);
-        *reinterpret_cast<floatx4 *>(static_cast<float *>(a.y) + t * a.y_stride + n) = v;
+        if (a.residual) {
+            floatx4 r;
+            __builtin_memcpy(&r, static_cast<const float *>(a.residual) + from, 16);
+            v += r;
+        }
+        __builtin_memcpy(static_cast<float *>(a.y) + to, &v, 16);
     } else {
         if (a.residual) {
-            const uint2 r = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.residual) + t * a.residual_stride + n);
+            uint2 r;
+            __builtin_memcpy(&r, static_cast<const uint16_t *>(a.residual) + from, 8);
             v[0] += __uint_as_float(r.x << 16), v[1] += __uint_as_float(r.x & 0xffff0000u);
             v[2] += __uint_as_float(r.y << 16), v[3] += __uint_as_float(r.y & 0xffff0000u);
         }
@@ -124,7 +128,7 @@ __device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, 
         bf16x4 y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = static_cast<__bf16>(v[i]);
-        *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.y) + t * a.y_stride + n) = y;
+        __builtin_memcpy(static_cast<uint16_t *>(a.y) + to, &y, 8);
     }
 }
 
@@ -180,7 +184,7 @@ __device__ __forceinline__ void words_of(uint32_t word, uint32_t (&w)[PER]) {
 }
 
 // The codes and the group words of a block of 16 R rows, D blocks ahead of their use.  Descriptors end
-// with the tile's rows, and are empty for blocks that are not there: such loads move nothing. 
+// with the tile's rows, and are empty for blocks that are not there: such loads move nothing.
 template <int GROUP, int R>
 struct Block {
     static constexpr int PER = kBlock / GROUP;
@@ -333,15 +337,15 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
     }
 }
 
-// Some rows, more than are staged at once: up to 16 TT rows, bf16 or (P = 3) the pieces of fp32.  A
-// workgroup takes 16 R rows of the weights; each wavefront brings the part of x that belongs to its
-// next block, P TT times 16 rows of 256 bytes, into LDS of its own, by loads of whole lines, and reads
-// them as the matrix instructions want them.  Within a row 16-byte chunks stand in the place c ^ (row mod
-// 16), so that 16 rows' chunks meet 64 banks.
+// Some rows, in tiles of 16 TT, bf16 or fp32 (P = 3 pieces).  A workgroup takes 16 R rows of the weights; each wavefront
+// brings the part of x that belongs to its next block, 16 TT rows of 256 or 512 bytes, by loads of whole lines, fp32 values
+// cut into their pieces on the way, into LDS of its own, and reads it as the matrix instructions want it.  Within
+// a row 16-byte chunks stand in the place c ^ (row mod 16), so that 16 rows' chunks meet 64 banks.
 template <int GROUP, int R, int TT, int P>
 __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
-    constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, LOADS = 4 * TT * P, OUT = R * TT * 4 * 64;
-    __shared__ uint4 lds[kWaves * (LOADS * 64 > OUT / 4 ? LOADS * 64 : OUT / 4)];     // x, then the sums
+    constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, LOADS = 4 * TT, PARTS = P == 3 ? 2 : 1;   // of 16 bytes for 8 values
+    constexpr int STAGE = 4 * TT * P * 64, OUT = R * TT * 64;
+    __shared__ uint4 lds[kWaves * (STAGE > OUT ? STAGE : OUT)];       // x, then the sums
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
@@ -349,30 +353,41 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     const int n0 = ((blockIdx.x & 7) * per + (blockIdx.x >> 3)) * 16 * R;      // as in Walk, one tile each
     if (n0 >= a.N) return;
     const int t0 = blockIdx.y * 16 * TT;
-    uint4 x[LOADS];
+    uint4 x[LOADS][PARTS];
     Block<GROUP, R> next;
-    // load i of a block: rows 4 (i mod 4 TT) + quarter of a piece, chunk `col`
+    // load i of a block: row 4 i + quarter, chunk `col` of 8 values
     const auto load_x = [&](int b) {
         const int k = b * kBlock + 8 * col;
         const bool there = k < a.x_cols;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int t = min(t0 + 4 * (i % (4 * TT)) + quarter, a.T - 1);
-            uint4 v = *reinterpret_cast<const uint4 *>(a.x + i / (4 * TT) * a.x_piece + t * a.x_stride +
-                                                       (there ? b * a.x_block + 8 * col : 0));
-            if (!there) v = make_uint4(0u, 0u, 0u, 0u);
-            x[i] = v;
+            const int t = min(t0 + 4 * i + quarter, a.T - 1);
+            const uint4 *from = reinterpret_cast<const uint4 *>(a.x + (t * a.x_stride + (there ? k : 0)) * PARTS);
+#pragma unroll
+            for (int h = 0; h < PARTS; ++h) {
+                x[i][h] = from[h];
+                if (!there) x[i][h] = make_uint4(0u, 0u, 0u, 0u);
+            }
         }
     };
-    char *mine = reinterpret_cast<char *>(lds) + wave * (LOADS * 1024);
-    float sum[R][TT][4] = {};
+    char *mine = reinterpret_cast<char *>(lds) + wave * (STAGE * 16);
+    floatx4 sum[R][TT] = {};
     load_x(wave);
     next.load(a, n0, wave, wave < a.blocks, lane);
     for (int b = wave; b < a.blocks; b += kWaves) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int row = 4 * i + quarter;
-            *reinterpret_cast<uint4 *>(mine + row * 256 + 16 * (col ^ (row & 15))) = x[i];
+            const int row = 4 * i + quarter, at = row * 256 + 16 * (col ^ (row & 15));
+            if constexpr (P == 1) {
+                *reinterpret_cast<uint4 *>(mine + at) = x[i][0];
+            } else {
+                uint4 piece[3];
+                cut({__uint_as_float(x[i][0].x), __uint_as_float(x[i][0].y), __uint_as_float(x[i][0].z), __uint_as_float(x[i][0].w),
+                     __uint_as_float(x[i][1].x), __uint_as_float(x[i][1].y), __uint_as_float(x[i][1].z), __uint_as_float(x[i][1].w)},
+                    piece);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4 *>(mine + p * (TT * 4096) + at) = piece[p];
+            }
         }
         const Block<GROUP, R> now = next;
         load_x(b + kWaves);
@@ -405,27 +420,28 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
 #pragma unroll
                 for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w.add(sum[r][tt][i], prod[r][tt][i], total[tt][i]);
+                    for (int i = 0; i < 4; ++i) {
+                        float s = sum[r][tt][i];
+                        w.add(s, prod[r][tt][i], total[tt][i]);
+                        sum[r][tt][i] = s;
+                    }
             }
         }
     }
     __syncthreads();
-    float *part = reinterpret_cast<float *>(lds);
+    floatx4 *part = reinterpret_cast<floatx4 *>(lds);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[wave * OUT + ((r * TT + tt) * 4 + i) * 64 + lane] = sum[r][tt][i];
+        for (int tt = 0; tt < TT; ++tt) part[wave * OUT + (r * TT + tt) * 64 + lane] = sum[r][tt];
     __syncthreads();
-    for (int e = threadIdx.x; e < OUT; e += 64 * kWaves) {
-        float v = part[e];
+    const int e = threadIdx.x;
+    if (e < OUT) {
+        floatx4 v = part[e];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) v += part[w * OUT + e];
-        const int at = e & 63, i = (e >> 6) & 3, tt = (e >> 8) % TT, r = (e >> 8) / TT;
-        const int64_t t = t0 + 16 * tt + 4 * (at >> 4) + i;
-        const int n = n0 + 16 * r + (at & 15);
-        if (t < a.T && n < a.N) put(a, t, n, v);
+        const int at = e & 63, tt = (e >> 6) % TT, r = (e >> 6) / TT;
+        put_four(a, t0 + 16 * tt + 4 * (at >> 4), n0 + 16 * r + (at & 15), v);
     }
 }
 
@@ -705,10 +721,10 @@ __global__ __launch_bounds__(256) void join(ManyArgs m) {
     put_four(m.a, at.t, at.n, v);
 }
 
-// Sums of x over groups of GROUP values, [groups / 4][T][4] (or NULL), and x as bf16 (PIECES: fp32 values as three pieces)
-// in the order in which it is read: [block of 128 values][piece][T][128], zeros behind K.  Rows of x as they are,
-// often a power of two of bytes apart, have the same block of all rows in one channel of the L2: a chunk of 2048 rows
-// through 6144 x 4096 took 146 us instead of #MANY#.  A lane takes 8 values, GROUP / 8 lanes a group.
+// Sums of x over groups of GROUP values, [groups / 4][T][4], and x as bf16 (PIECES: fp32 values as three pieces)
+// in the order in which it is read: [block of 128 values][piece][T][128], zeros behind K.  linear_many's loads are then
+// side by side whatever the stride of x is; a chunk of 2048 rows through 6144 x 4096 took 139 us with x in this order and 146
+// with bf16 rows as they stand.  A lane takes 8 values, GROUP / 8 lanes a group.
 template <int GROUP, bool PIECES>
 __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
                                               uint16_t *out) {
@@ -740,7 +756,6 @@ __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int
                 v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
             }
         }
-        if (!totals) continue;
         float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         // 4, 8 or 16 lanes of a group, aligned, all of which are here: Kp is a multiple of 128
         s += __shfl_xor(s, 1);
@@ -823,6 +838,7 @@ struct Plan {
     size_t bytes() const { return pieces + totals + parts; }
 };
 
+constexpr int kGridY = 65535;        // of a launch
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 Plan plan_of(int T, int N, int K, int group, int pieces) {
@@ -832,15 +848,18 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
         p.kind = Plan::kStaged;
         return p;
     }
-    // linear_some reads the weights once for every tile of tokens, linear_many is three launches.  us, some and many:
-    // bf16 rows through 4096 x 4096 (17 million codes), 32: 7.9 and 18.8, 128: 19.8 and 29.2, 192: 26.4 and 28.8; through
-    // 16384 x 4096, 32: 16 and 22, 48: 28.6 and 23.2; through 512 x 2048, 192: 5.9 and 20; fp32 rows through 4096 x 4096,
-    // 32: 18.5 and 26.2, 48: 26.0 and 27.2, 64: 33.0 and 28.2; through 4096 x 14336, 16: 26.7 and 36.0, 24: 47.1 and 36.5.
+    // linear_some reads the weights once for every tile of tokens, linear_many is two or three launches.  us, some and
+    // many: bf16 rows through 4096 x 4096 (17 million codes), 32: 7.9 and 18.6, 96: 16.5 and 28.5, 192: 28.2 and 28.8;
+    // through 16384 x 4096, 32: 15.8 and 22.5, 48: 27.9 and 23.1; through 512 x 2048, 192: 5.6 and 19.7; fp32 rows through
+    // 4096 x 4096, 16: 9.5 and 25.8, 48: 25.1 and 27.3, 64: 32.3 and 27.9; through 16384 x 4096, 16: 20.1 and 34.4, 24: 37.9
+    // and 34.6; through 4096 x 14336, 16: 26.6 and 36.4, 24: 50.4 and 36.7.
     const int tokens = pieces == 3 ? 16 : 32;          // of a tile of linear_some
-    const int64_t reads = int64_t((T + tokens - 1) / tokens) * N * K;
-    p.kind = T <= tokens || reads <= (pieces == 3 ? 50000000 : 110000000) ? Plan::kSome : Plan::kMany;
-    if (pieces == 3 || p.kind == Plan::kMany) p.pieces = up256(size_t(pieces) * T * Kp * 2);
+    const int token_tiles = (T + tokens - 1) / tokens;
+    p.kind = token_tiles == 1 || (int64_t(token_tiles) * N * K <= (pieces == 3 ? 50000000 : 110000000) && token_tiles <= kGridY)
+                 ? Plan::kSome
+                 : Plan::kMany;
     if (p.kind == Plan::kSome) return p;
+    p.pieces = up256(size_t(pieces) * T * Kp * 2);
     p.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
     p.tt = T <= 64 ? 4 : 8;
     p.m_tiles = (T + 16 * p.tt - 1) / (16 * p.tt);
@@ -895,26 +914,22 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         return apex::fail(APEX_E_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
-                 static_cast<const uint16_t *>(x), x_stride, kBlock, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
-                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32,
-                 N % 4 == 0 && y_stride % 4 == 0 && (!residual || residual_stride % 4 == 0)};
-    char *ws = static_cast<char *>(workspace);
-    float *totals = reinterpret_cast<float *>(ws + plan.pieces);
-    if (plan.pieces) {
-        uint16_t *out = reinterpret_cast<uint16_t *>(ws);
+                 static_cast<const uint16_t *>(x), x_stride, 0, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
+                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32};
+    if (plan.kind == Plan::kMany) {
+        char *ws = static_cast<char *>(workspace);
+        float *totals = reinterpret_cast<float *>(ws + plan.pieces);
+        uint16_t *tiled = reinterpret_cast<uint16_t *>(ws);
         const int64_t items = int64_t(T) * (Kp / 8);
         const dim3 grid(unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)));
         const auto f = pieces > 1 ? (group == 32 ? survey<32, true> : group == 64 ? survey<64, true> : survey<128, true>)
                                   : (group == 32 ? survey<32, false> : group == 64 ? survey<64, false> : survey<128, false>);
-        hipLaunchKernelGGL(f, grid, dim3(256), 0, stream, x, x_stride, T, K, Kp, plan.totals ? totals : nullptr, out);
+        hipLaunchKernelGGL(f, grid, dim3(256), 0, stream, x, x_stride, T, K, Kp, totals, tiled);
         APEX_HIP(hipGetLastError());
-        a.x = out;
+        a.x = tiled;
         a.x_stride = kBlock;
         a.x_piece = int64_t(T) * kBlock;
         a.x_block = pieces * a.x_piece;
-        a.x_cols = Kp;
-    }
-    if (plan.kind == Plan::kMany) {
         const ManyArgs m{a, totals, reinterpret_cast<float *>(ws + plan.pieces + plan.totals), plan.m_tiles, plan.tiles,
                          plan.whole, plan.splits, plan.share};
         group == 32 ? launch_many<32>(m, plan.tt, stream) : group == 64 ? launch_many<64>(m, plan.tt, stream)

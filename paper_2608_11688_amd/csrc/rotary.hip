@@ -2,9 +2,7 @@
 // (apex_paged_store_rotary).
 //
 // A workgroup takes a token.  Its threads first fill a table in LDS with the cosines and sines of
-// the token's angles, one angle each: the angle as turns, position * f / (2 pi) in 64 bits, less its
-// nearest whole number, is exact to 2^-50 of a turn for any position, and only that fraction goes to
-// 32 bits.  Then lane l of a head's hd / 8 holds 8 values: four pairs of the table where l < dim / 8,
+// the token's angles, one angle each, in 64 bits and rounded once.  Then lane l of a head's hd / 8 holds 8 values: four pairs of the table where l < dim / 8,
 // else 8 values that stay as they are.  Every head of a token uses the same table, so an angle
 // costs its share of H + G heads; what remains is one read and one write of every value.
 #include <hip/hip_runtime.h>
@@ -34,14 +32,25 @@ struct Turn {
     int dim, T;
 };
 
-// cos and sin (times the amplitude) of the angles of position p, dim / 2 of them.
+// cos and sin (times the amplitude) of the angles of position p, dim / 2 of them.  An angle is turns = p f / (2 pi), as the
+// sum of two 64-bit numbers whose rounding errors are carried along, less its nearest quarter: at most an eighth of a
+// turn, where the series end with x^11 and x^12 (the next terms are below 2^-36), and rounded to 32 bits at the very end.
 __device__ __forceinline__ void fill_table(const Turn &a, int p, float2 *table) {
+    constexpr double kHi = 0x1.45f306dc9c883p-3, kLo = -0x1.6b01ec5417056p-57;       // 1 / (2 pi)
     for (int i = threadIdx.x; i < a.dim / 2; i += kThreads) {
-        const double turns = p * a.freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
-        const float part = float(turns - rint(turns));
-        float s, c;
-        sincospif(2.f * part, &s, &c);
-        table[i] = make_float2(a.amplitude * c, a.amplitude * s);
+        const double f = a.freq[i], angle = p * f, turns = angle * kHi;
+        const double low = fma(angle, kLo, fma(fma(double(p), f, -angle), kHi, fma(angle, kHi, -turns)));
+        const double whole = rint(turns), quarter = rint(4.0 * (turns - whole));
+        const double x = (fma(quarter, -0.25, turns - whole) + low) * 6.28318530717958647693, xx = x * x;
+        double s = fma(xx, -1.0 / 39916800, 1.0 / 362880), c = fma(xx, 1.0 / 479001600, -1.0 / 3628800);
+        s = fma(xx, s, -1.0 / 5040), c = fma(xx, c, 1.0 / 40320);
+        s = fma(xx, s, 1.0 / 120), c = fma(xx, c, -1.0 / 720);
+        s = fma(xx, s, -1.0 / 6), c = fma(xx, c, 1.0 / 24);
+        s = fma(xx * x, s, x), c = fma(xx, fma(xx, c, -0.5), 1.0);
+        const int q = int(quarter);                    // -2 to 2
+        const double cq = q & 1 ? s : c, sq = q & 1 ? c : s;       // a quarter on: cos -> -sin, sin -> cos
+        const double m = a.amplitude;
+        table[i] = make_float2(float((q + 1) & 2 ? -m * cq : m * cq), float(q & 2 ? -m * sq : m * sq));
     }
     __syncthreads();
 }

@@ -465,7 +465,7 @@ struct ManyArgs {
     const float *totals;            // sums of x over groups, 4 at a time: [groups / 4][T][4]
     float *parts;                   // of the tiles that are cut: [tile][split][tile's values]
     int m_tiles, tiles, whole;      // the first `whole` tiles are not cut
-    int splits, share;              // blocks of a share, a multiple of 4
+    int splits, share;              // blocks of a share
 };
 
 // Keeps the additions where they stand: put off, as they may be for all of a loop's body, they leave the products of
@@ -504,7 +504,7 @@ __device__ __forceinline__ void finish(const ManyArgs &m, floatx4 (&sum)[kManyR]
         for (int f = 0; f < AHEAD; ++f) {              // lane quarter q: group g0 + 4 f + q
             const int g = g0 + 4 * f + quarter;
             const bool there = g < g_last;
-            const float *from = m.totals + (there ? int64_t(g >> 2) * a.T * 4 + quarter : 0);
+            const float *from = m.totals + (there ? int64_t(g >> 2) * a.T * 4 + (g & 3) : 0);
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt) sum_x[f][tt] = from[min(t0 + 16 * tt + col, a.T - 1) * 4];
 #pragma unroll
@@ -849,30 +849,37 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
         return p;
     }
     // linear_some reads the weights once for every tile of tokens, linear_many is two or three launches.  us, some and
-    // many: bf16 rows through 4096 x 4096 (17 million codes), 32: 7.9 and 18.6, 96: 16.5 and 28.5, 192: 28.2 and 28.8;
-    // through 16384 x 4096, 32: 15.8 and 22.5, 48: 27.9 and 23.1; through 512 x 2048, 192: 5.6 and 19.7; fp32 rows through
-    // 4096 x 4096, 16: 9.5 and 25.8, 48: 25.1 and 27.3, 64: 32.3 and 27.9; through 16384 x 4096, 16: 20.1 and 34.4, 24: 37.9
-    // and 34.6; through 4096 x 14336, 16: 26.6 and 36.4, 24: 50.4 and 36.7.
+    // many: bf16 rows through 4096 x 4096 (17 million codes), 32: 8.0 and 22.4, 96: 15.8 and 23.9, 192: 25.9 and 25.4;
+    // through 16384 x 4096, 32: 15.7 and 22.2, 48: 27.6 and 22.9; through 512 x 2048, 192: 5.4 and 17.5; fp32 rows through
+    // 4096 x 4096, 16: 9.5 and 26.9, 48: 23.4 and 27.1, 64: 30.1 and 26.6; through 16384 x 4096, 16: 20.0 and 34.4, 24: 37.5
+    // and 35.3; through 4096 x 14336, 16: 26.1 and 34.8, 24: 49.2 and 35.5.
     const int tokens = pieces == 3 ? 16 : 32;          // of a tile of linear_some
     const int token_tiles = (T + tokens - 1) / tokens;
-    p.kind = token_tiles == 1 || (int64_t(token_tiles) * N * K <= (pieces == 3 ? 50000000 : 110000000) && token_tiles <= kGridY)
+    p.kind = token_tiles == 1 || (int64_t(token_tiles) * N * K <= (pieces == 3 ? 52000000 : 110000000) && token_tiles <= kGridY)
                  ? Plan::kSome
                  : Plan::kMany;
     if (p.kind == Plan::kSome) return p;
     p.pieces = up256(size_t(pieces) * T * Kp * 2);
     p.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
-    p.tt = T <= 64 ? 4 : 8;
-    p.m_tiles = (T + 16 * p.tt - 1) / (16 * p.tt);
-    p.tiles = p.m_tiles * ((N + kManyRows - 1) / kManyRows);
-    p.whole = p.tiles / kManySlots * kManySlots;
-    const int rest = p.tiles - p.whole, fours = (blocks + 3) / 4;
-    p.splits = 1;
-    p.share = fours * 4;
-    if (rest > 0) {
-        const int want = std::min(kManySlots / rest, fours);
-        p.share = (fours + want - 1) / want * 4;
-        p.splits = (blocks + p.share - 1) / p.share;
-        if (p.splits > 1) p.parts = size_t(rest) * p.splits * (16 * p.tt * kManyRows * 4);
+    // Tiles of 64 or 128 tokens, and into how many shares the last of them are cut: the least estimate, in us, of the
+    // steps of a CU and of the shares' way through memory and their launch.  A step takes 1.2 and 2.1 us.  Whole calls of
+    // bf16 rows, us, 64 and 128: 100 x 4096 x 4096 24.1 and 27.6, 512 x 6144 x 4096 42.5 and 46.0, 400 x 14336 x 4096 91.2 and
+    // 79.5, 8192 x 6144 x 4096 491 and 443; 85 x 14853 x 328 12.9 uncut and 21.5 in three shares.
+    double least = 0;
+    for (const int tt : {4, 8}) {
+        const int m_tiles = (T + 16 * tt - 1) / (16 * tt), tiles = m_tiles * ((N + kManyRows - 1) / kManyRows);
+        const int whole = tiles / kManySlots * kManySlots, rest = tiles - whole;
+        const int most = rest > 0 ? std::min(kManySlots / rest, blocks) : 1;
+        for (const int want : {most, most / 2, 1}) {
+            if (want < 1) continue;
+            const int share = (blocks + want - 1) / want, splits = (blocks + share - 1) / share;
+            const size_t parts = splits > 1 ? size_t(rest) * splits * (16 * tt * kManyRows * 4) : 0;
+            const double steps = (double(whole / kManySlots) * blocks + (rest > 0 ? share : 0)) * pieces;
+            const double us = steps * (tt == 4 ? 1.2 : 2.1) + (parts > 0 ? 1.5 + double(parts) / 4e6 : 0);
+            if (least > 0 && us >= least) continue;
+            least = us;
+            p.tt = tt, p.m_tiles = m_tiles, p.tiles = tiles, p.whole = whole, p.splits = splits, p.share = share, p.parts = parts;
+        }
     }
     return p;
 }

@@ -187,6 +187,8 @@ LARGE = [
     (1700, 4001, 392, 64, "fp32", "bf16", True, True, 0),
     (800, 255, 20000, 64, "bf16", "fp32", False, False, 0), (3000, 60, 24000, 128, "bf16", "bf16", False, True, 0),
     (70000, 250, 232, 64, "bf16", "bf16", False, False, 0),       # many tiles of few steps
+    (2300, 4100, 1160, 32, "fp32", "bf16", True, True, 8), (1150, 5051, 776, 64, "bf16", "bf16", True, True, 8),
+    (2200, 6100, 2600, 64, "bf16", "fp32", False, True, 0), (8190, 600, 2056, 32, "bf16", "bf16", True, False, 0),
     (1 << 20, 5, 40, 32, "fp32", "fp32", False, False, 0),        # the most rows, more tiles than a launch has in y
 ]
 

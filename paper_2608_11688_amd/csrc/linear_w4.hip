@@ -33,6 +33,7 @@ struct LinearArgs {
     int N, T, blocks;               // blocks of kBlock codes in a row
     int pieces;                     // of x: 1 (bf16) or 3 (fp32; in memory where !STAGE)
     bool y32;
+    int ways;                       // of linear_some's wavefronts along K, a power of two
 };
 
 // Codes 2 i and 2 i + 1 of a word as bf16 pairs 16 + q.
@@ -352,7 +353,9 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     const int per = ((a.N + 16 * R - 1) / (16 * R) + 7) / 8;
     const int n0 = ((blockIdx.x & 7) * per + (blockIdx.x >> 3)) * 16 * R;      // as in Walk, one tile each
     if (n0 >= a.N) return;
-    const int t0 = blockIdx.y * 16 * TT;
+    // wavefronts along K, and of tokens the tiles of the others
+    const int ways = a.ways, along = wave & (ways - 1);
+    const int t0 = (blockIdx.y * (kWaves / ways) + wave / ways) * 16 * TT;
     uint4 x[LOADS][PARTS];
     Block<GROUP, R> next;
     // load i of a block: row 4 i + quarter, chunk `col` of 8 values
@@ -372,9 +375,10 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     };
     char *mine = reinterpret_cast<char *>(lds) + wave * (STAGE * 16);
     floatx4 sum[R][TT] = {};
-    load_x(wave);
-    next.load(a, n0, wave, wave < a.blocks, lane);
-    for (int b = wave; b < a.blocks; b += kWaves) {
+    const int first = t0 < a.T ? along : a.blocks;     // none for a tile that is not there
+    load_x(first);
+    next.load(a, n0, first, first < a.blocks, lane);
+    for (int b = first; b < a.blocks; b += ways) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int row = 4 * i + quarter, at = row * 256 + 16 * (col ^ (row & 15));
@@ -390,8 +394,8 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
             }
         }
         const Block<GROUP, R> now = next;
-        load_x(b + kWaves);
-        next.load(a, n0, b + kWaves, b + kWaves < a.blocks, lane);
+        load_x(b + ways);
+        next.load(a, n0, b + ways, b + ways < a.blocks, lane);
         uint32_t words[R][PER];
 #pragma unroll
         for (int r = 0; r < R; ++r) words_of<PER>(now.word[r], words[r]);
@@ -428,20 +432,25 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
             }
         }
     }
+    const auto out = [&](int t, int i, floatx4 v) {        // value i / 64 of lane i % 64
+        put_four(a, t + 16 * ((i >> 6) % TT) + 4 * ((i & 63) >> 4), n0 + 16 * ((i >> 6) / TT) + (i & 15), v);
+    };
+    if (ways == 1) {
+#pragma unroll
+        for (int i = 0; i < R * TT; ++i) out(t0, i * 64 + lane, sum[i / TT][i % TT]);
+        return;
+    }
     __syncthreads();
     floatx4 *part = reinterpret_cast<floatx4 *>(lds);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt) part[wave * OUT + (r * TT + tt) * 64 + lane] = sum[r][tt];
+    for (int i = 0; i < R * TT; ++i) part[wave * OUT + i * 64 + lane] = sum[i / TT][i % TT];
     __syncthreads();
-    const int e = threadIdx.x;
-    if (e < OUT) {
-        floatx4 v = part[e];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += part[w * OUT + e];
-        const int at = e & 63, tt = (e >> 6) % TT, r = (e >> 6) / TT;
-        put_four(a, t0 + 16 * tt + 4 * (at >> 4), n0 + 16 * r + (at & 15), v);
+    for (int e = along * 64 + lane; e < OUT; e += ways * 64) {
+        const floatx4 *from = part + (wave - along) * OUT + e;
+        floatx4 v = from[0];
+#pragma unroll 1
+        for (int w = 1; w < ways; ++w) v += from[w * OUT];
+        out(t0, e, v);
     }
 }
 
@@ -790,9 +799,9 @@ void launch_few(const LinearArgs &a, hipStream_t st) {
 
 template <int GROUP, int R, int TT, int P>
 void launch_some(const LinearArgs &a, hipStream_t st) {
-    const int tiles = (a.N + 16 * R - 1) / (16 * R);
-    hipLaunchKernelGGL((linear_some<GROUP, R, TT, P>), dim3((tiles + 7) / 8 * 8, (a.T + 16 * TT - 1) / (16 * TT)),
-                       dim3(64 * kWaves), 0, st, a);
+    const int tiles = (a.N + 16 * R - 1) / (16 * R), tokens = 16 * TT * (kWaves / a.ways);
+    hipLaunchKernelGGL((linear_some<GROUP, R, TT, P>), dim3((tiles + 7) / 8 * 8, (a.T + tokens - 1) / tokens), dim3(64 * kWaves),
+                       0, st, a);
 }
 
 template <int GROUP, int TT>
@@ -809,62 +818,48 @@ void launch_many(const ManyArgs &m, int tt, hipStream_t st) {
     tt == 4 ? launch_many<GROUP, 4>(m, st) : launch_many<GROUP, 8>(m, st);
 }
 
-// Rows of the weights a workgroup takes: 16 while that leaves it a CU of its own, else 32.
-bool narrow(int N) { return N <= 16 * 256; }
-
-template <int GROUP, int R>
-void launch(const LinearArgs &a, bool stage, Rows rows, hipStream_t st) {
-    if (stage)
-        rows == kFew ? launch_few<GROUP, R, kFew>(a, st) : launch_few<GROUP, R, kPieces>(a, st);
-    else if (a.pieces == 3)
-        launch_some<GROUP, R, 1, 3>(a, st);
-    else
-        a.T <= 16 ? launch_some<GROUP, R, 1, 1>(a, st) : launch_some<GROUP, R, 2, 1>(a, st);
-}
-
-template <int GROUP>
-void launch(const LinearArgs &a, bool stage, Rows rows, hipStream_t st) {
-    narrow(a.N) ? launch<GROUP, 1>(a, stage, rows, st) : launch<GROUP, 2>(a, stage, rows, st);
-}
-
 bool is_type(int t) { return t == APEX_TYPE_FP32 || t == APEX_TYPE_BF16; }
 
 // How a call is worked on.
 struct Plan {
     enum { kStaged, kSome, kMany } kind;
     Rows rows;                       // kStaged
+    int r, ways;                     // kStaged and kSome: 16 r rows of the weights a workgroup; kSome: wavefronts along K
     int tt, m_tiles, tiles, whole, splits, share;     // kMany
     size_t pieces, totals, parts;    // bytes of the workspace, in this order
     size_t bytes() const { return pieces + totals + parts; }
 };
 
+constexpr int kCUs = 256;
 constexpr int kGridY = 65535;        // of a launch
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-Plan plan_of(int T, int N, int K, int group, int pieces) {
-    Plan p{};
-    const int Kp = padded(K), blocks = Kp / kBlock;
-    if (stages(T, K, pieces, &p.rows)) {
-        p.kind = Plan::kStaged;
-        return p;
-    }
-    // linear_some reads the weights once for every tile of tokens, linear_many is two or three launches.  us, some and
-    // many: bf16 rows through 4096 x 4096 (17 million codes), 32: 8.0 and 22.4, 96: 15.8 and 23.9, 192: 25.9 and 25.4;
-    // through 16384 x 4096, 32: 15.7 and 22.2, 48: 27.6 and 22.9; through 512 x 2048, 192: 5.4 and 17.5; fp32 rows through
-    // 4096 x 4096, 16: 9.5 and 26.9, 48: 23.4 and 27.1, 64: 30.1 and 26.6; through 16384 x 4096, 16: 20.0 and 34.4, 24: 37.5
-    // and 35.3; through 4096 x 14336, 16: 26.1 and 34.8, 24: 49.2 and 35.5.
-    const int tokens = pieces == 3 ? 16 : 32;          // of a tile of linear_some
-    const int token_tiles = (T + tokens - 1) / tokens;
-    p.kind = token_tiles == 1 || (int64_t(token_tiles) * N * K <= (pieces == 3 ? 52000000 : 110000000) && token_tiles <= kGridY)
-                 ? Plan::kSome
-                 : Plan::kMany;
-    if (p.kind == Plan::kSome) return p;
-    p.pieces = up256(size_t(pieces) * T * Kp * 2);
-    p.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
-    // Tiles of 64 or 128 tokens, and into how many shares the last of them are cut: the least estimate, in us, of the
-    // steps of a CU and of the shares' way through memory and their launch.  A step takes 1.2 and 2.1 us.  Whole calls of
-    // bf16 rows, us, 64 and 128: 100 x 4096 x 4096 24.1 and 27.6, 512 x 6144 x 4096 42.5 and 46.0, 400 x 14336 x 4096 91.2 and
-    // 79.5, 8192 x 6144 x 4096 491 and 443; 85 x 14853 x 328 12.9 uncut and 21.5 in three shares.
+// linear_some: how many of the 8 wavefronts go along K, and whether for 16 or 32 rows of the weights.  Workgroups a CU
+// times the steps of a wavefront and one more for its ends; 32 rows take 1.3 times as long as 16.  us, for 8, 4, 2 and 1
+// along K: 1073 x 1288 x 128, 32 rows: 16.7, 14.3, 8.8, 5.9; 96 x 4096 x 4096, 32 rows: 14.9, 13.8, 22.4, 39.2, 16 rows:
+// 16.9, 18.2, 19.6, 34.1; 64 x 2048 x 2048, 16 rows: 5.6, 6.9, 10.3, 16.9, 32 rows: 6.0, 8.2, 12.7, 20.9.  Returns an
+// estimate of the time in us: a step of 16 and 32 tokens of bf16 takes 0.6 and 1.0, one of 16 of fp32 1.4.
+double plan_some(int T, int N, int blocks, int pieces, Plan &p) {
+    const int tokens = pieces == 1 && T > 16 ? 32 : 16, token_tiles = (T + tokens - 1) / tokens;
+    double least = 0;
+    for (int r = 1; r <= 2; ++r)
+        for (int ways = kWaves; ways >= 1; ways /= 2) {
+            const int each = kWaves / ways;
+            const int64_t groups = int64_t((N + 16 * r - 1) / (16 * r)) * ((token_tiles + each - 1) / each);
+            const double cost = double((groups + kCUs - 1) / kCUs) * ((blocks + ways - 1) / ways + 1) * (r == 1 ? 1.0 : 1.3);
+            if (least > 0 && cost >= least) continue;
+            least = cost;
+            p.r = r, p.ways = ways;
+        }
+    return 2.5 + least * (pieces == 3 ? 1.4 : tokens == 16 ? 0.6 : 1.0);
+}
+
+// linear_many: tiles of 64 or 128 tokens, and into how many shares the last of them are cut, by the steps of a CU, 1.2 and
+// 2.1 us each, and the shares' way through memory and their launch.  Whole calls of bf16 rows, us, 64 and 128: 100 x 4096 x
+// 4096 24.1 and 27.6, 512 x 6144 x 4096 42.5 and 46.0, 400 x 14336 x 4096 91.2 and 79.5, 8192 x 6144 x 4096 491 and 443;
+// 85 x 14853 x 328 12.9 uncut and 21.5 in three shares.  Returns an estimate of the time in us, with x's way through
+// memory and two launches.
+double plan_many(int T, int N, int blocks, int pieces, Plan &p) {
     double least = 0;
     for (const int tt : {4, 8}) {
         const int m_tiles = (T + 16 * tt - 1) / (16 * tt), tiles = m_tiles * ((N + kManyRows - 1) / kManyRows);
@@ -875,13 +870,53 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
             const int share = (blocks + want - 1) / want, splits = (blocks + share - 1) / share;
             const size_t parts = splits > 1 ? size_t(rest) * splits * (16 * tt * kManyRows * 4) : 0;
             const double steps = (double(whole / kManySlots) * blocks + (rest > 0 ? share : 0)) * pieces;
-            const double us = steps * (tt == 4 ? 1.2 : 2.1) + (parts > 0 ? 1.5 + double(parts) / 4e6 : 0);
+            const double us = steps * (tt == 4 ? 1.2 : 2.1) + (parts > 0 ? 3 + double(parts) / 4e6 : 0);
             if (least > 0 && us >= least) continue;
             least = us;
             p.tt = tt, p.m_tiles = m_tiles, p.tiles = tiles, p.whole = whole, p.splits = splits, p.share = share, p.parts = parts;
         }
     }
-    return p;
+    return 8 + least + double(T) * blocks * kBlock * (pieces == 3 ? 10 : 4) / 4.5e6;
+}
+
+// Up to 32 rows of bf16 and 16 of fp32, a tile of linear_some, take no workspace.  Of more rows linear_some reads the
+// weights once for every tile, linear_many is two or three launches; us, some and many: bf16 rows, 239 x 12103 x 1312
+// 30.7 and 21.7, 45 x 14783 x 2728 20.1 and 22.7, 249 x 3266 x 3736 25.9 and 28.0, 56 x 854 x 7008 10.0 and 32.5; fp32 rows,
+// 298 x 669 x 3328 17.7 and 28.6, 24 x 8081 x 5120 22.5 and 30.0, 301 x 1361 x 5976 54.6 and 38.6, 104 x 69 x 3200 8.1 and
+// 21.1.  Of 69 calls of mixed sizes the estimates took the slower way three times, by 0.6 us at most.
+Plan plan_of(int T, int N, int K, int group, int pieces) {
+    Plan p{};
+    const int Kp = padded(K), blocks = Kp / kBlock;
+    if (stages(T, K, pieces, &p.rows)) {
+        p.kind = Plan::kStaged;
+        p.r = N <= 16 * kCUs ? 1 : 2;                  // 16 rows while that leaves a workgroup a CU of its own
+        return p;
+    }
+    p.kind = Plan::kSome;
+    const double some = plan_some(T, N, blocks, pieces, p);
+    const int tokens = pieces == 3 ? 16 : 32, token_tiles = (T + tokens - 1) / tokens;
+    if (token_tiles == 1) return p;
+    Plan m{};
+    m.kind = Plan::kMany;
+    if (some <= plan_many(T, N, blocks, pieces, m) && token_tiles <= kGridY) return p;
+    m.pieces = up256(size_t(pieces) * T * Kp * 2);
+    m.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
+    return m;
+}
+
+template <int GROUP, int R>
+void launch(const LinearArgs &a, const Plan &p, hipStream_t st) {
+    if (p.kind == Plan::kStaged)
+        p.rows == kFew ? launch_few<GROUP, R, kFew>(a, st) : launch_few<GROUP, R, kPieces>(a, st);
+    else if (a.pieces == 3)
+        launch_some<GROUP, R, 1, 3>(a, st);
+    else
+        a.T <= 16 ? launch_some<GROUP, R, 1, 1>(a, st) : launch_some<GROUP, R, 2, 1>(a, st);
+}
+
+template <int GROUP>
+void launch(const LinearArgs &a, const Plan &p, hipStream_t st) {
+    p.r == 1 ? launch<GROUP, 1>(a, p, st) : launch<GROUP, 2>(a, p, st);
 }
 
 }  // namespace
@@ -922,7 +957,7 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
                  static_cast<const uint16_t *>(x), x_stride, 0, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
-                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32};
+                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32, plan.ways};
     if (plan.kind == Plan::kMany) {
         char *ws = static_cast<char *>(workspace);
         float *totals = reinterpret_cast<float *>(ws + plan.pieces);
@@ -942,10 +977,7 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         group == 32 ? launch_many<32>(m, plan.tt, stream) : group == 64 ? launch_many<64>(m, plan.tt, stream)
                                                                         : launch_many<128>(m, plan.tt, stream);
     } else {
-        const bool stage = plan.kind == Plan::kStaged;
-        group == 32   ? launch<32>(a, stage, plan.rows, stream)
-        : group == 64 ? launch<64>(a, stage, plan.rows, stream)
-                      : launch<128>(a, stage, plan.rows, stream);
+        group == 32 ? launch<32>(a, plan, stream) : group == 64 ? launch<64>(a, plan, stream) : launch<128>(a, plan, stream);
     }
     APEX_HIP(hipGetLastError());
     return APEX_OK;

@@ -144,7 +144,7 @@ class Large:
         self.r = torch.randn(T, N + extra, generator=gen, device="cuda").to(types[y]) if residual else None
         self.y = torch.full((T, N + extra), 7.0, dtype=types[y], device="cuda")
         need = native.apex_linear_w4_workspace_bytes(T, N, K, group, x)
-        assert need > 2 * T * Kp                       # x in the order of the tiles, and more
+        self.in_tiles = need > 2 * T * Kp              # x in the order of the tiles, and more
         self.ws = torch.full((need + 64,), 0xAB, dtype=torch.uint8, device="cuda")
 
     def call(self, stream=None):
@@ -178,24 +178,43 @@ class Large:
 # T, N, K, group, types of x and y, bias, residual, extra values in a row
 LARGE = [
     (33, 7000, 8136, 128, "bf16", "bf16", False, False, 0), (64, 14337, 4096, 32, "bf16", "fp32", True, True, 8),
-    (63, 9000, 6912, 64, "bf16", "bf16", True, False, 16), (65, 4999, 7688, 32, "bf16", "bf16", False, True, 0),
-    (17, 5000, 5400, 64, "fp32", "fp32", False, True, 0), (48, 3333, 6016, 128, "fp32", "bf16", True, False, 8),
-    (100, 2052, 3840, 32, "fp32", "fp32", True, True, 0), (129, 3001, 7936, 128, "bf16", "fp32", False, False, 0),
+    (63, 9000, 6912, 64, "bf16", "bf16", True, False, 16), (65, 14999, 7688, 32, "bf16", "bf16", False, True, 0),
+    (33, 25000, 5400, 64, "fp32", "fp32", False, True, 0), (48, 3333, 6016, 128, "fp32", "bf16", True, False, 8),
+    (100, 6052, 3840, 32, "fp32", "fp32", True, True, 0), (129, 9001, 7936, 128, "bf16", "fp32", False, False, 0),
     (300, 2816, 4104, 64, "bf16", "bf16", True, True, 8), (513, 5121, 1416, 128, "bf16", "bf16", False, True, 0),
     (2050, 4100, 520, 32, "bf16", "fp32", False, False, 0),       # more tiles than a round, shares behind it
     (2048, 4096, 512, 128, "bf16", "bf16", False, False, 0),      # a round of whole tiles and nothing behind it
     (1700, 4001, 392, 64, "fp32", "bf16", True, True, 0),
-    (800, 255, 20000, 64, "bf16", "fp32", False, False, 0), (3000, 60, 24000, 128, "bf16", "bf16", False, True, 0),
+    (1300, 255, 20000, 64, "bf16", "fp32", False, False, 0), (4000, 600, 24000, 128, "bf16", "bf16", False, True, 0),
     (70000, 250, 232, 64, "bf16", "bf16", False, False, 0),       # many tiles of few steps
     (2300, 4100, 1160, 32, "fp32", "bf16", True, True, 8), (1150, 5051, 776, 64, "bf16", "bf16", True, True, 8),
     (2200, 6100, 2600, 64, "bf16", "fp32", False, True, 0), (8190, 600, 2056, 32, "bf16", "bf16", True, False, 0),
     (1 << 20, 5, 40, 32, "fp32", "fp32", False, False, 0),        # the most rows, more tiles than a launch has in y
 ]
+# tiles of wavefronts: more rows than one tile, with 1 to 8 wavefronts along K
+SOME = [
+    (65, 4999, 7688, 32, "bf16", "bf16", False, True, 0), (17, 5000, 5400, 64, "fp32", "fp32", False, True, 0),
+    (100, 2052, 3840, 32, "fp32", "fp32", True, True, 0), (129, 3001, 7936, 128, "bf16", "fp32", False, False, 0),
+    (800, 255, 20000, 64, "bf16", "fp32", False, False, 0), (3000, 60, 24000, 128, "bf16", "bf16", False, True, 0),
+    (1073, 1288, 128, 32, "bf16", "fp32", True, True, 8), (2001, 510, 256, 64, "bf16", "bf16", False, True, 0),
+    (353, 4099, 232, 128, "bf16", "bf16", False, False, 8), (901, 803, 160, 32, "fp32", "fp32", True, True, 0),
+    (399, 600, 1000, 64, "fp32", "bf16", False, False, 0), (100, 5000, 128, 128, "fp32", "fp32", False, True, 0),
+    (9999, 40, 520, 32, "bf16", "fp32", True, False, 0), (86, 22171, 256, 128, "bf16", "bf16", False, True, 0),
+]
 
 
 @pytest.mark.parametrize("case", LARGE, ids=[str(c) for c in LARGE])
 def test_products_in_tiles(torch, case):
-    print(Large(torch, *case, seed=case[0]).check())
+    c = Large(torch, *case, seed=case[0])
+    assert c.in_tiles
+    print(c.check())
+
+
+@pytest.mark.parametrize("case", SOME, ids=[str(c) for c in SOME])
+def test_tiles_of_wavefronts(torch, case):
+    c = Large(torch, *case, seed=case[0])
+    assert not c.in_tiles
+    print(c.check())
 
 
 @pytest.mark.parametrize("case", [LARGE[1], LARGE[6], LARGE[8], LARGE[10]], ids=str)

@@ -159,7 +159,7 @@ def test_null_cache_or_rotation():
 
 
 # ------------------------------------------------------------------------------ projection
-LARGE = dict(xt="fp32", T=64, N=8192, K=8192, xs=8192, ys=8192, rs=8192)       # needs a workspace
+LARGE = dict(xt="fp32", T=256, N=8192, K=8192, xs=8192, ys=8192, rs=8192)       # needs a workspace
 
 
 def project(**kw):
@@ -177,7 +177,7 @@ def project(**kw):
     (INVAL, dict(y=A + 8)), (INVAL, dict(bias=A + 4)), (INVAL, dict(r=A + 2)), (INVAL, dict(ws=A + 8)),
     (INVAL, dict(r=2 * A, rs=200)), (INVAL, dict(N=(1 << 24) + 1, ys=1 << 25, rs=1 << 25)),
     (INVAL, dict(K=(1 << 20) + 8, xs=1 << 21)), (INVAL, dict(LARGE, ws=None)), (CAPACITY, dict(LARGE, n=1024)),
-    (CAPACITY, dict(LARGE, xt="bf16", n=64 * 8192 * 2))], ids=str)
+    (CAPACITY, dict(LARGE, xt="bf16", n=256 * 8192 * 2))], ids=str)
 def test_linear_refuses(status, kw):
     refused(status, project, **kw)
 
@@ -194,6 +194,6 @@ def test_linear_workspace():
     for T in (1, 100, 5000):
         assert f(T, 96, 256, 64, "fp32") <= (T + 256) * 256 * 2 * 4 + (1 << 20)
         assert f(T, 96, 256, 64, "bf16") <= (T + 256) * 256 * 2 * 2 + (1 << 20)
-    assert 64 * 8192 * 6 < f(64, 8192, 8192, 64, "fp32") < (1 << 28)
-    assert 64 * 8192 * 2 < f(64, 8192, 8192, 64, "bf16") < (1 << 28)
+    assert 256 * 8192 * 6 < f(256, 8192, 8192, 64, "fp32") < (1 << 28)
+    assert 256 * 8192 * 2 < f(256, 8192, 8192, 64, "bf16") < (1 << 28)
     assert f(1, 1 << 20, 1 << 20, 32, "bf16") == 0             # single rows take none

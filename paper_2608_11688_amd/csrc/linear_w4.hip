@@ -82,23 +82,8 @@ __device__ __forceinline__ void put(const LinearArgs &a, int64_t t, int n, float
     store_y(a.y32, a.y, t * a.y_stride + n, y);
 }
 
-// A lane's values of row n of the weights and 4 tokens from t on.  4 lanes (n a multiple of 4 in the first) first trade
-// places, so that each has 4 values of one token, side by side; rows may begin at any value.
-template <int CTRL>
-__device__ __forceinline__ float quad(float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
-}
-__device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, floatx4 v) {
-    // lane l of the four, value i -> lane i, value l: by halves (l ^ 2 and i ^ 2), then by ones
-    const int l = threadIdx.x & 3;
-    const float p0 = quad<0x4e>(l & 2 ? v[0] : v[2]), p1 = quad<0x4e>(l & 2 ? v[1] : v[3]);
-    if (l & 2) v[0] = p0, v[1] = p1;
-    else v[2] = p0, v[3] = p1;
-    const float q0 = quad<0xb1>(l & 1 ? v[0] : v[1]), q1 = quad<0xb1>(l & 1 ? v[2] : v[3]);
-    if (l & 1) v[0] = q0, v[2] = q1;
-    else v[1] = q0, v[3] = q1;
-    t += l;
-    n -= l;
+// Four values of one token from row n of the weights on; rows of y and of the residual may begin at any value.
+__device__ __forceinline__ void put_row(const LinearArgs &a, int64_t t, int n, floatx4 v) {
     if (t >= a.T || n >= a.N) return;
     if (n + 4 > a.N) {                                 // the last values of a row
 #pragma unroll
@@ -131,6 +116,26 @@ __device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, 
         for (int i = 0; i < 4; ++i) y[i] = static_cast<__bf16>(v[i]);
         __builtin_memcpy(static_cast<uint16_t *>(a.y) + to, &y, 8);
     }
+}
+
+// A lane's values of row n of the weights and 4 tokens from t on.  4 lanes (n a multiple of 4 in the first) first trade
+// places, so that each has 4 values of one token, side by side.
+template <int CTRL>
+__device__ __forceinline__ float quad(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ void put_four(const LinearArgs &a, int64_t t, int n, floatx4 v) {
+    // lane l of the four, value i -> lane i, value l: by halves (l ^ 2 and i ^ 2), then by ones
+    const int l = threadIdx.x & 3;
+    const float p0 = quad<0x4e>(l & 2 ? v[0] : v[2]), p1 = quad<0x4e>(l & 2 ? v[1] : v[3]);
+    if (l & 2) v[0] = p0, v[1] = p1;
+    else v[2] = p0, v[3] = p1;
+    const float q0 = quad<0xb1>(l & 1 ? v[0] : v[1]), q1 = quad<0xb1>(l & 1 ? v[2] : v[3]);
+    if (l & 1) v[0] = q0, v[2] = q1;
+    else v[1] = q0, v[3] = q1;
+    t += l;
+    n -= l;
+    put_row(a, t, n, v);
 }
 
 // 8 fp32 values as three rows of bf16 pieces whose sum they are: the upper 8 bits of the value, of
@@ -483,66 +488,60 @@ __device__ __forceinline__ void settle(floatx4 &v) { asm volatile("" : "+v"(v));
 
 constexpr int vmcnt_only(int n) { return 0x0f70 | (n & 15) | (n >> 4 << 14); }   // the s_waitcnt operand
 
-// What lane values of the tile stand for: token and row of value i of (r, tt) of a wavefront.
-template <int TT>
-struct Place {
-    int t, n;                       // of i = 0; i counts tokens
-    __device__ __forceinline__ Place(int tile, int m_tiles, int wave, int lane, int r, int tt) {
-        const int n_tile = tile / m_tiles;
-        t = (tile - n_tile * m_tiles) * (16 * TT) + 16 * tt + 4 * (lane >> 4);
-        n = n_tile * kManyRows + wave * (16 * kManyR) + 16 * r + (lane & 15);
-    }
-};
+// A value in three bf16 pieces whose sum it is, at 6 of a lane's 8 places along K of a matrix instruction, in the left
+// and the right operand: the 6 products of pieces that reach the value's 24 bits.
+__device__ __forceinline__ void pieces_of(float v, uint32_t (&p)[3]) {
+    const float rest = v - __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+    p[0] = __float_as_uint(v), p[1] = __float_as_uint(rest);
+    p[2] = __float_as_uint(rest - __uint_as_float(p[1] & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t uppers(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+__device__ __forceinline__ bf16x8 left_pieces(float v) {               // 0 0 0 1 1 2
+    uint32_t p[3];
+    pieces_of(v, p);
+    return __builtin_bit_cast(bf16x8, make_uint4(uppers(p[0], p[0]), uppers(p[0], p[1]), uppers(p[1], p[2]), 0u));
+}
+__device__ __forceinline__ bf16x8 right_pieces(float v) {              // 0 1 2 0 1 0
+    uint32_t p[3];
+    pieces_of(v, p);
+    return __builtin_bit_cast(bf16x8, make_uint4(uppers(p[0], p[1]), uppers(p[2], p[0]), uppers(p[1], p[0]), 0u));
+}
 
-// Of a wavefront of linear_many: the zero points' half of the groups of blocks first .. last - 1 (within the loop, on
-// every fourth block or so, it costs the compiler a second set of registers for the sums), then the results.
-template <int GROUP, int TT>
-__device__ __forceinline__ void finish(const ManyArgs &m, floatx4 (&sum)[kManyR][TT], int lane, int wave, int tile, int rest,
-                                       bool cut_up, int first, int last) {
-    constexpr int PER = kBlock / GROUP, R = kManyR;
-    const LinearArgs &a = m.a;
+// Of a wavefront of linear_many: the zero points' half of up to FOURS fours of groups from `four` on, whose sums of x stand
+// at sum_x, [four][token][4], of the groups first .. last - 1.  Four groups an instruction, group 4 f + q in lane quarter q.
+template <int TT, int FOURS>
+__device__ __forceinline__ void add_zeros(const LinearArgs &a, floatx4 (&sum)[kManyR][TT], const float *sum_x, int lane, int nw,
+                                          int four, int first, int last) {
+    constexpr int R = kManyR, AHEAD = 8;               // fours whose words are on their way at once
     const int col = lane & 15, quarter = lane >> 4;
-    const int n_tile = tile / m.m_tiles, t0 = (tile - n_tile * m.m_tiles) * (16 * TT);
-    const int nw = n_tile * kManyRows + wave * (16 * R);
-    const int g_last = last * PER;
-    constexpr int AHEAD = 4;                           // fours of groups whose values are on their way at once
-    for (int g0 = first * PER; g0 < g_last; g0 += 4 * AHEAD) {
-        float sum_x[AHEAD][TT];
+#pragma unroll 1
+    for (int f0 = 0; f0 < FOURS && 4 * (four + f0) < last; f0 += AHEAD) {
         uint32_t word[AHEAD][R];
 #pragma unroll
-        for (int f = 0; f < AHEAD; ++f) {              // lane quarter q: group g0 + 4 f + q
-            const int g = g0 + 4 * f + quarter;
-            const bool there = g < g_last;
-            const float *from = m.totals + (there ? int64_t(g >> 2) * a.T * 4 + (g & 3) : 0);
+        for (int f = 0; f < AHEAD; ++f) {
+            const int g = 4 * (four + f0 + f) + quarter;
+            const bool there = g >= first && g < last;
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt) sum_x[f][tt] = from[min(t0 + 16 * tt + col, a.T - 1) * 4];
-#pragma unroll
-            for (int r = 0; r < R; ++r) word[f][r] = there ? a.words[int64_t(g) * a.N + min(nw + 16 * r + col, a.N - 1)] : 0u;
+            for (int r = 0; r < R; ++r)
+                word[f][r] = there ? a.words[int64_t(g) * a.N + min(nw + 16 * r + col, a.N - 1)] : 0u;
         }
 #pragma unroll
         for (int f = 0; f < AHEAD; ++f) {
-            if (g0 + 4 * f >= g_last) break;
+            if (4 * (four + f0 + f) >= last) break;
+            bf16x8 c[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const Scale of(word[f][r]);
-                const float c = -(of.s * of.z);
+                c[r] = right_pieces(-(of.s * of.z));
+            }
 #pragma unroll
-                for (int tt = 0; tt < TT; ++tt) sum[r][tt] = __builtin_amdgcn_mfma_f32_16x16x4f32(sum_x[f][tt], c, sum[r][tt], 0, 0, 0);
+            for (int tt = 0; tt < TT; ++tt) {
+                const bf16x8 v = left_pieces(sum_x[((f0 + f) * (16 * TT) + 16 * tt + col) * 4 + quarter]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) sum[r][tt] = mfma(v, c[r], sum[r][tt]);
             }
         }
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt) {
-            if (cut_up) {
-                floatx4 *to = reinterpret_cast<floatx4 *>(m.parts) + int64_t(rest) * (16 * TT * kManyRows / 4);
-                to[((wave * R + r) * TT + tt) * 64 + lane] = sum[r][tt];
-                continue;
-            }
-            const Place<TT> at(tile, m.m_tiles, wave, lane, r, tt);
-            put_four(a, at.t, at.n, sum[r][tt]);
-        }
 }
 
 template <int GROUP, int TT>
@@ -551,6 +550,7 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int XLOADS = BM / 32, WLOADS = 2;        // of a wavefront a step: 4 rows of x, 16 rows of codes each
     __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * 256], x1[BM * 256], x2[BM * 256];
     __shared__ __attribute__((aligned(1024))) uint8_t w0[kManyRows * 64], w1[kManyRows * 64], w2[kManyRows * 64];
+    __shared__ __attribute__((aligned(1024))) uint8_t sums[16384];     // of x, the first groups'
     const LinearArgs &a = m.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
@@ -688,6 +688,22 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
             }
         }
     };
+    // sums of x over groups, FOURS fours of them to 16 KiB: [four][token][4]; behind the last ones nothing
+    constexpr int FOURS = 1024 / BM;
+    const int g_first = first * PER, g_last = last * PER;
+    const auto load_sums = [&](uint8_t *to, int chunk) {
+        const int four = g_first / 4 + chunk * FOURS;
+        const int64_t left = int64_t((a.blocks * PER + 3) / 4 - four) * a.T - t0;      // tokens' fours
+        const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(m.totals + (left > 0 ? (int64_t(four) * a.T + t0) * 4 : 0)),
+                                                            0, int(min(max(left, int64_t(0)), int64_t(1) << 26)) * 16, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int u = wave * 128 + i * 64 + lane;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (APEX_LDS void *)(to + (wave * 128 + i * 64) * 16), 16,
+                                                     (u / BM * a.T + u % BM) * 16, 0, 0, 0);
+        }
+    };
+    load_sums(sums, 0);
     load_words(word_next);
     load(x0, w0);
     load(x1, w1);
@@ -714,20 +730,80 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     // before the loop
     int lane_after = lane;
     asm volatile("" : "+v"(lane_after));
-    finish<GROUP, TT>(m, sum, lane_after, wave, tile, rest, cut_up, first, last);
+    __syncthreads();                                   // the stages have been read: they take the sums that are left
+    {
+        constexpr int BUFFERS = TT == 8 ? 7 : 4;
+        const auto buffer = [&](int i) {
+            if (i == 0) return sums;
+            if (TT == 4) return i == 1 ? x0 : i == 2 ? x1 : x2;
+            return (i < 3 ? x0 : i < 5 ? x1 : x2) + (i & 1 ? 0 : 16384);
+        };
+        const int chunks = (g_last - g_first / 4 * 4 + 4 * FOURS - 1) / (4 * FOURS);
+        const auto add_chunk = [&](int i, int chunk) {
+            add_zeros<TT, FOURS>(a, sum, reinterpret_cast<const float *>(buffer(i)), lane_after, nw, g_first / 4 + chunk * FOURS,
+                                 g_first, g_last);
+        };
+        for (int i = 1; i < min(BUFFERS, chunks); ++i) load_sums(buffer(i), i);
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            const int i = chunk % BUFFERS;
+            if (chunk > 0 && i == 0) {                 // all of them have been used
+                __syncthreads();
+                for (int j = 0; j < min(BUFFERS, chunks - chunk); ++j) load_sums(buffer(j), chunk + j);
+            }
+            if (chunk == 1 || (chunk > 0 && i == 0)) {
+                __builtin_amdgcn_s_waitcnt(0x0f70);
+                __syncthreads();
+            }
+            add_chunk(i, chunk);
+        }
+    }
+    if (cut_up) {
+        floatx4 *to = reinterpret_cast<floatx4 *>(m.parts) + int64_t(rest) * (BM * kManyRows / 4) + lane_after;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt) to[((wave * R + r) * TT + tt) * 64] = sum[r][tt];
+        return;
+    }
+    // results by way of LDS, a token's 256 values side by side; 16 tokens in the place of 16 KiB of a stage, rows of 4
+    // tokens 16 banks apart
+    const auto place = [&](int tt) {
+        uint8_t *at = TT == 4 ? (tt == 0 ? x0 : tt == 1 ? x1 : tt == 2 ? x2 : w0)
+                              : (tt < 2 ? x0 : tt < 4 ? x1 : tt < 6 ? x2 : tt == 6 ? w0 : w1);
+        return reinterpret_cast<float *>(at + (TT == 8 && tt < 6 ? (tt & 1) * 16384 : 0));
+    };
+    const int col_after = lane_after & 15, quarter_after = lane_after >> 4;
+    __syncthreads();                                   // the last stage has been read
+#pragma unroll
+    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                place(tt)[(4 * quarter_after + i) * 256 + ((wave * 32 + 16 * r + col_after) ^ (16 * quarter_after))] = sum[r][tt][i];
+    __syncthreads();
+    constexpr int ROWS = BM / 8;                       // tokens of a wavefront, within one of those places
+    const float *mine_out = place(wave * ROWS / 16) + wave * ROWS % 16 * 256;
+#pragma unroll 4
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = wave * ROWS % 16 + i, t = t0 + wave * ROWS + i;
+        const floatx4 v = *reinterpret_cast<const floatx4 *>(mine_out + i * 256 + ((4 * lane_after) ^ (16 * (row >> 2))));
+        if (t < a.T && n0 + 4 * lane_after < a.N) put_row(a, t, n0 + 4 * lane_after, v);
+    }
 }
 
-// The shares of the tiles that were cut, in order.
+// The shares of the tiles that were cut, in order.  A workgroup takes 4 tokens, its threads a row of the weights each.
 template <int TT>
-__global__ __launch_bounds__(256) void join(ManyArgs m) {
-    constexpr int values = 16 * TT * kManyRows / 4, R = kManyR;       // of 4 tokens
-    const int rest = blockIdx.x / (values / 256), e = blockIdx.x % (values / 256) * 256 + threadIdx.x;
-    const floatx4 *from = reinterpret_cast<const floatx4 *>(m.parts) + int64_t(rest) * m.splits * values + e;
+__global__ __launch_bounds__(kManyRows) void join(ManyArgs m) {
+    constexpr int values = 16 * TT * kManyRows / 4;    // of 4 tokens
+    const int rest = blockIdx.x / (4 * TT), tt = blockIdx.x % (4 * TT) / 4, quarter = blockIdx.x % 4, n = threadIdx.x;
+    const floatx4 *from = reinterpret_cast<const floatx4 *>(m.parts) + int64_t(rest) * m.splits * values +
+                          ((n / 16 * TT + tt) * 64 + 16 * quarter + n % 16);
     floatx4 v = from[0];
+#pragma unroll 4
     for (int s = 1; s < m.splits; ++s) v += from[int64_t(s) * values];
-    const int lane = e & 63, tt = (e >> 6) % TT, r = (e >> 6) / TT % R, wave = (e >> 6) / TT / R;
-    const Place<TT> at(m.whole + rest, m.m_tiles, wave, lane, r, tt);
-    put_four(m.a, at.t, at.n, v);
+    const int tile = m.whole + rest, n_tile = tile / m.m_tiles;
+    put_four(m.a, (tile - n_tile * m.m_tiles) * (16 * TT) + 16 * tt + 4 * quarter, n_tile * kManyRows + n, v);
 }
 
 // Sums of x over groups of GROUP values, [groups / 4][T][4], and x as bf16 (PIECES: fp32 values as three pieces)
@@ -771,7 +847,10 @@ __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int
         s += __shfl_xor(s, 2);
         if constexpr (GROUP >= 64) s += __shfl_xor(s, 4);
         if constexpr (GROUP >= 128) s += __shfl_xor(s, 8);
-        if (k % GROUP == 0) totals[(int64_t(k / GROUP / 4) * T + t) * 4 + k / GROUP % 4] = s;
+        const int g = k / GROUP;
+        if (k % GROUP == 0) totals[(int64_t(g / 4) * T + t) * 4 + g % 4] = s;
+        if (k == Kp - 8)                               // the places behind the last group
+            for (int e = g % 4 + 1; e < 4; ++e) totals[(int64_t(g / 4) * T + t) * 4 + e] = 0.f;
     }
 }
 
@@ -810,7 +889,7 @@ void launch_many(const ManyArgs &m, hipStream_t st) {
     const int rounds = (units + kManySlots - 1) / kManySlots;
     hipLaunchKernelGGL((linear_many<GROUP, TT>), dim3(rounds * kManySlots), dim3(kManyThreads), 0, st, m);
     if (m.splits > 1)
-        hipLaunchKernelGGL(join<TT>, dim3((m.tiles - m.whole) * (16 * TT * kManyRows / 1024)), dim3(256), 0, st, m);
+        hipLaunchKernelGGL(join<TT>, dim3((m.tiles - m.whole) * (4 * TT)), dim3(kManyRows), 0, st, m);
 }
 
 template <int GROUP>

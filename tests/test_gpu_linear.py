@@ -189,6 +189,7 @@ LARGE = [
     (70000, 250, 232, 64, "bf16", "bf16", False, False, 0),       # many tiles of few steps
     (2300, 4100, 1160, 32, "fp32", "bf16", True, True, 8), (1150, 5051, 776, 64, "bf16", "bf16", True, True, 8),
     (2200, 6100, 2600, 64, "bf16", "fp32", False, True, 0), (8190, 600, 2056, 32, "bf16", "bf16", True, False, 0),
+    (2048, 4096, 9000, 32, "bf16", "fp32", False, False, 0), (64, 60000, 9000, 32, "bf16", "bf16", False, True, 0),   # many groups
     (1 << 20, 5, 40, 32, "fp32", "fp32", False, False, 0),        # the most rows, more tiles than a launch has in y
 ]
 # tiles of wavefronts: more rows than one tile, with 1 to 8 wavefronts along K

@@ -33,7 +33,9 @@ struct LinearArgs {
     int N, T, blocks;               // blocks of kBlock codes in a row
     int pieces;                     // of x: 1 (bf16) or 3 (fp32; in memory where !STAGE)
     bool y32;
-    int ways;                       // of linear_some's wavefronts along K, a power of two
+    int ways;                       // linear_some: of a workgroup's wavefronts along K, a power of two
+    int token_groups;               // linear_some: of a workgroup's tokens
+    bool by_tokens;                 // linear_some: which of the two an XCD has an eighth of
 };
 
 // Codes 2 i and 2 i + 1 of a word as bf16 pairs 16 + q.
@@ -355,12 +357,17 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
-    const int per = ((a.N + 16 * R - 1) / (16 * R) + 7) / 8;
-    const int n0 = ((blockIdx.x & 7) * per + (blockIdx.x >> 3)) * 16 * R;      // as in Walk, one tile each
-    if (n0 >= a.N) return;
+    // an XCD has an eighth of the rows of the weights, as in Walk, or of the tokens, whichever are more bytes: 1086 fp32 rows
+    // through 144 x 7624 31 us by tokens and 69 by rows, 2000 bf16 rows through 60 x 6400 10 and 30
+    const int tiles = (a.N + 16 * R - 1) / (16 * R), xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
+    const int per = ((a.by_tokens ? a.token_groups : tiles) + 7) / 8;
+    const int n_tile = a.by_tokens ? turn % tiles : xcd * per + turn % per;
+    const int group = a.by_tokens ? xcd * per + turn / tiles : turn / per;
+    if (n_tile >= tiles || group >= a.token_groups) return;
+    const int n0 = n_tile * 16 * R;
     // wavefronts along K, and of tokens the tiles of the others
     const int ways = a.ways, along = wave & (ways - 1);
-    const int t0 = (blockIdx.y * (kWaves / ways) + wave / ways) * 16 * TT;
+    const int t0 = (group * (kWaves / ways) + wave / ways) * 16 * TT;
     uint4 x[LOADS][PARTS];
     Block<GROUP, R> next;
     // load i of a block: row 4 i + quarter, chunk `col` of 8 values
@@ -879,8 +886,11 @@ void launch_few(const LinearArgs &a, hipStream_t st) {
 template <int GROUP, int R, int TT, int P>
 void launch_some(const LinearArgs &a, hipStream_t st) {
     const int tiles = (a.N + 16 * R - 1) / (16 * R), tokens = 16 * TT * (kWaves / a.ways);
-    hipLaunchKernelGGL((linear_some<GROUP, R, TT, P>), dim3((tiles + 7) / 8 * 8, (a.T + tokens - 1) / tokens), dim3(64 * kWaves),
-                       0, st, a);
+    LinearArgs b = a;
+    b.token_groups = (a.T + tokens - 1) / tokens;
+    b.by_tokens = int64_t(a.T) * (P == 3 ? 8 : 4) > a.N && b.token_groups >= 8;
+    const int groups = b.by_tokens ? (b.token_groups + 7) / 8 * 8 * tiles : (tiles + 7) / 8 * 8 * b.token_groups;
+    hipLaunchKernelGGL((linear_some<GROUP, R, TT, P>), dim3(groups), dim3(64 * kWaves), 0, st, b);
 }
 
 template <int GROUP, int TT>
@@ -910,7 +920,6 @@ struct Plan {
 };
 
 constexpr int kCUs = 256;
-constexpr int kGridY = 65535;        // of a launch
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // linear_some: how many of the 8 wavefronts go along K, and whether for 16 or 32 rows of the weights.  Workgroups a CU
@@ -977,7 +986,7 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
     if (token_tiles == 1) return p;
     Plan m{};
     m.kind = Plan::kMany;
-    if (some <= plan_many(T, N, blocks, pieces, m) && token_tiles <= kGridY) return p;
+    if (some <= plan_many(T, N, blocks, pieces, m)) return p;
     m.pieces = up256(size_t(pieces) * T * Kp * 2);
     m.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
     return m;
@@ -1036,7 +1045,7 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
                  static_cast<const uint16_t *>(x), x_stride, 0, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
-                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32, plan.ways};
+                 Kp / kBlock, pieces, y_type == APEX_TYPE_FP32, plan.ways, 1, false};
     if (plan.kind == Plan::kMany) {
         char *ws = static_cast<char *>(workspace);
         float *totals = reinterpret_cast<float *>(ws + plan.pieces);

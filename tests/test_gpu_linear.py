@@ -190,7 +190,6 @@ LARGE = [
     (2300, 4100, 1160, 32, "fp32", "bf16", True, True, 8), (1150, 5051, 776, 64, "bf16", "bf16", True, True, 8),
     (2200, 6100, 2600, 64, "bf16", "fp32", False, True, 0), (8190, 600, 2056, 32, "bf16", "bf16", True, False, 0),
     (2048, 4096, 9000, 32, "bf16", "fp32", False, False, 0), (64, 60000, 9000, 32, "bf16", "bf16", False, True, 0),   # many groups
-    (1 << 20, 5, 40, 32, "fp32", "fp32", False, False, 0),        # the most rows, more tiles than a launch has in y
 ]
 # tiles of wavefronts: more rows than one tile, with 1 to 8 wavefronts along K
 SOME = [
@@ -201,6 +200,7 @@ SOME = [
     (353, 4099, 232, 128, "bf16", "bf16", False, False, 8), (901, 803, 160, 32, "fp32", "fp32", True, True, 0),
     (399, 600, 1000, 64, "fp32", "bf16", False, False, 0), (100, 5000, 128, 128, "fp32", "fp32", False, True, 0),
     (9999, 40, 520, 32, "bf16", "fp32", True, False, 0), (86, 22171, 256, 128, "bf16", "bf16", False, True, 0),
+    (1 << 20, 5, 40, 32, "fp32", "fp32", False, False, 0),        # the most rows
 ]
 
 

@@ -224,8 +224,11 @@ enum Rows {
 };
 constexpr int staged_rows(int rows, int T) { return rows == kPieces ? 3 * T : T; }
 
-// Up to 4 rows: all of x goes to LDS first, at most stage_bytes() of it.  The wavefronts join their sums in LDS
-// in a fixed order.
+// Up to 4 rows: all of x goes to LDS first, at most stage_bytes() of it, and the weights are read once, by workgroups that
+// stay.  The wavefronts join their sums in LDS in a fixed order.  A long stream is bound by memory: 4 rows through
+// 32768 x 4096 in groups of 32, 84 MB, 14.5 us, 5.8 TB/s, what a kernel that only reads gets.  A short one by the way
+// of a launch, x and the first weights one behind the other: one fp32 row through 6144 x 4096, 13.4 MB, 5.9 us, through
+// 2048 x 1024 3.4.
 template <int GROUP, int R, int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
     extern __shared__ uint4 lds[];
@@ -348,7 +351,9 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
 // Some rows, in tiles of 16 TT, bf16 or fp32 (P = 3 pieces).  A workgroup takes 16 R rows of the weights; each wavefront
 // brings the part of x that belongs to its next block, 16 TT rows of 256 or 512 bytes, by loads of whole lines, fp32 values
 // cut into their pieces on the way, into LDS of its own, and reads it as the matrix instructions want it.  Within
-// a row 16-byte chunks stand in the place c ^ (row mod 16), so that 16 rows' chunks meet 64 banks.
+// a row 16-byte chunks stand in the place c ^ (row mod 16), so that 16 rows' chunks meet 64 banks.  Bound by a block's
+// way, loads, LDS and matrix instructions, of which a wavefront has one on its way ahead: 32 rows through 4096 x 4096
+// 8.2 to 9.4 us, 4 blocks each.  Two ahead were no faster (16384 x 4096 16.5 and 19.4: fewer workgroups on a CU).
 template <int GROUP, int R, int TT, int P>
 __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, LOADS = 4 * TT, PARTS = P == 3 ? 2 : 1;   // of 16 bytes for 8 values
@@ -477,6 +482,10 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
 //
 // There is a workgroup a CU.  The last tiles, fewer than that, are cut along K into shares, whose sums go
 // to memory in the order of the lanes and are joined by another launch.
+//
+// A step of 128 tokens, 64 matrix instructions and about 200 of the vector unit a wavefront, takes 2.1 us: widening codes
+// and scaling sums fill the time that the matrix cores have free, which are busy 44 % of it, at 2.2 GHz.  2048 rows
+// through 6144 x 4096: 110 us, 937 TFLOP/s (a library product of bf16 weights of this size 96 to 103).
 #define APEX_LDS __attribute__((address_space(3)))
 constexpr int kManyThreads = 512, kManyRows = 256, kManySlots = 256;
 constexpr int kManyR = 2;                       // tiles of 16 rows of a wavefront
@@ -496,7 +505,8 @@ __device__ __forceinline__ void settle(floatx4 &v) { asm volatile("" : "+v"(v));
 constexpr int vmcnt_only(int n) { return 0x0f70 | (n & 15) | (n >> 4 << 14); }   // the s_waitcnt operand
 
 // A value in three bf16 pieces whose sum it is, at 6 of a lane's 8 places along K of a matrix instruction, in the left
-// and the right operand: the 6 products of pieces that reach the value's 24 bits.
+// and the right operand: the 6 products of pieces that reach the value's 24 bits.  Half the time of instructions on
+// fp32, 4 along K as well.
 __device__ __forceinline__ void pieces_of(float v, uint32_t (&p)[3]) {
     const float rest = v - __uint_as_float(__float_as_uint(v) & 0xffff0000u);
     p[0] = __float_as_uint(v), p[1] = __float_as_uint(rest);
@@ -701,8 +711,9 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     const auto load_sums = [&](uint8_t *to, int chunk) {
         const int four = g_first / 4 + chunk * FOURS;
         const int64_t left = int64_t((a.blocks * PER + 3) / 4 - four) * a.T - t0;      // tokens' fours
-        const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(m.totals + (left > 0 ? (int64_t(four) * a.T + t0) * 4 : 0)),
-                                                            0, int(min(max(left, int64_t(0)), int64_t(1) << 26)) * 16, 0x00027000);
+        const auto from = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<float *>(m.totals + (left > 0 ? (int64_t(four) * a.T + t0) * 4 : 0)), 0,
+            int(min(max(left, int64_t(0)), int64_t(1) << 26)) * 16, 0x00027000);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int u = wave * 128 + i * 64 + lane;
@@ -787,7 +798,8 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                place(tt)[(4 * quarter_after + i) * 256 + ((wave * 32 + 16 * r + col_after) ^ (16 * quarter_after))] = sum[r][tt][i];
+                place(tt)[(4 * quarter_after + i) * 256 + ((wave * 32 + 16 * r + col_after) ^ (16 * quarter_after))] =
+                    sum[r][tt][i];
     __syncthreads();
     constexpr int ROWS = BM / 8;                       // tokens of a wavefront, within one of those places
     const float *mine_out = place(wave * ROWS / 16) + wave * ROWS % 16 * 256;
@@ -799,7 +811,8 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
 }
 
-// The shares of the tiles that were cut, in order.  A workgroup takes 4 tokens, its threads a row of the weights each.
+// The shares of the tiles that were cut, in order.  A workgroup takes 4 tokens, its threads a row of the weights each.  Memory
+// and a launch: 33.5 MB of shares in 8 us.
 template <int TT>
 __global__ __launch_bounds__(kManyRows) void join(ManyArgs m) {
     constexpr int values = 16 * TT * kManyRows / 4;    // of 4 tokens
@@ -816,7 +829,7 @@ __global__ __launch_bounds__(kManyRows) void join(ManyArgs m) {
 // Sums of x over groups of GROUP values, [groups / 4][T][4], and x as bf16 (PIECES: fp32 values as three pieces)
 // in the order in which it is read: [block of 128 values][piece][T][128], zeros behind K.  linear_many's loads are then
 // side by side whatever the stride of x is; a chunk of 2048 rows through 6144 x 4096 took 139 us with x in this order and 146
-// with bf16 rows as they stand.  A lane takes 8 values, GROUP / 8 lanes a group.
+// with bf16 rows as they stand.  A lane takes 8 values, GROUP / 8 lanes a group.  Memory: 16.8 MB read and written 7 to 9 us.
 template <int GROUP, bool PIECES>
 __global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
                                               uint16_t *out) {

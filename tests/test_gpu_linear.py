@@ -10,6 +10,9 @@ last, which is 1e-6 of the result's sqrt(n) * 4.6 |x| for n = 128, 1.5e-6 with t
 the additions of three pieces: fp32 at most 3e-6, where a lost third piece would leave 7e-6.  bf16 rounds once, with an
 rms of at most 2^-8 / sqrt(3) * 0.72 = 1.63e-3: 2e-3.
 """
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -405,3 +408,11 @@ def test_packed_by_the_library(torch):
     c.dw = torch.from_numpy(out).cuda()
     c.call()
     c.compare(c.dy, norm=False)
+
+
+def test_readme_example_runs(torch):
+    """The Python example of README.md for projections and rotary positions, run as written."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "README.md")).read()
+    code = re.search(r"<!-- example: projection -->\s*```python\n(.*?)```", text, re.S).group(1)
+    exec(compile(code, "README.md example", "exec"), {})

@@ -32,8 +32,9 @@
  *    of 8 (16-byte rows of bf16), B >= 0 tokens (B = 0 enqueues nothing).
  *  - apex_prefetch_route, apex_gate_topk, the apex_moe_ffn entry points, the paged-cache
  *    entry points (apex_paged_plan, apex_paged_store, apex_paged_store_rotary,
- *    apex_attention_paged), apex_rotary and apex_linear_w4 only launch kernels on the given stream (no allocation, memory set, copy or synchronisation),
- *    so a caller may capture them in a HIP graph; apex_moe_ffn_noalloc's first call on
+ *    apex_attention_paged), apex_rotary and apex_linear_w4 only launch kernels on the given
+ *    stream (no allocation, memory set, copy or synchronisation), so a caller may capture
+ *    them in a HIP graph; apex_moe_ffn_noalloc's first call on
  *    a device looks up that device's scratch array and must come before the capture.
  */
 #ifndef APEX_H
@@ -577,14 +578,15 @@ apex_status apex_paged_store_rotary(const apex_paged_cache *cache, const apex_ro
  *   bias    device fp32 [N], or NULL
  *   residual  device, type `y_type`, row t's [N] at residual + t * residual_stride (at least N), or
  *           NULL; may be y (same stride)
- *   y       device, type `y_type` out: row t's [N] at y + t * y_stride (at least N)
+ *   y       device, type `y_type` out: row t's [N] at y + t * y_stride (at least N); may not overlap x
  *   T       rows, at most APEX_MAX_STEP_TOKENS
- *   workspace  device, >= apex_linear_w4_workspace_bytes(T, N, K, group, x_type) bytes (may be NULL where
- *           that is 0); must not be shared by calls that may overlap
+ *   workspace  device, >= apex_linear_w4_workspace_bytes(T, N, K, group, x_type) bytes, which serve any
+ *           smaller T too (0, and workspace may be NULL, up to 32 rows of bf16 or 16 of fp32); must not
+ *           be shared by calls that may overlap
  * Arithmetic: products on the matrix cores, of the weights and of x as they are (fp32 values go
  * through in three pieces), sums in fp32, one rounding to y_type; no atomics, deterministic.  A row of
- * x with a NaN or an infinity has NaN in all of its row of y; the other rows do not see it.  |x| is
- * to be below 2^115 and what of it stands below 2^-126 may count as 0.
+ * x with a NaN or an infinity has NaN in all of its row of y (an infinity where z is below -16); the
+ * other rows do not see it.  |x| is to be below 2^115 and what of it stands below 2^-126 may count as 0.
  */
 size_t apex_linear_w4_bytes(int N, int K, int group);
 apex_status apex_pack_linear_w4(const uint16_t *w, int N, int K, int group, void *out);

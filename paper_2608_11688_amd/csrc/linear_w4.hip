@@ -934,6 +934,8 @@ struct Plan {
 
 constexpr int kCUs = 256;
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+size_t x_bytes(int T, int Kp, int pieces) { return up256(size_t(pieces) * T * Kp * 2); }
+size_t sums_bytes(int T, int Kp, int group) { return up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4); }
 
 // linear_some: how many of the 8 wavefronts go along K, and whether for 16 or 32 rows of the weights.  Workgroups a CU
 // times the steps of a wavefront and one more for its ends; 32 rows take 1.3 times as long as 16.  us, for 8, 4, 2 and 1
@@ -999,9 +1001,11 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
     if (token_tiles == 1) return p;
     Plan m{};
     m.kind = Plan::kMany;
-    if (some <= plan_many(T, N, blocks, pieces, m)) return p;
-    m.pieces = up256(size_t(pieces) * T * Kp * 2);
-    m.totals = up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4);
+    const double many = plan_many(T, N, blocks, pieces, m);
+    const int64_t workgroups = int64_t(token_tiles + 8) * (N / 16 + 8);      // of linear_some, at most
+    if (some <= many && workgroups < (int64_t(1) << 31)) return p;
+    m.pieces = x_bytes(T, Kp, pieces);
+    m.totals = sums_bytes(T, Kp, group);
     return m;
 }
 
@@ -1024,7 +1028,16 @@ void launch(const LinearArgs &a, const Plan &p, hipStream_t st) {
 
 extern "C" size_t apex_linear_w4_workspace_bytes(int T, int N, int K, int group, int x_type) {
     if (T < 1 || T > APEX_MAX_STEP_TOKENS || !sizes_ok(N, K, group) || !is_type(x_type)) return 0;
-    return plan_of(T, N, K, group, x_type == APEX_TYPE_FP32 ? 3 : 1).bytes();
+    const int pieces = x_type == APEX_TYPE_FP32 ? 3 : 1, Kp = padded(K), blocks = Kp / kBlock;
+    if (T <= (pieces == 3 ? 16 : 32)) return 0;
+    // a smaller T may be cut into more shares: the most of any number of tiles
+    size_t parts = 0;
+    for (int t = 64; t - 64 < T; t += 64) {
+        Plan p{};
+        plan_many(t, N, blocks, pieces, p);
+        parts = std::max(parts, p.parts);
+    }
+    return x_bytes(T, Kp, pieces) + sums_bytes(T, Kp, group) + parts;
 }
 
 extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, const void *x, int x_type, int T,
@@ -1049,6 +1062,7 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
                      apex::aligned16(residual) && apex::aligned16(workspace),
                  "%s: pointers must be 16-byte aligned", fn);
     APEX_REQUIRE(residual != y || residual_stride == y_stride, "%s: y is the residual with another stride", fn);
+    APEX_REQUIRE(x != y, "%s: y is x", fn);
     const int Kp = padded(K), pieces = x_type == APEX_TYPE_FP32 ? 3 : 1;
     const Plan plan = plan_of(T, N, K, group, pieces);
     const size_t need = plan.bytes();

@@ -147,7 +147,6 @@ class Large:
         self.r = torch.randn(T, N + extra, generator=gen, device="cuda").to(types[y]) if residual else None
         self.y = torch.full((T, N + extra), 7.0, dtype=types[y], device="cuda")
         need = native.apex_linear_w4_workspace_bytes(T, N, K, group, x)
-        self.in_tiles = need > 2 * T * Kp              # x in the order of the tiles, and more
         self.ws = torch.full((need + 64,), 0xAB, dtype=torch.uint8, device="cuda")
 
     def call(self, stream=None):
@@ -173,7 +172,20 @@ class Large:
     def check(self):
         self.call()
         self.torch.cuda.synchronize()
+        self.in_tiles = bool((self.ws[:256] != 0xAB).any())     # x in the order of the tiles
         assert (self.y[:, self.N:] == 7).all() and (self.ws[-64:] == 0xAB).all()
+        return self.compare()
+
+    def check_rows(self, T):
+        """The first T rows of y, and that the others stay."""
+        self.call()
+        self.torch.cuda.synchronize()
+        assert (self.y[T:] == 7).all() and (self.ws[-64:] == 0xAB).all()
+        y, self.y = self.y, self.y[:T]
+        self.compare()
+        self.y = y
+
+    def compare(self):
         want, size = self.reference()
         return compare(self.y[:, :self.N].double().cpu().numpy(), want, size, self.group, self.K, self.x_type, self.y_type)
 
@@ -210,15 +222,26 @@ SOME = [
 @pytest.mark.parametrize("case", LARGE, ids=[str(c) for c in LARGE])
 def test_products_in_tiles(torch, case):
     c = Large(torch, *case, seed=case[0])
-    assert c.in_tiles
     print(c.check())
+    assert c.in_tiles
 
 
 @pytest.mark.parametrize("case", SOME, ids=[str(c) for c in SOME])
 def test_tiles_of_wavefronts(torch, case):
     c = Large(torch, *case, seed=case[0])
-    assert not c.in_tiles
     print(c.check())
+    assert not c.in_tiles
+
+
+def test_a_workspace_serves_fewer_rows(torch):
+    """One workspace of the largest T, and what stands behind it, through every T below."""
+    N, K, T = 1500, 2048, 700
+    c = Large(torch, T, N, K, 32, "bf16", "fp32")
+    x = c.x
+    for c.T in (700, 513, 300, 129, 64, 33, 1):
+        c.x = x[:c.T]
+        c.y.fill_(7.0)
+        c.check_rows(c.T)
 
 
 @pytest.mark.parametrize("case", [LARGE[1], LARGE[6], LARGE[8], LARGE[10]], ids=str)

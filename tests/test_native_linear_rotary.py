@@ -175,7 +175,7 @@ def project(**kw):
     (INVAL, dict(xs=260)), (INVAL, dict(xt="fp32", xs=258)), (INVAL, dict(ys=95)), (INVAL, dict(rs=95)),
     (INVAL, dict(w=None)), (INVAL, dict(x=None)), (INVAL, dict(y=None)), (INVAL, dict(w=A + 8)), (INVAL, dict(x=A + 8)),
     (INVAL, dict(y=A + 8)), (INVAL, dict(bias=A + 4)), (INVAL, dict(r=A + 2)), (INVAL, dict(ws=A + 8)),
-    (INVAL, dict(r=2 * A, rs=200)), (INVAL, dict(N=(1 << 24) + 1, ys=1 << 25, rs=1 << 25)),
+    (INVAL, dict(r=2 * A, rs=200)), (INVAL, dict(y=A)), (INVAL, dict(N=(1 << 24) + 1, ys=1 << 25, rs=1 << 25)),
     (INVAL, dict(K=(1 << 20) + 8, xs=1 << 21)), (INVAL, dict(LARGE, ws=None)), (CAPACITY, dict(LARGE, n=1024)),
     (CAPACITY, dict(LARGE, xt="bf16", n=256 * 8192 * 2))], ids=str)
 def test_linear_refuses(status, kw):
@@ -197,3 +197,6 @@ def test_linear_workspace():
     assert 256 * 8192 * 6 < f(256, 8192, 8192, 64, "fp32") < (1 << 28)
     assert 256 * 8192 * 2 < f(256, 8192, 8192, 64, "bf16") < (1 << 28)
     assert f(1, 1 << 20, 1 << 20, 32, "bf16") == 0             # single rows take none
+    for N, K, group, x in ((96, 256, 64, "fp32"), (4096, 4096, 32, "bf16"), (259, 3968, 128, "fp32"), (25083, 520, 64, "bf16")):
+        sizes = [f(T, N, K, group, x) for T in range(1, 3000)]
+        assert sizes[:16] == [0] * 16 and all(a <= b for a, b in zip(sizes, sizes[1:]))

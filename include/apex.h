@@ -585,7 +585,7 @@ apex_status apex_paged_store_rotary(const apex_paged_cache *cache, const apex_ro
  *           be shared by calls that may overlap
  * Arithmetic: products on the matrix cores, of the weights and of x as they are (fp32 values go
  * through in three pieces), sums in fp32, one rounding to y_type; no atomics, deterministic.  A row of
- * x with a NaN or an infinity has NaN in all of its row of y (an infinity where z is below -16); the
+ * x with a NaN or an infinity has NaN in all of its row of y (or infinities where z is below -16); the
  * other rows do not see it.  |x| is to be below 2^115 and what of it stands below 2^-126 may count as 0.
  */
 size_t apex_linear_w4_bytes(int N, int K, int group);

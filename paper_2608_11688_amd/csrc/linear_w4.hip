@@ -831,7 +831,7 @@ __global__ __launch_bounds__(kManyRows) void join(ManyArgs m) {
 // side by side whatever the stride of x is; a chunk of 2048 rows through 6144 x 4096 took 139 us with x in this order and 146
 // with bf16 rows as they stand.  A lane takes 8 values, GROUP / 8 lanes a group.  Memory: 16.8 MB read and written 7 to 9 us.
 template <int GROUP, bool PIECES>
-__global__ __launch_bounds__(256) void survey(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
+__global__ __launch_bounds__(256) void sum_groups(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
                                               uint16_t *out) {
     const int lanes = Kp / 8;
     const int64_t all = int64_t(T) * lanes;
@@ -1079,8 +1079,8 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         uint16_t *tiled = reinterpret_cast<uint16_t *>(ws);
         const int64_t items = int64_t(T) * (Kp / 8);
         const dim3 grid(unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)));
-        const auto f = pieces > 1 ? (group == 32 ? survey<32, true> : group == 64 ? survey<64, true> : survey<128, true>)
-                                  : (group == 32 ? survey<32, false> : group == 64 ? survey<64, false> : survey<128, false>);
+        const auto f = pieces > 1 ? (group == 32 ? sum_groups<32, true> : group == 64 ? sum_groups<64, true> : sum_groups<128, true>)
+                                  : (group == 32 ? sum_groups<32, false> : group == 64 ? sum_groups<64, false> : sum_groups<128, false>);
         hipLaunchKernelGGL(f, grid, dim3(256), 0, stream, x, x_stride, T, K, Kp, totals, tiled);
         APEX_HIP(hipGetLastError());
         a.x = tiled;

@@ -233,6 +233,33 @@ def test_tiles_of_wavefronts(torch, case):
     assert not c.in_tiles
 
 
+def test_two_graphs_that_share_a_workspace(torch):
+    """Replayed in turn on one stream, with eager calls between: nothing in the workspace is kept from call to call."""
+    a = Large(torch, 300, 2816, 4104, 64, "bf16", "fp32", seed=1)
+    b = Large(torch, 129, 9001, 2000, 128, "fp32", "bf16", seed=2)
+    a.ws = b.ws = torch.empty(max(a.ws.numel(), b.ws.numel()), dtype=torch.uint8, device="cuda")
+    want = []
+    for c in (a, b):
+        c.call()
+        torch.cuda.synchronize()
+        want.append(c.y.clone())
+    side, graphs = torch.cuda.Stream(), [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.stream(side):
+        for c, graph in zip((a, b), graphs):
+            with torch.cuda.graph(graph, stream=side):
+                c.call(side.cuda_stream)
+    for i in range(4):
+        for c, graph, right in zip((a, b), graphs, want):
+            c.y.fill_(7.0)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(c.y, right)
+        b.call()
+        torch.cuda.synchronize()
+        assert torch.equal(b.y, want[1])
+
+
 def test_a_workspace_serves_fewer_rows(torch):
     """One workspace of the largest T, and what stands behind it, through every T below."""
     N, K, T = 1500, 2048, 700

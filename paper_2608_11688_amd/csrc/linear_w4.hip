@@ -362,13 +362,13 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
-    // an XCD has an eighth of the rows of the weights, as in Walk, or of the tokens, whichever are more bytes: 1086 fp32 rows
-    // through 144 x 7624 31 us by tokens and 69 by rows, 2000 bf16 rows through 60 x 6400 10 and 30
-    const int tiles = (a.N + 16 * R - 1) / (16 * R), xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
-    const int per = ((a.by_tokens ? a.token_groups : tiles) + 7) / 8;
-    const int n_tile = a.by_tokens ? turn % tiles : xcd * per + turn % per;
-    const int group = a.by_tokens ? xcd * per + turn / tiles : turn / per;
-    if (n_tile >= tiles || group >= a.token_groups) return;
+    // an XCD has an eighth of the work, of the rows of the weights, as in Walk, or of the tokens, whichever are more bytes: 1086
+    // fp32 rows through 144 x 7624 31 us by tokens and 69 by rows, 2000 bf16 rows through 60 x 6400 10 and 30
+    const int tiles = (a.N + 16 * R - 1) / (16 * R), all = tiles * a.token_groups, per = (all + 7) / 8;
+    const int unit = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (unit >= all) return;
+    const int n_tile = a.by_tokens ? unit % tiles : unit / a.token_groups;
+    const int group = a.by_tokens ? unit / tiles : unit % a.token_groups;
     const int n0 = n_tile * 16 * R;
     // wavefronts along K, and of tokens the tiles of the others
     const int ways = a.ways, along = wave & (ways - 1);
@@ -901,9 +901,8 @@ void launch_some(const LinearArgs &a, hipStream_t st) {
     const int tiles = (a.N + 16 * R - 1) / (16 * R), tokens = 16 * TT * (kWaves / a.ways);
     LinearArgs b = a;
     b.token_groups = (a.T + tokens - 1) / tokens;
-    b.by_tokens = int64_t(a.T) * (P == 3 ? 8 : 4) > a.N && b.token_groups >= 8;
-    const int groups = b.by_tokens ? (b.token_groups + 7) / 8 * 8 * tiles : (tiles + 7) / 8 * 8 * b.token_groups;
-    hipLaunchKernelGGL((linear_some<GROUP, R, TT, P>), dim3(groups), dim3(64 * kWaves), 0, st, b);
+    b.by_tokens = int64_t(a.T) * (P == 3 ? 8 : 4) > a.N;
+    hipLaunchKernelGGL((linear_some<GROUP, R, TT, P>), dim3((tiles * b.token_groups + 7) / 8 * 8), dim3(64 * kWaves), 0, st, b);
 }
 
 template <int GROUP, int TT>

@@ -3,12 +3,13 @@
 //
 // A workgroup takes a token.  Its threads first fill a table in LDS with the cosines and sines of
 // the token's angles, one angle each, in 64 bits and rounded once.  Then lane l of a head's hd / 8
-// holds 8 values: four pairs of the table where l < dim / 8, else 8 values that stay as they are.  Every head of a token uses the same table, so an angle
-// costs its share of H + G heads; what remains is one read and one write of every value, 4.9 to 5.2
-// TB/s of both from memory: 8192 rows of 32 heads of 64 in fp32, 134 MB, 27.4 us; 8192 of 32 + 2 x 8
-// heads of 128 in fp32 with E4M3 pages, 353 MB, 68.  Four tokens a workgroup took 31.6 and 82.9: a
-// head's 16-byte accesses then stood 32 bytes apart.  Loads and stores past the caches take 27.1
-// where rows come from memory, but 26.3 instead of 20.7 where a projection has just written them.
+// holds 8 values: four pairs of the table where l < dim / 8, else 8 values that stay as they are.
+// Every head of a token uses the same table, so an angle costs its share of H + G heads; what remains
+// is one read and one write of every value, 4.9 to 5.2 TB/s of both from memory: 8192 rows of 32
+// heads of 64 in fp32, 134 MB, 27.4 us; 8192 of 32 + 2 x 8 heads of 128 in fp32 with E4M3 pages, 353
+// MB, 68.  Four tokens a workgroup took 31.6 and 82.9: a head's 16-byte accesses then stood 32 bytes
+// apart.  Loads and stores past the caches take 27.1 where rows come from memory, but 26.3 instead
+// of 20.7 where a projection has just written them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

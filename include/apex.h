@@ -584,7 +584,11 @@ apex_status apex_paged_store_rotary(const apex_paged_cache *cache, const apex_ro
  *           smaller T too (0, and workspace may be NULL, up to 32 rows of bf16 or 16 of fp32); must not
  *           be shared by calls that may overlap
  * Arithmetic: products on the matrix cores, of the weights and of x as they are (fp32 values go
- * through in three pieces), sums in fp32, one rounding to y_type; no atomics, deterministic.  A row of
+ * through in three pieces), sums in fp32, one rounding to y_type; no atomics, deterministic.  Each
+ * group's sum has its zero point's part taken off before groups are added, so that the error of an
+ * fp32 result goes with what one group sums, |s| (32 + q + |z|) |x|, and neither with the row's length
+ * nor with the mean of x (measured, 2-norm over many results relative to theirs, weights around 0: up
+ * to 3e-7 for bf16 rows and 1.2e-6 for fp32 ones).  A row of
  * x with a NaN or an infinity has NaN in all of its row of y (or infinities where z is below -16); the
  * other rows do not see it.  |x| is to be below 2^115 and what of it stands below 2^-126 may count as 0.
  */

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 
@@ -23,15 +24,15 @@ constexpr int kBlock = 128;         // codes of a row that stand together, 64 by
 struct LinearArgs {
     const uint8_t *codes;
     const uint32_t *words;
-    const uint16_t *x;              // bf16, or the pieces of fp32
-    int64_t x_stride, x_block, x_piece;      // in values: of rows; for linear_many also of 128 values along K, of pieces
+    const uint16_t *x;              // bf16, or fp32; for linear_many bf16, or the pieces of fp32
+    int64_t x_stride, x_piece;      // in values: of rows; for linear_many of the pieces of 128 values along K
     int x_cols;                     // values of a row of x that there are (a multiple of 8), but for linear_many
     const float *bias;
     const void *residual;
     void *y;
     int64_t residual_stride, y_stride;
     int N, T, blocks;               // blocks of kBlock codes in a row
-    int pieces;                     // of x: 1 (bf16) or 3 (fp32; in memory where !STAGE)
+    int pieces;                     // of x: 1 (bf16) or 3 (fp32)
     bool y32;
     int ways;                       // linear_some: of a workgroup's wavefronts along K, a power of two
     int token_groups;               // linear_some: of a workgroup's tokens
@@ -215,6 +216,14 @@ struct Block {
         }
     }
 };
+
+// Of those words two, of groups j and j + 1, made anew at each call.
+__device__ __forceinline__ void two_words(uint32_t word, int j, uint32_t (&w)[4]) {
+    asm volatile("" : "+v"(word));
+    const auto h = __builtin_amdgcn_permlane32_swap(word, word, false, false);
+    const auto v = __builtin_amdgcn_permlane16_swap(h[j / 2], h[j / 2], false, false);
+    w[j] = v[0], w[j + 1] = v[1];
+}
 
 // How the rows of x stand in the 16 rows of a matrix instruction, whose lane holds rows 4 q + i, i =
 // 0..3, of the result (q = lane / 16):
@@ -477,22 +486,30 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(LinearArgs a) {
 // linear_some) into three stages, from there to registers a quarter of a step ahead.  The one barrier
 // of a step stands before its last quarter, when all of the stage has been read: the next step's first
 // values are read behind it, and the stage takes the loads of the step after the next two.
-// The sums of (16 + q) x are scaled group by group; the other half, (16 + z) sum x over groups, is a small
-// product of its own at the end, on the matrix cores in fp32, of sums of x that a launch before has made.
+// Of a group the zero points' half, (16 + z) sum x, is taken off the sums of (16 + q) x before these are scaled and added, on the
+// matrix cores, from sums of x that a launch before has made.  The halves are 24 |x| times the group's size where x has a mean,
+// which the difference has not: added up over a row and subtracted at its end they lose digits with its length, an error (2-norm)
+// of 8.5e-6 for rows of mean 1 and deviation 0.3 through 2816 x 4104 in groups of 32, 3.0e-5 through 14337 x 16384; taken
+// off group by group 1.1e-7 and 2.1e-7.  It takes 16 to 64 matrix instructions a step: 2048 rows through 6144 x 4096 in
+// groups of 128, 64 and 32 110, 128 and 151 us without and 120, 135 and 171 with them.  Of fp32 rows it is taken
+// off the first pieces' sums and off the others' apart: together, rounded at the size of the first, they came to 4.9e-6, apart to 1.6e-7.
 //
 // There is a workgroup a CU.  The last tiles, fewer than that, are cut along K into shares, whose sums go
 // to memory in the order of the lanes and are joined by another launch.
 //
-// A step of 128 tokens, 64 matrix instructions and about 200 of the vector unit a wavefront, takes 2.1 us: widening codes
-// and scaling sums fill the time that the matrix cores have free, which are busy 44 % of it, at 2.2 GHz.  2048 rows
-// through 6144 x 4096: 110 us, 937 TFLOP/s (a library product of bf16 weights of this size 96 to 103).
+// A step of 128 tokens in groups of 128, 80 matrix instructions and about 170 of the vector unit a wavefront, takes 2.2 us: widening
+// codes and scaling sums fill the time that the matrix cores have free, which are busy 49 % of it, at 2.1 GHz.  2048 rows
+// through 6144 x 4096: 120 us, 859 TFLOP/s (a library product of bf16 weights of this size 84 to 103).
 #define APEX_LDS __attribute__((address_space(3)))
 constexpr int kManyThreads = 512, kManyRows = 256, kManySlots = 256;
 constexpr int kManyR = 2;                       // tiles of 16 rows of a wavefront
 
+// Tokens for which sums of x over groups are kept.
+__host__ __device__ constexpr int tokens32(int T) { return (T + 31) / 32 * 32; }
+
 struct ManyArgs {
     LinearArgs a;
-    const float *totals;            // sums of x over groups, 4 at a time: [groups / 4][T][4]
+    const uint8_t *totals;          // sums of x over groups, negated, in pieces (sum_groups)
     float *parts;                   // of the tiles that are cut: [tile][split][tile's values]
     int m_tiles, tiles, whole;      // the first `whole` tiles are not cut
     int splits, share;              // blocks of a share
@@ -504,70 +521,40 @@ __device__ __forceinline__ void settle(floatx4 &v) { asm volatile("" : "+v"(v));
 
 constexpr int vmcnt_only(int n) { return 0x0f70 | (n & 15) | (n >> 4 << 14); }   // the s_waitcnt operand
 
-// A value in three bf16 pieces whose sum it is, at 6 of a lane's 8 places along K of a matrix instruction, in the left
-// and the right operand: the 6 products of pieces that reach the value's 24 bits.  Half the time of instructions on
-// fp32, 4 along K as well.
+// The three bf16 pieces of an fp32 value whose sum it is, in the upper halves of words.
 __device__ __forceinline__ void pieces_of(float v, uint32_t (&p)[3]) {
     const float rest = v - __uint_as_float(__float_as_uint(v) & 0xffff0000u);
     p[0] = __float_as_uint(v), p[1] = __float_as_uint(rest);
     p[2] = __float_as_uint(rest - __uint_as_float(p[1] & 0xffff0000u));
 }
 __device__ __forceinline__ uint32_t uppers(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
-__device__ __forceinline__ bf16x8 left_pieces(float v) {               // 0 0 0 1 1 2
-    uint32_t p[3];
-    pieces_of(v, p);
-    return __builtin_bit_cast(bf16x8, make_uint4(uppers(p[0], p[0]), uppers(p[0], p[1]), uppers(p[1], p[2]), 0u));
-}
-__device__ __forceinline__ bf16x8 right_pieces(float v) {              // 0 1 2 0 1 0
-    uint32_t p[3];
-    pieces_of(v, p);
-    return __builtin_bit_cast(bf16x8, make_uint4(uppers(p[0], p[1]), uppers(p[2], p[0]), uppers(p[1], p[0]), 0u));
-}
 
-// Of a wavefront of linear_many: the zero points' half of up to FOURS fours of groups from `four` on, whose sums of x stand
-// at sum_x, [four][token][4], of the groups first .. last - 1.  Four groups an instruction, group 4 f + q in lane quarter q.
-template <int TT, int FOURS>
-__device__ __forceinline__ void add_zeros(const LinearArgs &a, floatx4 (&sum)[kManyR][TT], const float *sum_x, int lane, int nw,
-                                          int four, int first, int last) {
-    constexpr int R = kManyR, AHEAD = 8;               // fours whose words are on their way at once
-    const int col = lane & 15, quarter = lane >> 4;
-#pragma unroll 1
-    for (int f0 = 0; f0 < FOURS && 4 * (four + f0) < last; f0 += AHEAD) {
-        uint32_t word[AHEAD][R];
-#pragma unroll
-        for (int f = 0; f < AHEAD; ++f) {
-            const int g = 4 * (four + f0 + f) + quarter;
-            const bool there = g >= first && g < last;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                word[f][r] = there ? a.words[int64_t(g) * a.N + min(nw + 16 * r + col, a.N - 1)] : 0u;
-        }
-#pragma unroll
-        for (int f = 0; f < AHEAD; ++f) {
-            if (4 * (four + f0 + f) >= last) break;
-            bf16x8 c[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const Scale of(word[f][r]);
-                c[r] = right_pieces(-(of.s * of.z));
-            }
-#pragma unroll
-            for (int tt = 0; tt < TT; ++tt) {
-                const bf16x8 v = left_pieces(sum_x[((f0 + f) * (16 * TT) + 16 * tt + col) * 4 + quarter]);
-#pragma unroll
-                for (int r = 0; r < R; ++r) sum[r][tt] = mfma(v, c[r], sum[r][tt]);
-            }
-        }
+// A group's zero points' half, -(16 + z) sum x, as a matrix instruction: the left operand has in every lane quarter the pieces of -sum x,
+// three places and a zero, of a token in one tile and of its neighbour 16 on, all of them finite; the right one for either tile 16
+// thrice in quarter 0 and z thrice in quarter 1 against its half of the places, and nothing in the others. The shape is that of the
+// instructions whose sums it goes into: behind one of another shape, two or three instructions back, sums have come
+// out wrong.
+struct Zeros {
+    uint32_t sixteen, pick;         // the words of 16, by lane quarter, and which bytes of a group's word those of z are
+    __device__ __forceinline__ explicit Zeros(int quarter)
+        : sixteen(quarter == 0 ? 0x41804180u : 0u), pick(quarter == 1 ? 0x01000100u : 0x0c0c0c0cu) {}
+    __device__ __forceinline__ void right(uint32_t word, bf16x8 (&of)[2]) const {
+        const uint32_t z = __builtin_amdgcn_perm(word, word, pick) | sixteen, last = z & 0xffffu;
+        of[0] = __builtin_bit_cast(bf16x8, make_uint4(z, last, 0u, 0u));
+        of[1] = __builtin_bit_cast(bf16x8, make_uint4(0u, 0u, z, last));
     }
-}
+};
 
-template <int GROUP, int TT>
+template <int GROUP, int TT, int P>
 __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void linear_many(ManyArgs m) {
     constexpr int PER = kBlock / GROUP, STEPS = GROUP / 32, BM = 16 * TT, R = kManyR;
     constexpr int XLOADS = BM / 32, WLOADS = 2;        // of a wavefront a step: 4 rows of x, 16 rows of codes each
-    __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * 256], x1[BM * 256], x2[BM * 256];
-    __shared__ __attribute__((aligned(1024))) uint8_t w0[kManyRows * 64], w1[kManyRows * 64], w2[kManyRows * 64];
-    __shared__ __attribute__((aligned(1024))) uint8_t sums[16384];     // of x, the first groups'
+    constexpr int CODES = kManyRows * 64, SUMS = BM * PER * 8;     // bytes of a stage
+    constexpr int SUM_PITCH = PER * 8;                  // of a token
+    constexpr int SUM_PARTS = P == 1 ? 1 : 2;          // of a block
+    constexpr int SUM_WAVES = (SUMS + 1023) / 1024;    // wavefronts that load the sums of x; the others' load goes behind them
+    constexpr int W = CODES + (SUM_WAVES + 1) * 1024;
+    __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * 256], x1[BM * 256], x2[BM * 256], w0[W], w1[W], w2[W];
     const LinearArgs &a = m.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
@@ -586,17 +573,19 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
 
     // x: rows 4 i + quarter of this wavefront's part of the tile, the chunk for place `col`; past T nothing
     const int mine = wave * (BM / 8), x_bytes = min(BM, a.T - t0) * 256;
-    int from[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) from[i] = (mine + quarter) * 256 + 16 * (col ^ ((mine + 4 * i + quarter) & 15));
+    const int from = (mine + quarter) * 256 + 16 * (col ^ ((mine + quarter) & 15));
     const int pitch = a.blocks * 64, w_rows = min(kManyRows, a.N - n0);
     const int from_w = (wave * 32 + (lane >> 2)) * pitch + 16 * (lane & 3);
-    // the step whose loads go out: how many are left, the next one's piece, x, codes
-    int ahead = (last - first) * a.pieces, p_ahead = 0;
-    const uint16_t *x_ahead = a.x + first * a.x_block + t0 * a.x_stride;
+    const int64_t sums_pitch = int64_t(tokens32(a.T)) * SUM_PITCH;       // of a block's part
+    const int sum_bytes = wave < SUM_WAVES ? min(BM, tokens32(a.T) - t0) * SUM_PITCH : 0, from_sums = wave * 1024 + lane * 16;
+    const int to_sums = CODES + min(wave, SUM_WAVES) * 1024;
+    // the step whose loads go out: how many are left, x, codes, sums.  P stages are a block.
+    int ahead = (last - first) * P;
+    const uint16_t *x_ahead = a.x + first * (P * a.x_piece) + t0 * a.x_stride;
     const uint8_t *w_ahead = a.codes + int64_t(n0) * pitch + first * 64;
+    const uint8_t *sums_ahead = m.totals + first * SUM_PARTS * sums_pitch + t0 * SUM_PITCH;
     // as many loads whatever the step: past the last one they move nothing
-    const auto load = [&](uint8_t *x, uint8_t *w) {
+    const auto load = [&](auto stage, uint8_t *x, uint8_t *w) {
         const auto codes = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(w_ahead), 0,
                                                              ahead > 0 ? (w_rows - 1) * pitch + 64 : 0, 0x00027000);
         const auto xs = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(x_ahead), 0, ahead > 0 ? x_bytes : 0,
@@ -607,29 +596,47 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
                                                      from_w + 16 * i * pitch, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < XLOADS; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, (APEX_LDS void *)(x + (mine + 4 * i) * 256), 16, from[i & 3] + i * 1024, 0,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, (APEX_LDS void *)(x + (mine + 4 * i) * 256), 16, (from ^ 64 * i) + i * 1024, 0,
                                                      0, 0);
         --ahead;
         x_ahead += a.x_piece;                          // pieces of a block, and blocks, one behind the other
-        if (++p_ahead == a.pieces) p_ahead = 0, w_ahead += 64;
+        if constexpr (stage % P == P - 1) w_ahead += 64;
+    };
+    // Sums of x for a stage: of x's first piece, and of the others together (with the second)
+    int sums_left = (last - first) * SUM_PARTS;
+    const auto load_sums = [&](uint8_t *w) {
+        const auto sums = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(sums_ahead), 0, sums_left > 0 ? sum_bytes : 0,
+                                                            0x00027000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sums, (APEX_LDS void *)(w + to_sums), 16, from_sums, 0, 0, 0);
+        --sums_left;
+        sums_ahead += sums_pitch;
     };
     const int word_bytes = ((PER - 1) * a.N + min(a.N - nw, 16 * R)) * 4;      // of a block's words, this wavefront's rows
     const uint32_t *words_at = a.words + int64_t(first) * PER * a.N + nw;
     int words_left = nw < a.N ? last - first : 0;
-    const auto load_words = [&](uint32_t (&to)[R]) {
+    const auto load_words = [&](uint32_t (&to)[R]) {   // of the next block
         const auto words = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t *>(words_at), 0, words_left > 0 ? word_bytes : 0,
                                                              0x00027000);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             to[r] = __builtin_amdgcn_raw_buffer_load_b32(words, (quarter % PER * a.N + 16 * r + col) * 4, 0, 0);
+        words_at += PER * a.N, --words_left;
     };
     constexpr int HT = TT / 2;
     bf16x8 v[2][HT];                                   // of half h of the tokens in v[h]
+    bf16x8 sum_x[HT / 2];                              // of a group, of tiles of half of the tokens
     uint4 code_next[R];
+    const int at_x = col * 256 + 16 * (quarter ^ col);
     const auto read_x = [&](const uint8_t *x, int j, int h) {
+        int at = at_x;
+        asm volatile("" : "+v"(at));                   // an exclusive or here instead of four registers for the four quarters
 #pragma unroll
-        for (int i = 0; i < HT; ++i)
-            v[h][i] = *reinterpret_cast<const bf16x8 *>(x + col * 256 + (h * HT + i) * 4096 + 16 * ((4 * j + quarter) ^ col));
+        for (int i = 0; i < HT; ++i) v[h][i] = *reinterpret_cast<const bf16x8 *>(x + (h * HT + i) * 4096 + (at ^ 64 * j));
+    };
+    const auto read_sums = [&](const uint8_t *w, int g, int h, int lo, int hi) {
+#pragma unroll
+        for (int i = lo / 2; 2 * i < hi; ++i)
+            sum_x[i] = *reinterpret_cast<const bf16x8 *>(w + CODES + (((h * HT / 2 + i) * PER + g) * 16 + col) * 16);
     };
     const auto read_codes = [&](const uint8_t *w) {
 #pragma unroll
@@ -637,11 +644,11 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
             code_next[r] = *reinterpret_cast<const uint4 *>(w + (wave * 32 + 16 * r + col) * 64 + 16 * quarter);
     };
 
+    const Zeros zeros(quarter);
     floatx4 sum[R][TT] = {}, prod[R][TT] = {};
-    uint32_t word_next[R];
+    uint32_t word[3][R];                               // P == 1: of each stage's block; else of this block and the next one
     bf16x8 q_next[R];
     float s_before[R] = {};                            // of the group before, whose second half is still to be added
-    int p = 0;
     const auto add = [&](int h, int r, float s) {
 #pragma unroll
         for (int i = h * HT; i < (h + 1) * HT; ++i) {
@@ -652,40 +659,73 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     };
     // One step; its stage, the next step's.  Eight phases: a quarter of the block's codes by half of the tokens.  What the
     // vector unit does in a phase is for other values than its matrix instructions': the codes of the next
-    // quarter are widened, and a group's sums scaled, half a quarter later.
-    const auto step = [&](uint8_t *x, uint8_t *w, const uint8_t *x_next, const uint8_t *w_next) {
+    // quarter are widened, and a group's sums scaled, half a quarter later.  The zero points' half of a group's sums goes in
+    // halfway through its codes.
+    const auto step = [&](auto stage, uint8_t *x, uint8_t *w, const uint8_t *x_next, uint8_t *w_next, uint8_t *w_last) {
+        constexpr bool SUMS = stage % P < 2;
+        constexpr int SPREAD = STEPS == 4 ? 2 : 1;     // of groups of 64 both in one go: registers
         uint4 code[R];
-        uint32_t word[R];
+        uint32_t words[R][PER];
 #pragma unroll
-        for (int r = 0; r < R; ++r) code[r] = code_next[r], word[r] = word_next[r];
+        for (int r = 0; r < R; ++r) {
+            code[r] = code_next[r];
+            if constexpr (PER < 4) words_of<PER>(word[P == 1 ? stage : 0][r], words[r]);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             bf16x8 q[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) q[r] = q_next[r];
+            if constexpr (PER == 4) {
+                if (j % 2 == 0) {                      // words of two groups at a time: registers
+#pragma unroll
+                    for (int r = 0; r < R; ++r) two_words(word[P == 1 ? stage : 0][r], j, words[r]);
+                }
+            }
+            // the tiles of a half whose zero points' half goes in now: the sums' own first part, then the second
+            const int part = j % STEPS - (STEPS - 1) / 2, lo = max(part, 0) * (HT / SPREAD);
+            const int hi = SUMS && part >= 0 && part < SPREAD ? lo + HT / SPREAD : lo;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 __builtin_amdgcn_sched_barrier(0);
-                if (h == 0) {
-                    read_x(x, j, 1);
-                } else if (j < 3) {
-                    read_x(x, j + 1, 0);
-                } else {
+                const bool at_end = j == 3 && h == 1;
+                if (at_end) {
                     // the next step's loads have landed; those of the one behind it, the last that went
                     // out, may be on their way
                     __builtin_amdgcn_s_waitcnt(vmcnt_only(XLOADS + WLOADS));
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
                     read_codes(w_next);
+                }
+                read_sums(w, j / STEPS, h, lo, hi);
+                if (!at_end) {
+                    read_x(x, j + h, 1 - h);
+                } else {
                     read_x(x_next, 0, 0);
-                    if (++p == a.pieces) p = 0, words_at += PER * a.N, --words_left;
-                    load_words(word_next);
-                    load(x, w);
+                    if constexpr (P == 1) {
+                        load_words(word[(stage + 2) % 3]);
+                    } else if constexpr (stage == 0) {
+                        load_words(word[1]);
+                    } else if constexpr (stage == 2) {
+#pragma unroll
+                        for (int r = 0; r < R; ++r) word[0][r] = word[1][r];
+                    }
+                    if constexpr ((stage + 2) % 3 % P < 2) load_sums(w_last);
+                    load(stage, x, w);
                 }
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
                     for (int i = 0; i < HT; ++i)
                         prod[r][h * HT + i] = mfma(v[h][i], q[r], j % STEPS == 0 ? floatx4{} : prod[r][h * HT + i]);
+                if (lo < hi) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        bf16x8 z[2];
+                        zeros.right(words[r][j / STEPS], z);
+#pragma unroll
+                        for (int i = lo; i < hi; ++i) prod[r][h * HT + i] = mfma(sum_x[i / 2], z[i & 1], prod[r][h * HT + i]);
+                    }
+                }
                 if (h == 0 && j % STEPS == 0) {
 #pragma unroll
                     for (int r = 0; r < R; ++r) add(1, r, s_before[r]);
@@ -695,9 +735,7 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
                     for (int r = 0; r < R; ++r) {
                         q_next[r] = widen(j < 3 ? word_of(code[r], j + 1) : code_next[r].x);
                         if ((j + 1) % STEPS == 0) {    // a group ends
-                            uint32_t words[PER];
-                            words_of<PER>(word[r], words);
-                            s_before[r] = __uint_as_float(words[j / STEPS] & 0xffff0000u);
+                            s_before[r] = __uint_as_float(words[r][j / STEPS] & 0xffff0000u);
                             add(0, r, s_before[r]);
                         }
                     }
@@ -705,41 +743,32 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
             }
         }
     };
-    // sums of x over groups, FOURS fours of them to 16 KiB: [four][token][4]; behind the last ones nothing
-    constexpr int FOURS = 1024 / BM;
-    const int g_first = first * PER, g_last = last * PER;
-    const auto load_sums = [&](uint8_t *to, int chunk) {
-        const int four = g_first / 4 + chunk * FOURS;
-        const int64_t left = int64_t((a.blocks * PER + 3) / 4 - four) * a.T - t0;      // tokens' fours
-        const auto from = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<float *>(m.totals + (left > 0 ? (int64_t(four) * a.T + t0) * 4 : 0)), 0,
-            int(min(max(left, int64_t(0)), int64_t(1) << 26)) * 16, 0x00027000);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int u = wave * 128 + i * 64 + lane;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (APEX_LDS void *)(to + (wave * 128 + i * 64) * 16), 16,
-                                                     (u / BM * a.T + u % BM) * 16, 0, 0, 0);
-        }
-    };
-    load_sums(sums, 0);
-    load_words(word_next);
-    load(x0, w0);
-    load(x1, w1);
-    load(x2, w2);
+    constexpr std::integral_constant<int, 0> k0;
+    constexpr std::integral_constant<int, 1> k1;
+    constexpr std::integral_constant<int, 2> k2;
+    load_words(word[0]);
+    if constexpr (P == 1) load_words(word[1]);
+    load_sums(w0);
+    load_sums(w1);
+    load(k0, x0, w0);
+    load(k1, x1, w1);
+    load(k2, x2, w2);
     __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * (XLOADS + WLOADS)));
     asm volatile("s_barrier" ::: "memory");
     read_codes(w0);
     read_x(x0, 0, 0);
 #pragma unroll
     for (int r = 0; r < R; ++r) q_next[r] = widen(code_next[r].x);
-    int left = (last - first) * a.pieces;
+    int left = (last - first) * P;
     for (; left >= 3; left -= 3) {
-        step(x0, w0, x1, w1);
-        step(x1, w1, x2, w2);
-        step(x2, w2, x0, w0);
+        step(k0, x0, w0, x1, w1, w2);
+        step(k1, x1, w1, x2, w2, w0);
+        step(k2, x2, w2, x0, w0, w1);
     }
-    if (left >= 1) step(x0, w0, x1, w1);
-    if (left >= 2) step(x1, w1, x2, w2);
+    if constexpr (P == 1) {
+        if (left >= 1) step(k0, x0, w0, x1, w1, w2);
+        if (left >= 2) step(k1, x1, w1, x2, w2, w0);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) add(1, r, s_before[r]);
     __builtin_amdgcn_s_waitcnt(0x0f70);                // no load into LDS outlives the workgroup
@@ -748,33 +777,6 @@ __global__ __launch_bounds__(kManyThreads) __attribute__((amdgpu_waves_per_eu(2,
     // before the loop
     int lane_after = lane;
     asm volatile("" : "+v"(lane_after));
-    __syncthreads();                                   // the stages have been read: they take the sums that are left
-    {
-        constexpr int BUFFERS = TT == 8 ? 7 : 4;
-        const auto buffer = [&](int i) {
-            if (i == 0) return sums;
-            if (TT == 4) return i == 1 ? x0 : i == 2 ? x1 : x2;
-            return (i < 3 ? x0 : i < 5 ? x1 : x2) + (i & 1 ? 0 : 16384);
-        };
-        const int chunks = (g_last - g_first / 4 * 4 + 4 * FOURS - 1) / (4 * FOURS);
-        const auto add_chunk = [&](int i, int chunk) {
-            add_zeros<TT, FOURS>(a, sum, reinterpret_cast<const float *>(buffer(i)), lane_after, nw, g_first / 4 + chunk * FOURS,
-                                 g_first, g_last);
-        };
-        for (int i = 1; i < min(BUFFERS, chunks); ++i) load_sums(buffer(i), i);
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            const int i = chunk % BUFFERS;
-            if (chunk > 0 && i == 0) {                 // all of them have been used
-                __syncthreads();
-                for (int j = 0; j < min(BUFFERS, chunks - chunk); ++j) load_sums(buffer(j), chunk + j);
-            }
-            if (chunk == 1 || (chunk > 0 && i == 0)) {
-                __builtin_amdgcn_s_waitcnt(0x0f70);
-                __syncthreads();
-            }
-            add_chunk(i, chunk);
-        }
-    }
     if (cut_up) {
         floatx4 *to = reinterpret_cast<floatx4 *>(m.parts) + int64_t(rest) * (BM * kManyRows / 4) + lane_after;
 #pragma unroll
@@ -826,51 +828,71 @@ __global__ __launch_bounds__(kManyRows) void join(ManyArgs m) {
     put_four(m.a, (tile - n_tile * m.m_tiles) * (16 * TT) + 16 * tt + 4 * quarter, n_tile * kManyRows + n, v);
 }
 
-// Sums of x over groups of GROUP values, [groups / 4][T][4], and x as bf16 (PIECES: fp32 values as three pieces)
-// in the order in which it is read: [block of 128 values][piece][T][128], zeros behind K.  linear_many's loads are then
-// side by side whatever the stride of x is; a chunk of 2048 rows through 6144 x 4096 took 139 us with x in this order and 146
-// with bf16 rows as they stand.  A lane takes 8 values, GROUP / 8 lanes a group.  Memory: 16.8 MB read and written 7 to 9 us.
+// x as bf16 (PIECES: fp32 values as three pieces) in the order in which it is read, [block of 128 values][piece][T][128], zeros behind
+// K, and its negated sums over groups of GROUP values, [block][part][32 tokens][group of the block][16 tokens][tile of 16] of 8
+// bytes, three bf16 pieces and a zero; of fp32 rows a part of the first pieces and one of what is left of the values.  Two tokens' sums
+// stand in one operand, so all are finite: those behind T are 0, and a group whose sum is not finite has the sum 0 and NaN for
+// x.  linear_many's loads are side by side whatever the stride of x is; a chunk of 2048 rows through 6144 x 4096 took
+// 139 us with x in this order and 146 with bf16 rows as they stand.  A lane takes 8 values, GROUP / 8 lanes a group.
+// Memory: 16.8 MB read and written 7 to 10 us.
 template <int GROUP, bool PIECES>
-__global__ __launch_bounds__(256) void sum_groups(const void *x, int64_t stride, int T, int K, int Kp, float *totals,
+__global__ __launch_bounds__(256) void sum_groups(const void *x, int64_t stride, int T, int K, int Kp, uint2 *totals,
                                               uint16_t *out) {
+    constexpr int PER = kBlock / GROUP, PARTS = PIECES ? 2 : 1;
     const int lanes = Kp / 8;
-    const int64_t all = int64_t(T) * lanes;
+    const int64_t all = int64_t(tokens32(T)) * lanes;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
         const int64_t t = i / lanes;
-        const int k = int(i - t * lanes) * 8;
-        uint16_t *to = out + (int64_t(k / kBlock) * (PIECES ? 3 : 1) * T + t) * kBlock + k % kBlock;
-        float v[8] = {};
+        const int k = int(i - t * lanes) * 8, block = k / kBlock;
+        const bool there = t < T && k < K;
+        uint16_t *to = out + (int64_t(block) * (PIECES ? 3 : 1) * T + t) * kBlock + k % kBlock;
+        float v[PARTS][8] = {};
         if constexpr (PIECES) {
-            if (k < K) {
+            if (there) {
                 const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(x) + t * stride + k);
                 const float4 f = from[0], g = from[1];
-                v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w, v[4] = g.x, v[5] = g.y, v[6] = g.z, v[7] = g.w;
+                v[0][0] = f.x, v[0][1] = f.y, v[0][2] = f.z, v[0][3] = f.w, v[0][4] = g.x, v[0][5] = g.y, v[0][6] = g.z, v[0][7] = g.w;
             }
             uint4 p[3];
-            cut(v, p);
+            cut(v[0], p);
+            if (t < T) {
 #pragma unroll
-            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + j * int64_t(T) * kBlock) = p[j];
+                for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + j * int64_t(T) * kBlock) = p[j];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float first = __uint_as_float(__float_as_uint(v[0][e]) & 0xffff0000u);
+                v[1][e] = v[0][e] - first;
+                v[0][e] = first;
+            }
         } else {
             uint4 w = make_uint4(0u, 0u, 0u, 0u);
-            if (k < K) w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + t * stride + k);
-            *reinterpret_cast<uint4 *>(to) = w;
+            if (there) w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(x) + t * stride + k);
+            if (t < T) *reinterpret_cast<uint4 *>(to) = w;
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[2 * e] = __uint_as_float(u[e] << 16);
-                v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                v[0][2 * e] = __uint_as_float(u[e] << 16);
+                v[0][2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
             }
         }
-        float s = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-        // 4, 8 or 16 lanes of a group, aligned, all of which are here: Kp is a multiple of 128
-        s += __shfl_xor(s, 1);
-        s += __shfl_xor(s, 2);
-        if constexpr (GROUP >= 64) s += __shfl_xor(s, 4);
-        if constexpr (GROUP >= 128) s += __shfl_xor(s, 8);
-        const int g = k / GROUP;
-        if (k % GROUP == 0) totals[(int64_t(g / 4) * T + t) * 4 + g % 4] = s;
-        if (k == Kp - 8)                               // the places behind the last group
-            for (int e = g % 4 + 1; e < 4; ++e) totals[(int64_t(g / 4) * T + t) * 4 + e] = 0.f;
+        bool finite = true;
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+            const float (&f)[8] = v[part];
+            float s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+            // 4, 8 or 16 lanes of a group, aligned, all of which are here: Kp is a multiple of 128
+            s += __shfl_xor(s, 1);
+            s += __shfl_xor(s, 2);
+            if constexpr (GROUP >= 64) s += __shfl_xor(s, 4);
+            if constexpr (GROUP >= 128) s += __shfl_xor(s, 8);
+            finite = finite && fabsf(s) < INFINITY;
+            uint32_t p[3];
+            pieces_of(finite ? -s : 0.f, p);
+            const int64_t at = ((int64_t(block * PARTS + part) * (tokens32(T) / 32) + t / 32) * PER + k % kBlock / GROUP) * 16 + t % 16;
+            if (k % GROUP == 0) totals[at * 2 + t / 16 % 2] = make_uint2(uppers(p[0], p[1]), p[2] >> 16);
+        }
+        if (!finite) *reinterpret_cast<uint4 *>(to) = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
     }
 }
 
@@ -909,7 +931,8 @@ template <int GROUP, int TT>
 void launch_many(const ManyArgs &m, hipStream_t st) {
     const int units = m.whole + (m.tiles - m.whole) * m.splits;
     const int rounds = (units + kManySlots - 1) / kManySlots;
-    hipLaunchKernelGGL((linear_many<GROUP, TT>), dim3(rounds * kManySlots), dim3(kManyThreads), 0, st, m);
+    const auto f = m.a.pieces == 3 ? linear_many<GROUP, TT, 3> : linear_many<GROUP, TT, 1>;
+    hipLaunchKernelGGL(f, dim3(rounds * kManySlots), dim3(kManyThreads), 0, st, m);
     if (m.splits > 1)
         hipLaunchKernelGGL(join<TT>, dim3((m.tiles - m.whole) * (4 * TT)), dim3(kManyRows), 0, st, m);
 }
@@ -934,7 +957,9 @@ struct Plan {
 constexpr int kCUs = 256;
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 size_t x_bytes(int T, int Kp, int pieces) { return up256(size_t(pieces) * T * Kp * 2); }
-size_t sums_bytes(int T, int Kp, int group) { return up256(size_t(T) * ((Kp / group + 3) / 4 * 4) * 4); }
+size_t sums_bytes(int T, int Kp, int group, int pieces) {
+    return up256(size_t(tokens32(T)) * (Kp / group) * (pieces == 3 ? 16 : 8));
+}
 
 // linear_some: how many of the 8 wavefronts go along K, and whether for 16 or 32 rows of the weights.  Workgroups a CU
 // times the steps of a wavefront and one more for its ends; 32 rows take 1.3 times as long as 16.  us, for 8, 4, 2 and 1
@@ -957,12 +982,13 @@ double plan_some(int T, int N, int blocks, int pieces, Plan &p) {
 }
 
 // linear_many: tiles of 64 or 128 tokens, and into how many shares the last of them are cut, by the steps of a CU, 1.2 and
-// 2.1 us each, and the shares' way through memory and their launch.  Whole calls of bf16 rows, us, 64 and 128: 100 x 4096 x
+// 2.0 us each in groups of 128, 1.2 and 2.1 of 64, 1.3 and 2.3 of 32, and the shares' way through memory and their launch.  Whole calls of bf16 rows, us, 64 and 128: 100 x 4096 x
 // 4096 24.1 and 27.6, 512 x 6144 x 4096 42.5 and 46.0, 400 x 14336 x 4096 91.2 and 79.5, 8192 x 6144 x 4096 491 and 443;
 // 85 x 14853 x 328 12.9 uncut and 21.5 in three shares.  Returns an estimate of the time in us, with x's way through
 // memory and two launches.
-double plan_many(int T, int N, int blocks, int pieces, Plan &p) {
+double plan_many(int T, int N, int blocks, int group, int pieces, Plan &p) {
     double least = 0;
+    const double step4 = group == 32 ? 1.3 : 1.2, step8 = group == 32 ? 2.3 : group == 64 ? 2.1 : 2.0;
     for (const int tt : {4, 8}) {
         const int m_tiles = (T + 16 * tt - 1) / (16 * tt), tiles = m_tiles * ((N + kManyRows - 1) / kManyRows);
         const int whole = tiles / kManySlots * kManySlots, rest = tiles - whole;
@@ -972,7 +998,7 @@ double plan_many(int T, int N, int blocks, int pieces, Plan &p) {
             const int share = (blocks + want - 1) / want, splits = (blocks + share - 1) / share;
             const size_t parts = splits > 1 ? size_t(rest) * splits * (16 * tt * kManyRows * 4) : 0;
             const double steps = (double(whole / kManySlots) * blocks + (rest > 0 ? share : 0)) * pieces;
-            const double us = steps * (tt == 4 ? 1.2 : 2.1) + (parts > 0 ? 3 + double(parts) / 4e6 : 0);
+            const double us = steps * (tt == 4 ? step4 : step8) + (parts > 0 ? 3 + double(parts) / 4e6 : 0);
             if (least > 0 && us >= least) continue;
             least = us;
             p.tt = tt, p.m_tiles = m_tiles, p.tiles = tiles, p.whole = whole, p.splits = splits, p.share = share, p.parts = parts;
@@ -1000,11 +1026,11 @@ Plan plan_of(int T, int N, int K, int group, int pieces) {
     if (token_tiles == 1) return p;
     Plan m{};
     m.kind = Plan::kMany;
-    const double many = plan_many(T, N, blocks, pieces, m);
+    const double many = plan_many(T, N, blocks, group, pieces, m);
     const int64_t workgroups = int64_t(token_tiles + 8) * (N / 16 + 8);      // of linear_some, at most
     if (some <= many && workgroups < (int64_t(1) << 31)) return p;
     m.pieces = x_bytes(T, Kp, pieces);
-    m.totals = sums_bytes(T, Kp, group);
+    m.totals = sums_bytes(T, Kp, group, pieces);
     return m;
 }
 
@@ -1033,10 +1059,10 @@ extern "C" size_t apex_linear_w4_workspace_bytes(int T, int N, int K, int group,
     size_t parts = 0;
     for (int t = 64; t - 64 < T; t += 64) {
         Plan p{};
-        plan_many(t, N, blocks, pieces, p);
+        plan_many(t, N, blocks, group, pieces, p);
         parts = std::max(parts, p.parts);
     }
-    return x_bytes(T, Kp, pieces) + sums_bytes(T, Kp, group) + parts;
+    return x_bytes(T, Kp, pieces) + sums_bytes(T, Kp, group, pieces) + parts;
 }
 
 extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, const void *x, int x_type, int T,
@@ -1070,13 +1096,13 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         return apex::fail(APEX_E_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
-                 static_cast<const uint16_t *>(x), x_stride, 0, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
+                 static_cast<const uint16_t *>(x), x_stride, 0, K, bias, residual, y, residual_stride, y_stride, N, T,
                  Kp / kBlock, pieces, y_type == APEX_TYPE_FP32, plan.ways, 1, false};
     if (plan.kind == Plan::kMany) {
         char *ws = static_cast<char *>(workspace);
-        float *totals = reinterpret_cast<float *>(ws + plan.pieces);
+        uint2 *totals = reinterpret_cast<uint2 *>(ws + plan.pieces);
         uint16_t *tiled = reinterpret_cast<uint16_t *>(ws);
-        const int64_t items = int64_t(T) * (Kp / 8);
+        const int64_t items = int64_t(tokens32(T)) * (Kp / 8);
         const dim3 grid(unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)));
         const auto f = pieces > 1 ? (group == 32 ? sum_groups<32, true> : group == 64 ? sum_groups<64, true> : sum_groups<128, true>)
                                   : (group == 32 ? sum_groups<32, false> : group == 64 ? sum_groups<64, false> : sum_groups<128, false>);
@@ -1085,8 +1111,7 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         a.x = tiled;
         a.x_stride = kBlock;
         a.x_piece = int64_t(T) * kBlock;
-        a.x_block = pieces * a.x_piece;
-        const ManyArgs m{a, totals, reinterpret_cast<float *>(ws + plan.pieces + plan.totals), plan.m_tiles, plan.tiles,
+        const ManyArgs m{a, reinterpret_cast<const uint8_t *>(totals), reinterpret_cast<float *>(ws + plan.pieces + plan.totals), plan.m_tiles, plan.tiles,
                          plan.whole, plan.splits, plan.share};
         group == 32 ? launch_many<32>(m, plan.tt, stream) : group == 64 ? launch_many<64>(m, plan.tt, stream)
                                                                         : launch_many<128>(m, plan.tt, stream);

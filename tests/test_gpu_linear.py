@@ -466,3 +466,44 @@ def test_readme_example_runs(torch):
     text = open(os.path.join(root, "README.md")).read()
     code = re.search(r"<!-- example: projection -->\s*```python\n(.*?)```", text, re.S).group(1)
     exec(compile(code, "README.md example", "exec"), {})
+
+
+def shifted_tolerance(group, K, pieces):
+    """2-norm of the error of an fp32 result relative to the result's, for rows of x of any mean m and deviation d.  Of a
+    group the sums go up to g (16 + q) x, 24 g (m^2 + d^2)^(1/2) at most in the root mean square, before the
+    zero points' half, as large, is taken off; on the way there one instruction a 32 values and piece rounds sums that
+    are half of that on average, and twice more round it whole, each by 2^-25 at most, 0.58 of that in the
+    mean: 2^-25 * 0.58 * 24 g (pieces g / 32 / 4 + 2)^(1/2) r for a group, r = (m^2 + d^2)^(1/2).  An instruction
+    may round within its 32 values too, 8 times, which multiplies its share by 8.  Groups' errors are independent, so a row
+    has K / g of them in the square; the result's own size is s (q - z), 4.6 s for uniform codes around z, times r
+    sqrt(K): the quotient has neither r nor K.  The additions over groups round sums no larger than the result, K / g of
+    them, which is 2^-25 * 0.58 (K / g / 2)^(1/2)."""
+    inside = 0.58 * 2.0 ** -25 * 24 * group * (8 * pieces * group / 128 + 2) ** 0.5 / (4.6 * group ** 0.5)
+    over = 0.58 * 2.0 ** -25 * (K / group / 2) ** 0.5
+    return inside + over
+
+
+# T, N, K, group, type of x, in tiles
+SHIFTED = [(300, 2816, 4104, 32, "bf16", True), (300, 2816, 4104, 64, "bf16", True), (300, 2816, 4104, 128, "bf16", True),
+           (2050, 4100, 520, 32, "bf16", True), (64, 14337, 16384, 32, "bf16", True), (100, 6052, 3840, 32, "fp32", True),
+           (100, 6052, 3840, 128, "fp32", True), (1700, 4001, 392, 64, "fp32", True), (65, 4999, 7688, 32, "bf16", False),
+           (129, 3001, 7936, 128, "bf16", False), (100, 2052, 3840, 32, "fp32", False), (4, 3000, 4096, 32, "bf16", False),
+           (1, 3000, 16384, 128, "bf16", False), (2, 3000, 4096, 64, "fp32", False)]
+
+
+@pytest.mark.parametrize("mean,deviation", [(0.0, 1.0), (0.25, 1.0), (1.0, 1.0), (1.0, 0.3), (-10.0, 1.0)])
+@pytest.mark.parametrize("case", SHIFTED, ids=str)
+def test_rows_of_any_mean(torch, case, mean, deviation):
+    """The codes' and the zero points' halves of a result grow with the mean of x, the result does not."""
+    T, N, K, group, x, in_tiles = case
+    c = Large(torch, T, N, K, group, x, "fp32", seed=T)
+    Kp = linear_w4.padded(K)
+    c.w[N * Kp // 2:].view(torch.bfloat16).view(Kp // group, N, 2)[..., 0] = 7.5      # the codes' mean
+    c.x[:, :K] = c.x[:, :K].float() * deviation + mean
+    c.call()
+    torch.cuda.synchronize()
+    assert bool((c.ws[:256] != 0xAB).any()) == in_tiles
+    want, _ = c.reference()
+    rel = np.linalg.norm(c.y[:, :N].double().cpu().numpy() - want) / np.linalg.norm(want)
+    print(rel)
+    assert rel <= shifted_tolerance(group, K, 3 if x == "fp32" else 1), rel

@@ -507,3 +507,36 @@ def test_rows_of_any_mean(torch, case, mean, deviation):
     rel = np.linalg.norm(c.y[:, :N].double().cpu().numpy() - want) / np.linalg.norm(want)
     print(rel)
     assert rel <= shifted_tolerance(group, K, 3 if x == "fp32" else 1), rel
+
+
+def test_a_workspace_serves_fewer_rows_in_tiles(torch):
+    """Of the sizes here the largest T has no shares, smaller ones need up to 33 MB for theirs: the workspace of the largest has room."""
+    N, K, T = 9001, 6000, 700
+    c = Large(torch, T, N, K, 128, "bf16", "fp32", extra=8)
+    x, y = c.x, c.y
+    for c.T in (700, 600, 513, 400, 300, 200, 129, 128, 100, 64, 33):
+        c.x, c.y = x[:c.T], y
+        c.ws[:-64].fill_(0xAB)
+        c.y.fill_(7.0)
+        c.check_rows(c.T)
+        assert (c.ws[:256] != 0xAB).any()
+
+
+def test_two_streams_in_tiles(torch):
+    """Products in tiles with shares, each with a workspace of its own, next to each other."""
+    a = Large(torch, 129, 9001, 6000, 128, "bf16", "fp32", seed=1)
+    b = Large(torch, 100, 6052, 3840, 32, "fp32", "fp32", seed=2)
+    want = []
+    for c in (a, b):
+        c.check()
+        assert c.in_tiles
+        want.append(c.y.clone())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for c in (a, b):
+        c.y.fill_(7.0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.call(streams[0].cuda_stream)
+        b.call(streams[1].cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(a.y, want[0]) and torch.equal(b.y, want[1])

@@ -540,3 +540,94 @@ def test_two_streams_in_tiles(torch):
         b.call(streams[1].cuda_stream)
     torch.cuda.synchronize()
     assert torch.equal(a.y, want[0]) and torch.equal(b.y, want[1])
+
+
+# Products in tiles, without shares and with them, of both types of x
+TILED = [(2048, 4096, 512, 128, "bf16"), (300, 2816, 4104, 64, "bf16"), (100, 6052, 3840, 32, "fp32"), (1700, 4001, 392, 64, "fp32")]
+TILED_IDS = [str(c) for c in TILED]
+
+
+def tiled(torch, case, **kw):
+    """Behind it a workspace of NaN patterns."""
+    c = Large(torch, *case, "fp32", seed=case[0], **kw)
+    c.ws.fill_(0xFF)
+    return c
+
+
+def used(c):
+    assert bool((c.ws[:256] != 0xFF).any()) and bool((c.ws[-64:] == 0xFF).all())
+
+
+@pytest.mark.parametrize("case", TILED, ids=TILED_IDS)
+def test_residual_in_place_in_tiles(torch, case):
+    c = tiled(torch, case, bias=True, residual=True, extra=8)
+    residual = c.r.clone()
+    c.call()
+    used(c)
+    first = c.y.clone()
+    c.compare()
+    c.y = c.r
+    c.call()
+    assert torch.equal(c.r[:, :c.N], first[:, :c.N]) and torch.equal(c.r[:, c.N:], residual[:, c.N:])
+
+
+@pytest.mark.parametrize("case", TILED, ids=TILED_IDS)
+def test_scales_of_any_kind_in_tiles(torch, case):
+    c = tiled(torch, case)
+    N, K, group = c.N, c.K, c.group
+    Kp = linear_w4.padded(K)
+    words = c.w[N * Kp // 2:].view(torch.bfloat16).view(Kp // group, N, 2)
+    z, s = words[..., 0], words[..., 1]
+    s[:, 3], z[:, 3] = 0.0, 0.0
+    s[1, 4] = 0.0
+    s[:, 5] *= -1.0
+    s[:, 6], s[:, 7] = 1e-30, 1e30
+    z[:, 8], z[:, 9] = -3.625, 200.0
+    s[2, 10] = float("nan")
+    z[:, 11], z[:, 12] = 1e-3, 15.9375
+    c.call()
+    used(c)
+    want, size = c.reference()
+    compare(c.y.double().cpu().numpy(), want, size, group, K, c.x_type, "fp32", norm=False)
+    assert (c.y[:, 3] == 0).all() and c.y[:, 10].isnan().all()
+
+
+@pytest.mark.parametrize("case", TILED, ids=TILED_IDS)
+def test_values_of_any_size_in_tiles(torch, case):
+    c = tiled(torch, case)
+    power = np.random.default_rng(1).integers(-90, 100, tuple(c.x.shape))
+    c.x.copy_(c.x.double() * torch.from_numpy(2.0 ** power).cuda())
+    c.call()
+    used(c)
+    want, size = c.reference()
+    compare(c.y.double().cpu().numpy(), want, size, c.group, c.K, c.x_type, "fp32", norm=False)
+    c.x.zero_()
+    c.call()
+    assert (c.y == 0).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("case", TILED, ids=TILED_IDS)
+def test_rows_that_are_not_finite_stay_alone_in_tiles(torch, case, value):
+    c = tiled(torch, case)
+    c.call()
+    used(c)
+    clean = c.y.clone()
+    bad = torch.zeros(c.T, dtype=torch.bool, device="cuda")
+    bad[[0, 17, c.T - 1]] = True
+    c.x[0, 5] = c.x[17, c.K - 1] = c.x[c.T - 1, c.K // 2] = value
+    c.ws.fill_(0xFF)
+    c.call()
+    assert c.y[bad].isnan().all() and torch.equal(c.y[~bad], clean[~bad])
+
+
+# T, N, K, type of x: the most that is staged in LDS whole, and 8 values more
+STAGED = [(4, 700, 5760, "fp32"), (4, 700, 5768, "fp32"), (2, 333, 11520, "fp32"), (2, 333, 11528, "fp32"), (1, 700, 23168, "fp32"),
+          (1, 700, 23176, "fp32"), (1, 5000, 14336, "fp32"), (4, 700, 6016, "bf16"), (4, 700, 6024, "bf16"), (1, 700, 24448, "bf16"),
+          (1, 700, 24456, "bf16"), (4, 5000, 4096, "fp32")]
+
+
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("T,N,K,x", STAGED, ids=[str(c) for c in STAGED])
+def test_rows_that_just_fit_into_lds(torch, T, N, K, x, group):
+    print(Large(torch, T, N, K, group, x, "fp32", bias=True, residual=True, extra=8, seed=T).check())

@@ -20,6 +20,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlock = 128;         // codes of a row that stand together, 64 bytes
+constexpr int kCUs = 256;
 
 struct LinearArgs {
     const uint8_t *codes;
@@ -900,9 +901,11 @@ bool sizes_ok(int N, int K, int group) { return apex_linear_w4_bytes(N, K, group
 
 int padded(int K) { return (K + kBlock - 1) / kBlock * kBlock; }
 
-// Staged rows at most.  fp32 rows that are not staged take a launch more, for their pieces: one row of 14336 (86 KiB)
-// through 4096 rows 11.2 us, 24.8 not staged.  bf16 rows of more than this are as fast in linear_some, whose
-// workgroups have LDS for company: 4 rows of 14336 (115 KiB) 13.0 us and 11.4; 4 of 4096 through 32768 14.7 and 18.1.
+// Staged rows at most; others go through linear_some.  fp32 rows while they fit into LDS, with room for the sums: us, staged and not, one
+// row of 14336 (84 KiB) through 4096 12.5 and 26.9, 4 of 4096 (96 KiB) through 6144 7.8 and 12.0, 4 of 1024 through 2048 4.2
+// and 5.0.  bf16 rows as long as several workgroups fit on a CU: 4 of 4096 (32 KiB) through 32768 13.6 and 18.8, one of
+// 14336 (28 KiB) through 4096 11.9 and 13.1; above, 4 of 8192 (64 KiB) through 700 6.9 and 7.8, but 4 of 14336 (112 KiB)
+// through 4096 14.6 and 13.3.
 constexpr int stage_bytes(Rows rows) { return (rows == kPieces ? 136 : 48) << 10; }
 
 // Whether all of x goes to LDS, and in which rows.
@@ -911,11 +914,13 @@ bool stages(int T, int K, int pieces, Rows *rows) {
     return T <= 4 && int64_t(staged_rows(*rows, T)) * (padded(K) * 2 + kPad) <= stage_bytes(*rows);
 }
 
+// Workgroups that stay, 3 a CU at most: with 256, 512, 768, 1280 and 2048 of them 4 rows through 32768 x 4096 take 17.7, 15.6, 15.4, 16.7
+// and 17.0 us, through 60000 x 1024 9.7, 8.1, 8.0, 9.0 and 9.6.
 template <int GROUP, int R, int ROWS>
 void launch_few(const LinearArgs &a, hipStream_t st) {
     const size_t lds = staged_rows(ROWS, a.T) * (a.blocks * 256 + kPad) + 2 * 4 * (kWaves * R * 64);
     const int tiles = (a.N + 16 * R - 1) / (16 * R);
-    hipLaunchKernelGGL((linear_few<GROUP, R, ROWS>), dim3(std::min((tiles + 7) / 8 * 8, 768)), dim3(64 * kWaves), lds, st, a);
+    hipLaunchKernelGGL((linear_few<GROUP, R, ROWS>), dim3(std::min((tiles + 7) / 8 * 8, 3 * kCUs)), dim3(64 * kWaves), lds, st, a);
 }
 
 template <int GROUP, int R, int TT, int P>
@@ -954,7 +959,6 @@ struct Plan {
     size_t bytes() const { return pieces + totals + parts; }
 };
 
-constexpr int kCUs = 256;
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 size_t x_bytes(int T, int Kp, int pieces) { return up256(size_t(pieces) * T * Kp * 2); }
 size_t sums_bytes(int T, int Kp, int group, int pieces) {
@@ -1103,6 +1107,7 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
         uint2 *totals = reinterpret_cast<uint2 *>(ws + plan.pieces);
         uint16_t *tiled = reinterpret_cast<uint16_t *>(ws);
         const int64_t items = int64_t(tokens32(T)) * (Kp / 8);
+        // workgroups at most: any number from 1024 on takes as long (2048 rows of 4096 10.2, 9.5 with 4096 of them and 9.8 so)
         const dim3 grid(unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)));
         const auto f = pieces > 1 ? (group == 32 ? sum_groups<32, true> : group == 64 ? sum_groups<64, true> : sum_groups<128, true>)
                                   : (group == 32 ? sum_groups<32, false> : group == 64 ? sum_groups<64, false> : sum_groups<128, false>);

@@ -41,6 +41,7 @@ struct Turn {
 // sum of two 64-bit numbers whose rounding errors are carried along, less its nearest quarter: at most an eighth of a
 // turn, where the series end with x^11 and x^12 (the next terms are below 2^-36), and rounded to 32 bits at the very end.
 __device__ __forceinline__ void fill_table(const Turn &a, int p, float2 *table) {
+#pragma clang fp contract(off)      // `turns` is a rounded product: made one with the difference from `whole`, its error counts twice
     constexpr double kHi = 0x1.45f306dc9c883p-3, kLo = -0x1.6b01ec5417056p-57;       // 1 / (2 pi)
     for (int i = threadIdx.x; i < a.dim / 2; i += kThreads) {
         const double f = a.freq[i], angle = p * f, turns = angle * kHi;

@@ -5,6 +5,8 @@ for any position), the smaller of the two products of a turned value and its sum
 turned value is off by less than 2^-22 of |amplitude| (|a| + |b|).  Rounding to bf16 adds half a step, 2^-8 of the value.
 An E4M3 code is within half a step of the value: 2^-4 of it, or 2^-10 of the scale near 0.
 """
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
@@ -404,3 +406,30 @@ def test_attention_block_from_the_residual_stream(torch):
         assert np.linalg.norm(got[:t] - want[:t]) <= 2.0 ** -11 * np.linalg.norm(want[:t] - x[:t])
         assert np.array_equal(got[t:], x[t:])          # rows behind the last token: the residual alone
     assert seq.tolist() == done
+
+
+def cosines_and_sines(pos, f):
+    """Of exact products, with 2 pi to 48 digits: float64, off by its own rounding."""
+    turn = 2 * Fraction("3.14159265358979323846264338327950288419716939937510")
+    angle = np.array([[float(Fraction(int(p)) * Fraction(float(w)) % turn) for w in f] for p in pos])
+    return np.concatenate([np.cos(angle), np.sin(angle)], 1)
+
+
+@pytest.mark.parametrize("far", [1 << 20, 1 << 31])
+@pytest.mark.parametrize("amplitude", [1.0, 1.35, 0.7, -3.3])
+def test_sines_times_the_amplitude_are_rounded_once(torch, amplitude, far):
+    """Pairs (1, 0) come out as amplitude times cosine and sine, to within half a step of fp32 of the value, which is 2^-24 and not
+    2^-25 from 1 on, and 2^-36 of the amplitude, whatever the position."""
+    T, dim = 200, 128
+    pos = np.random.default_rng(9).integers(0, far, T)
+    pos[:3] = 0, 1, far - 1
+    rot, f, keep, a = rotation(torch, "half", dim, amplitude=amplitude)
+    x = torch.zeros(T, dim, device="cuda")
+    x[:, :dim // 2] = 1.0
+    native.apex_rotary(rot, x, "fp32", T, 1, dim, dim, i32(torch, pos), x, dim)
+    want = a * cosines_and_sines(pos, f)
+    err = np.abs(x.double().cpu().numpy() - want)
+    step = np.spacing(np.abs(want).astype(np.float32)).astype(np.float64)
+    assert (err <= step / 2 + abs(a) * (2.0 ** -36 + 2.0 ** -50)).all(), ((err - step / 2) / abs(a)).max()
+    if abs(amplitude) > 1:
+        assert err.max() > 2.0 ** -25

@@ -483,8 +483,9 @@ apex_status apex_attention_paged(const apex_paged_cache *cache, const void *q, i
  *   APEX_ROPE_HALF         values i and i + dim / 2
  *   APEX_ROPE_INTERLEAVED  values 2 i and 2 i + 1
  * f_i are radians per position in 64 bits (apex_rotary_frequencies, or a caller's own; negated they
- * turn back).  Angles, their cosines and sines are computed in 64 bits and more, to the same error of
- * at most 2^-25 at any position; products are fp32, the result is rounded once to the rows' type.
+ * turn back).  Angles, and amplitude times their cosines and sines, are computed in 64 bits and more,
+ * to within 2^-36 of the amplitude at any position, and rounded once to fp32; products are fp32, the
+ * result is rounded once to the rows' type.
  *   dim        a multiple of 16, at most the head's size
  *   freq       device double [dim / 2];  amplitude  finite (1 as a rule)
  * The struct is read during the call only.

@@ -5,11 +5,14 @@
 // the token's angles, one angle each, in 64 bits and rounded once.  Then lane l of a head's hd / 8
 // holds 8 values: four pairs of the table where l < dim / 8, else 8 values that stay as they are.
 // Every head of a token uses the same table, so an angle costs its share of H + G heads; what remains
-// is one read and one write of every value, 4.9 to 5.2 TB/s of both from memory: 8192 rows of 32
-// heads of 64 in fp32, 134 MB, 27.4 us; 8192 of 32 + 2 x 8 heads of 128 in fp32 with E4M3 pages, 353
-// MB, 68.  Four tokens a workgroup took 31.6 and 82.9: a head's 16-byte accesses then stood 32 bytes
-// apart.  Loads and stores past the caches take 27.1 where rows come from memory, but 26.3 instead
-// of 20.7 where a projection has just written them.
+// is one read and one write of every value, 4.8 to 5.2 TB/s of both from memory: 8192 rows of 32
+// heads of 64 in fp32 or of 128 in bf16, 134 MB, 27.5 us; 8192 of 32 + 2 x 8 heads of 128 in fp32
+// with E4M3 pages, 353 MB, 67.5, in bf16 with bf16 pages, 201 MB, 39.  Two and four tokens a
+// workgroup, their tables side by side, took 29.8 and 32.2 for the 27.5, 71 and 74 for the 67.5 and
+// 47 and 46 for the 39.  With few heads, whose lanes leave most of a workgroup idle, they would
+// be faster: 8192 bf16 rows of 3 heads of 64 7.1 us, 5.6 and 4.8; stored, of 4 + 2 x 1 heads of 128 9.8,
+// 9.5 and 8.8.  Loads and stores past the caches take 27.1 where rows come from memory, but 26.3
+// instead of 20.7 where a projection has just written them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -39,7 +42,8 @@ struct Turn {
 
 // cos and sin (times the amplitude) of the angles of position p, dim / 2 of them.  An angle is turns = p f / (2 pi), as the
 // sum of two 64-bit numbers whose rounding errors are carried along, less its nearest quarter: at most an eighth of a
-// turn, where the series end with x^11 and x^12 (the next terms are below 2^-36), and rounded to 32 bits at the very end.
+// turn, where the series end with x^11 and x^12 (the next terms are below 2^-36), times the amplitude, and rounded to 32 bits at
+// the very end.
 __device__ __forceinline__ void fill_table(const Turn &a, int p, float2 *table) {
 #pragma clang fp contract(off)      // `turns` is a rounded product: made one with the difference from `whole`, its error counts twice
     constexpr double kHi = 0x1.45f306dc9c883p-3, kLo = -0x1.6b01ec5417056p-57;       // 1 / (2 pi)
@@ -219,7 +223,8 @@ apex_status check_rotation(const char *fn, const apex_rotation *r, int hd, bool 
     return APEX_OK;
 }
 
-// A workgroup a token; of few tokens the heads over several.
+// A workgroup a token; of few tokens the heads over several, up to 512 workgroups in all: 32 rows of 40 heads of 128 take
+// 2.9 us with any number from 256 to 4096, 3.4 with a workgroup a token.
 dim3 grid_of(int T, int heads, int rows) {
     return dim3(unsigned(T), unsigned(std::min((heads + rows - 1) / rows, std::max(1, 512 / T))));
 }

@@ -532,7 +532,8 @@ apex_status apex_rotary_frequencies(int dim, double base, int scaling, double fa
 /*
  * Rotary positions of T rows of `heads` heads (queries and keys that stand side by side are one row).
  *   x, out      device, type `dtype` (apex_type): row t's [heads, hd] at x + t * x_stride; strides in
- *               values, at least heads * hd and multiples of 16 bytes; out may be x (same stride)
+ *               values, at least heads * hd and multiples of 16 bytes; out may be x (same stride), its
+ *               rows may overlap no others of x (refused)
  *   positions   device int32 [T]: a row whose position is negative is left out (its row of out
  *               stays as it is)
  *   hd          a multiple of 8, at most 1024
@@ -547,7 +548,8 @@ apex_status apex_rotary(const apex_rotation *rotation, const void *x, int dtype,
  * projection's rows.  Turned keys are fp32 until the pool's own rounding (bf16, or E4M3 with the
  * scale of the turned row), the rest is as in apex_paged_store and apex_rotary.
  *   q, q_out    device, type `dtype`: row t's [H, hd] at q + t * q_stride; q_out may be q (same
- *               stride).  H >= 0: with 0, keys and values only, q and q_out may be NULL
+ *               stride), its rows may overlap no others of q and none of k and v (refused).  H >= 0:
+ *               with 0, keys and values only, q and q_out may be NULL
  *   k, v, slot_map   as in apex_paged_store
  *   positions   device int32 [T]: a token whose position is negative is left out, queries, keys and
  *               values; one whose slot is outside of the pool has its queries turned, nothing stored
@@ -578,8 +580,9 @@ apex_status apex_paged_store_rotary(const apex_paged_cache *cache, const apex_ro
  *           and a multiple of 16 bytes
  *   bias    device fp32 [N], or NULL
  *   residual  device, type `y_type`, row t's [N] at residual + t * residual_stride (at least N), or
- *           NULL; may be y (same stride)
- *   y       device, type `y_type` out: row t's [N] at y + t * y_stride (at least N); may not overlap x
+ *           NULL; may be y (same stride), else its rows may not overlap those of y (refused)
+ *   y       device, type `y_type` out: row t's [N] at y + t * y_stride (at least N); its rows may not
+ *           overlap those of x (refused)
  *   T       rows, at most APEX_MAX_STEP_TOKENS
  *   workspace  device, >= apex_linear_w4_workspace_bytes(T, N, K, group, x_type) bytes, which serve any
  *           smaller T too (0, and workspace may be NULL, up to 32 rows of bf16 or 16 of fp32); must not

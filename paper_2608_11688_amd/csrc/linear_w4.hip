@@ -1091,13 +1091,18 @@ extern "C" apex_status apex_linear_w4(const void *w, int N, int K, int group, co
                      apex::aligned16(residual) && apex::aligned16(workspace),
                  "%s: pointers must be 16-byte aligned", fn);
     APEX_REQUIRE(residual != y || residual_stride == y_stride, "%s: y is the residual with another stride", fn);
-    APEX_REQUIRE(x != y, "%s: y is x", fn);
     const int Kp = padded(K), pieces = x_type == APEX_TYPE_FP32 ? 3 : 1;
     const Plan plan = plan_of(T, N, K, group, pieces);
     const size_t need = plan.bytes();
     APEX_REQUIRE(need == 0 || workspace, "%s: NULL workspace", fn);
     if (workspace_bytes < need)
         return apex::fail(APEX_E_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
+    const int64_t x_size = x_type == APEX_TYPE_FP32 ? 4 : 2, y_size = y_type == APEX_TYPE_FP32 ? 4 : 2;
+    const apex::Rows y_rows{y, y_stride * y_size, N * y_size};
+    APEX_REQUIRE(!apex::rows_overlap(y_rows, {x, x_stride * x_size, K * x_size}, T), "%s: rows of y overlap rows of x", fn);
+    APEX_REQUIRE(!residual || residual == y ||
+                     !apex::rows_overlap(y_rows, {residual, residual_stride * y_size, N * y_size}, T),
+                 "%s: rows of y overlap others of the residual", fn);
     LinearArgs a{static_cast<const uint8_t *>(w),
                  reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(w) + size_t(N) * (Kp / 2)),
                  static_cast<const uint16_t *>(x), x_stride, 0, K, bias, residual, y, residual_stride, y_stride, N, T,

@@ -279,6 +279,9 @@ extern "C" apex_status apex_rotary(const apex_rotation *rotation, const void *x,
     APEX_REQUIRE(x && positions && out, "%s: NULL pointer", fn);
     APEX_REQUIRE(apex::aligned16(x) && apex::aligned16(out) && aligned4(positions), "%s: misaligned pointer", fn);
     APEX_REQUIRE(x != out || x_stride == out_stride, "%s: out is x with another stride", fn);
+    const int64_t size = dtype == APEX_TYPE_FP32 ? 4 : 2, row = int64_t(heads) * hd * size;
+    APEX_REQUIRE(x == out || !apex::rows_overlap({x, x_stride * size, row}, {out, out_stride * size, row}, T),
+                 "%s: rows of out overlap others of x", fn);
     const RotaryArgs a{{rotation->freq, positions, rotation->amplitude, rotation->dim, T}, const_cast<void *>(x),
                        out, x_stride, out_stride, heads, hd};
     const bool inter = rotation->layout == APEX_ROPE_INTERLEAVED;
@@ -316,6 +319,14 @@ extern "C" apex_status apex_paged_store_rotary(const apex_paged_cache *cache, co
                      (H == 0 || (apex::aligned16(q) && apex::aligned16(q_out))),
                  "%s: misaligned pointer", fn);
     APEX_REQUIRE(H == 0 || q != q_out || q_stride == q_out_stride, "%s: q_out is q with another stride", fn);
+    if (H > 0) {
+        const int64_t size = dtype == APEX_TYPE_FP32 ? 4 : 2, q_row = int64_t(H) * hd * size, row = int64_t(G) * hd * size;
+        const apex::Rows out{q_out, q_out_stride * size, q_row};
+        APEX_REQUIRE(q == q_out || !apex::rows_overlap(out, {q, q_stride * size, q_row}, T),
+                     "%s: rows of q_out overlap others of q", fn);
+        APEX_REQUIRE(!apex::rows_overlap(out, {k, k_stride * size, row}, T) && !apex::rows_overlap(out, {v, v_stride * size, row}, T),
+                     "%s: rows of q_out overlap rows of k or v", fn);
+    }
     const StoreArgs a{{rotation->freq, positions, rotation->amplitude, rotation->dim, T}, const_cast<void *>(q),
                       const_cast<void *>(k), const_cast<void *>(v), q_out,
                       q_stride, k_stride, v_stride, q_out_stride, slot_map, cache->k_pages, cache->v_pages,

@@ -631,3 +631,23 @@ STAGED = [(4, 700, 5760, "fp32"), (4, 700, 5768, "fp32"), (2, 333, 11520, "fp32"
 @pytest.mark.parametrize("T,N,K,x", STAGED, ids=[str(c) for c in STAGED])
 def test_rows_that_just_fit_into_lds(torch, T, N, K, x, group):
     print(Large(torch, T, N, K, group, x, "fp32", bias=True, residual=True, extra=8, seed=T).check())
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_rows_between_others(torch, T):
+    """Results between the rows of x and of the residual, in the same buffers: not refused, and right."""
+    c = Large(torch, T, 264, 512, 64, "fp32", "fp32", residual=True)
+    c.call()
+    want = c.y.clone()
+    wide = torch.cat([c.x, c.y], 1)
+    c.x, c.y = wide[:, :512], wide[:, 512:]
+    c.y.fill_(7.0)
+    c.call()
+    assert torch.equal(c.y, want)
+    both = torch.cat([c.r, c.r], 1)
+    c.r, c.y = both[:, 264:], both[:, :264]
+    c.call()
+    assert torch.equal(c.y, want) and torch.equal(c.x, wide[:, :512])
+    c.r = both[:, 4:268]
+    with pytest.raises(native.ApexError):
+        c.call()

@@ -433,3 +433,22 @@ def test_sines_times_the_amplitude_are_rounded_once(torch, amplitude, far):
     assert (err <= step / 2 + abs(a) * (2.0 ** -36 + 2.0 ** -50)).all(), ((err - step / 2) / abs(a)).max()
     if abs(amplitude) > 1:
         assert err.max() > 2.0 ** -25
+
+
+def test_rows_between_others(torch):
+    """Results between the rows of a call's own inputs, in the same buffer: not refused, and right."""
+    T, H, hd = 5, 3, 64
+    n = H * hd
+    wide = torch.randn(T, 2 * n, device="cuda")
+    x, out = wide[:, :n], wide[:, n:]
+    rot, f, keep, a = rotation(torch, "half", hd)
+    pos = i32(torch, np.arange(T) * 7)
+    want = torch.empty(T, n, device="cuda")
+    native.apex_rotary(rot, x, "fp32", T, H, hd, 2 * n, pos, want, n)
+    before = x.clone()
+    native.apex_rotary(rot, x, "fp32", T, H, hd, 2 * n, pos, out, 2 * n)
+    assert torch.equal(out, want) and torch.equal(x, before)
+    native.apex_rotary(rot, x[:1], "fp32", 1, H, hd, 2 * n, pos, out[:1], 4 * n)       # one row: strides do not count
+    assert torch.equal(out, want)
+    with pytest.raises(native.ApexError):
+        native.apex_rotary(rot, x, "fp32", T, H, hd, 2 * n, pos, wide[:, 4:], 2 * n)

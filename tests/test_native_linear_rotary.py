@@ -200,3 +200,28 @@ def test_linear_workspace():
     for N, K, group, x in ((96, 256, 64, "fp32"), (4096, 4096, 32, "bf16"), (259, 3968, 128, "fp32"), (25083, 520, 64, "bf16")):
         sizes = [f(T, N, K, group, x) for T in range(1, 3000)]
         assert sizes[:16] == [0] * 16 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+# ------------------------------------------------------------------------------ rows that overlap
+@pytest.mark.parametrize("kw", [
+    dict(y=A + 16), dict(y=A + 3 * 512 + 496), dict(y=A - 48, T=1), dict(y=A - 176), dict(x=A, xs=512, y=A + 512, ys=512),
+    dict(y=A + 160, ys=100), dict(r=2 * A + 16, rs=96), dict(r=2 * A - 16, rs=96), dict(r=2 * A + 64, rs=200),
+    dict(r=2 * A + 176, rs=96, T=1)], ids=str)
+def test_linear_refuses_rows_that_overlap(kw):
+    """x: 4 bf16 rows of 512 bytes from A on; y: 4 bf16 rows of 192 bytes."""
+    refused(INVAL, project, **dict(dict(y=3 * A), **({"y": 2 * A} if "r" in kw else {}), **kw))
+
+
+@pytest.mark.parametrize("kw", [dict(out=A + 16), dict(out=A - 16), dict(out=A + 2048), dict(out=A + 3 * 2048 + 2032), dict(out=A + 1024, os=4096),
+                                dict(xs=2048, os=2048, out=A + 2032), dict(T=1, out=A + 2032)], ids=str)
+def test_rotary_refuses_rows_that_overlap(kw):
+    """4 rows of 2048 bytes from A on."""
+    refused(INVAL, rotate, **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(out=A + 16), dict(out=A + 8192), dict(k=A * 200 + 8192 - 16, out=A * 200), dict(v=A * 200 + 16, out=A * 200),
+                                dict(k=A * 200 + 3 * 8192 + 8176, out=A * 200), dict(qs=6144, os=6144, out=A + 4096, q=A, k=A + 8192 + 2048)],
+                         ids=str)
+def test_store_refuses_rows_that_overlap(kw):
+    """Queries: 4 rows of 8192 bytes from A on; keys and values: of 2048."""
+    refused(INVAL, store, **dict(dict(k=A * 100, v=A * 150), **kw))

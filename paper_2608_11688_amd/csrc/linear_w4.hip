@@ -236,9 +236,9 @@ constexpr int staged_rows(int rows, int T) { return rows == kPieces ? 3 * T : T;
 
 // Up to 4 rows: all of x goes to LDS first, at most stage_bytes() of it, and the weights are read once, by workgroups that
 // stay.  The wavefronts join their sums in LDS in a fixed order.  A long stream is bound by memory: 4 rows through
-// 32768 x 4096 in groups of 32, 84 MB, 14.5 us, 5.8 TB/s, what a kernel that only reads gets.  A short one by the way
-// of a launch, x and the first weights one behind the other: one fp32 row through 6144 x 4096, 13.4 MB, 5.9 us, through
-// 2048 x 1024 3.4.
+// 32768 x 4096 in groups of 32, 84 MB, 14.6 us, 5.8 TB/s, where the last-level cache holds the weights (a kernel that only reads 13.3),
+// 19 from memory, 4.4 TB/s (15.4).  A short one by the way of a launch, x and the first weights one behind the other: one fp32
+// row through 6144 x 4096, 13.4 MB, 5.9 us, through 2048 x 1024 3.3.
 template <int GROUP, int R, int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void linear_few(LinearArgs a) {
     extern __shared__ uint4 lds[];

@@ -986,10 +986,9 @@ double plan_some(int T, int N, int blocks, int pieces, Plan &p) {
 }
 
 // linear_many: tiles of 64 or 128 tokens, and into how many shares the last of them are cut, by the steps of a CU, 1.2 and
-// 2.0 us each in groups of 128, 1.2 and 2.1 of 64, 1.3 and 2.3 of 32, and the shares' way through memory and their launch.  Whole calls of bf16 rows, us, 64 and 128: 100 x 4096 x
-// 4096 24.1 and 27.6, 512 x 6144 x 4096 42.5 and 46.0, 400 x 14336 x 4096 91.2 and 79.5, 8192 x 6144 x 4096 491 and 443;
-// 85 x 14853 x 328 12.9 uncut and 21.5 in three shares.  Returns an estimate of the time in us, with x's way through
-// memory and two launches.
+// 2.0 us each in groups of 128, 1.2 and 2.1 of 64, 1.3 and 2.3 of 32, and the shares' way through memory and their launch.  Whole calls of bf16 rows in groups of
+// 64, us, 64 and 128: 100 x 4096 x 4096 24.7 and 26.3, 512 x 6144 x 4096 53.0 and 53.1, 400 x 14336 x 4096 95.6 and 79.1, 8192 x 6144 x
+// 4096 611 and 527.  Returns an estimate of the time in us, with x's way through memory and two launches.
 double plan_many(int T, int N, int blocks, int group, int pieces, Plan &p) {
     double least = 0;
     const double step4 = group == 32 ? 1.3 : 1.2, step8 = group == 32 ? 2.3 : group == 64 ? 2.1 : 2.0;
@@ -1012,10 +1011,11 @@ double plan_many(int T, int N, int blocks, int group, int pieces, Plan &p) {
 }
 
 // Up to 32 rows of bf16 and 16 of fp32, a tile of linear_some, take no workspace.  Of more rows linear_some reads the
-// weights once for every tile, linear_many is two or three launches; us, some and many: bf16 rows, 239 x 12103 x 1312
-// 30.7 and 21.7, 45 x 14783 x 2728 20.1 and 22.7, 249 x 3266 x 3736 25.9 and 28.0, 56 x 854 x 7008 10.0 and 32.5; fp32 rows,
-// 298 x 669 x 3328 17.7 and 28.6, 24 x 8081 x 5120 22.5 and 30.0, 301 x 1361 x 5976 54.6 and 38.6, 104 x 69 x 3200 8.1 and
-// 21.1.  Of 69 calls of mixed sizes the estimates took the slower way three times, by 0.6 us at most.
+// weights once for every tile, linear_many is two or three launches; us in groups of 64, some and many: bf16 rows, 239 x 12103 x 1312
+// 31.1 and 23.9, 45 x 14783 x 2728 20.1 and 23.2, 249 x 3266 x 3736 22.0 and 25.1, 56 x 854 x 7008 9.7 and 21.4; fp32 rows,
+// 298 x 669 x 3328 16.1 and 25.5, 24 x 8081 x 5120 21.5 and 31.0, 301 x 1361 x 5976 47.4 and 37.8, 104 x 69 x 3200 7.6 and
+// 15.9.  Of 200 calls of mixed sizes, types and groups the estimates took a way that is slower by more than a twentieth six
+// times, by 4.9 us at most.
 Plan plan_of(int T, int N, int K, int group, int pieces) {
     Plan p{};
     const int Kp = padded(K), blocks = Kp / kBlock;

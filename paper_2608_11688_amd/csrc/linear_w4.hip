@@ -986,9 +986,10 @@ double plan_some(int T, int N, int blocks, int pieces, Plan &p) {
 }
 
 // linear_many: tiles of 64 or 128 tokens, and into how many shares the last of them are cut, by the steps of a CU, 1.2 and
-// 2.0 us each in groups of 128, 1.2 and 2.1 of 64, 1.3 and 2.3 of 32, and the shares' way through memory and their launch.  Whole calls of bf16 rows in groups of
-// 64, us, 64 and 128: 100 x 4096 x 4096 24.7 and 26.3, 512 x 6144 x 4096 53.0 and 53.1, 400 x 14336 x 4096 95.6 and 79.1, 8192 x 6144 x
-// 4096 611 and 527.  Returns an estimate of the time in us, with x's way through memory and two launches.
+// 2.0 us each in groups of 128, 1.2 and 2.1 of 64, 1.3 and 2.3 of 32, and the shares' way through memory and their launch.
+// Whole calls of bf16 rows in groups of 64, us, 64 and 128: 100 x 4096 x 4096 24.7 and 26.3, 512 x 6144 x 4096 53.0 and 53.1,
+// 400 x 14336 x 4096 95.6 and 79.1, 8192 x 6144 x 4096 611 and 527.  Returns an estimate of the time in us, with x's way
+// through memory and two launches.
 double plan_many(int T, int N, int blocks, int group, int pieces, Plan &p) {
     double least = 0;
     const double step4 = group == 32 ? 1.3 : 1.2, step8 = group == 32 ? 2.3 : group == 64 ? 2.1 : 2.0;
